@@ -16,6 +16,9 @@
  *   pk_window_pattern     Sec. 3.1 "Decoding Stage", Eq. 5: the pattern of a window of
  *                         vectors (per-channel Chebyshev centre)
  *   pk_dequantize         the reconstruction rule below Eq. 6 (debug / parity)
+ *   pk_fp8_append, pk_fp8_attention, pk_fp8_weights, pk_fp8_evict
+ *                         a cache of 8-bit codes with a scale per block of tokens, for
+ *                         what 2 or 4 bits do not serve (its own section below)
  *
  * Conventions shared by every call
  *   - All tensor pointers are DEVICE pointers unless marked "host".  Structs
@@ -375,6 +378,142 @@ pk_status pk_window_pattern(const void *x, int64_t set_stride, int32_t n_sets, i
 pk_status pk_dequantize(const pk_config *cfg, const pk_cache *cache, const pk_state *state,
                         const void *patterns_k, const void *patterns_v, int32_t t0, int32_t t1,
                         float *k_out, float *v_out, void *stream);
+
+/*
+ * An 8-bit cache without pattern tables, for layers or models where 2 or 4 bits lose too much: append, attention of one or
+ * several query tokens per sequence, the attention weight that every cached token received, and eviction by it.
+ *
+ * Format
+ *   k_codes, v_codes [N][t_capacity][d] uint8   e4m3 (sign, 4 bits of exponent with bias 7, 3 of mantissa; no infinities,
+ *                                               0x7f / 0xff are NaN)
+ *   k_scale, v_scale [N][t_capacity/block] float  scale of `block` consecutive tokens of one stream: the smallest power of
+ *                                               two 2^e, e >= -126, with max |x| <= 448 * 2^e over the finite values that were
+ *                                               put into the block.  The sign bit is set where the block holds a NaN code.
+ *   pos    [N][t_capacity] int32                position of every cached token in its text
+ *   weight [N][t_capacity] float                attention weight accumulated by pk_fp8_weights; may be NULL
+ *   x = code * |scale|.  An infinite or NaN value is stored as NaN; the others of its block are stored as if it were not there.
+ *   A power of two costs e4m3 nothing (its relative step is the same at every power of two) and x / 2^e is exact, so every code
+ *   is the nearest one, ties to even.  A block that is filled in several appends keeps one scale: where a later vector needs a
+ *   larger one, the codes already there are rounded to it (exact but for values under 2^-6 of the new scale).
+ * Paged: with page_tokens > 0 the code and scale arrays hold n_pages pages of [n_kv_heads][page_tokens] tokens, token t of
+ *   stream (seq, head) in row (page_table[seq][t / page_tokens] * n_kv_heads + head) * page_tokens + t % page_tokens; entries
+ *   are clamped to the pool.  pos and weight stay per stream.
+ * States: DEVICE int32 [n_seq][4], 16-byte aligned: tokens held, position of the next token, 0, 0 of every sequence (all zeros
+ *   for an empty cache).  The kernels read it when they run, so a captured graph can be replayed while sequences grow; the
+ *   number of tokens held is clamped to [0, t_capacity].  The third word counts an append's workgroups while it runs
+ *   and is 0 between calls.
+ * counts: optional DEVICE int32 [n_seq]: a sequence uses the first counts[i] of the n tokens of the call (clamped to [0, n]);
+ *   NULL: all of them.  Rows past a sequence's count are neither read nor written.
+ * Tensors of vectors are addressed by three strides in elements; the d elements of a vector are contiguous.  Strides are
+ *   multiples of 8, pointers 16-byte aligned.
+ * Calls enqueue on `stream` and return; errors are found on the host before anything is launched, as everywhere above.
+ * Appends and evictions change their cache: calls that touch the same cache belong on one stream.
+ */
+typedef enum { PK_DTYPE_FP16 = 0, PK_DTYPE_BF16 = 1 } pk_dtype;
+
+typedef enum { PK_FP8_OP_ATTENTION = 0, PK_FP8_OP_EVICT = 1 } pk_fp8_op;
+
+typedef struct {
+    int32_t n_seq;       /* >= 1; n_seq * n_kv_heads at most 65535                                     */
+    int32_t n_kv_heads;  /* >= 1                                                                       */
+    int32_t n_q_heads;   /* multiple of n_kv_heads, at most 64 of them per KV head                     */
+    int32_t head_dim;    /* 64, 96, 128 or 256                                                         */
+    int32_t block;       /* tokens per scale: 32, 64 or 128                                            */
+    int32_t t_capacity;  /* tokens per stream, a multiple of block and of 64, at most 2^25             */
+    int32_t dtype;       /* pk_dtype of vectors, queries and outputs                                   */
+    int32_t page_tokens; /* 0, or a power of two >= 128 that divides t_capacity                        */
+    int32_t n_pages;     /* pages in the pool (page_tokens > 0), >= 1                                  */
+} pk_fp8_config;
+
+typedef struct {
+    uint64_t k_codes, v_codes, k_scale, v_scale, pos, weight;
+    uint64_t total; /* sum of the above, each rounded up to `align` */
+    uint32_t align; /* required alignment of every array (16)       */
+} pk_fp8_layout;
+
+typedef struct {
+    void *k_codes, *v_codes;
+    float *k_scale, *v_scale;
+    int32_t *pos;
+    float *weight;             /* NULL: not tracked                                                    */
+    const int32_t *page_table; /* DEVICE int32 [n_seq][t_capacity / page_tokens] when page_tokens > 0  */
+} pk_fp8_cache;
+
+/* Elements between sequences, tokens and heads of a tensor of vectors. */
+typedef struct {
+    int64_t seq, token, head;
+} pk_strides;
+
+/* What is done to the scores.  s = softmax_scale * q.k; cap > 0: s = cap * tanh(s / cap); slopes: s -= slopes[query head] *
+ * (pos of the query - pos of the key); window > 0: keys `window` or more positions back are masked. */
+typedef struct {
+    float softmax_scale;
+    float cap;
+    int32_t window;
+    const float *slopes; /* DEVICE float [n_q_heads] or NULL */
+} pk_fp8_scores;
+
+/* Byte sizes of the arrays.  Host-only. */
+pk_status pk_fp8_cache_layout(const pk_fp8_config *cfg, pk_fp8_layout *out /* host, out */);
+
+/*
+ * Bytes of workspace.  PK_FP8_OP_ATTENTION: a = n_query, b = bound of the call (0 where the call needs none; not monotonic in a:
+ * many query tokens fill the chip without splitting the keys).  PK_FP8_OP_EVICT: a = budget, cfg = the source's.  0 for an invalid
+ * configuration or negative a, b.  Host-only.
+ */
+size_t pk_fp8_workspace_bytes(const pk_fp8_config *cfg, pk_fp8_op op, int64_t a, int64_t b);
+
+/*
+ * Append n_new (counts[i]) vectors per stream behind the tokens that are there, at the next positions of their sequences, with
+ * weight 0.  Vectors that would exceed t_capacity are left out: the state tells how many are held.
+ *   states      DEVICE, in; states_out: DEVICE, out: the states afterwards.  NULL or `states` itself: in place.  Otherwise the two
+ *               must not overlap, and `states` stays as it is: a caller that verifies drafts can go back to it (an append to the
+ *               shorter state overwrites the tokens behind it; a block's scale does not shrink).
+ *   k_new, v_new  16-bit vectors (cfg->dtype), vector (seq, token, head) at seq*ks.seq + token*ks.token + head*ks.head
+ * n_new == 0: states_out receives the states, nothing else changes.
+ */
+pk_status pk_fp8_append(const pk_fp8_config *cfg, const pk_fp8_cache *cache, int32_t *states, int32_t *states_out, const void *k_new,
+                        const void *v_new, const pk_strides *ks, const pk_strides *vs, int32_t n_new, const int32_t *counts,
+                        void *stream);
+
+/*
+ * Attention of the last n_query (counts[i]) tokens of every sequence, which have been appended, over the tokens that the cache
+ * holds: query i of n sees the first (held - n + i + 1) of them, less what the window masks.
+ *   bound      host: no sequence holds more tokens than this (t_capacity is always right); sizes the launch and the
+ *              workspace.  Results do not depend on sequences staying below it, only the balance of the work does.
+ *   q, qs      queries, (seq, token, head) as above; out, os: results in the same type
+ *   lse        optional float [n_seq][n_q_heads][n_query]: log-sum-exp of the scores
+ * A query that sees no token has out = 0 and lse = -inf.  Masked tokens never contribute, whatever their codes are.
+ * Scores and outputs are accumulated in binary32 (e4m3 codes and the queries are exact in the fp16 operands of the matrix
+ * instructions; bfloat16 queries are brought to fp16's range by a power of two per query first, which drops what lies under
+ * 2^-31 of a query's largest element); softmax numerators are rounded to fp16, their sum is not.
+ */
+pk_status pk_fp8_attention(const pk_fp8_config *cfg, const pk_fp8_cache *cache, const int32_t *states, int32_t bound, const void *q,
+                           const pk_strides *qs, int32_t n_query, const int32_t *counts, const pk_fp8_scores *scores, void *out,
+                           const pk_strides *os, float *lse, void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The attention weight of every cached token: weight[n][t] (+)= sum over the query heads of the KV head and the query tokens of
+ * exp(s - lse), the softmax weight that pk_fp8_attention gave it.  Arguments as there; lse as it returned them (a row whose lse
+ * is -inf adds nothing).  accumulate == 0: the weights of the tokens held are set instead.  Needs cache->weight.
+ * Sums are formed in a fixed order: results are reproducible bit for bit.
+ */
+pk_status pk_fp8_weights(const pk_fp8_config *cfg, const pk_fp8_cache *cache, const int32_t *states, int32_t bound, const void *q,
+                         const pk_strides *qs, int32_t n_query, const int32_t *counts, const pk_fp8_scores *scores, const float *lse,
+                         int32_t accumulate, void *stream);
+
+/*
+ * Bring every sequence that holds more than `budget` tokens down to it: per stream the first keep_first and the last keep_last
+ * tokens stay, and of the others those with the largest weight (ties to the earlier token; NaN counts as the smallest), in their order.
+ * The result goes to another cache, of any capacity >= budget and its own paging: blocks are formed anew from the kept tokens, pos
+ * and weight move along (weight if both caches have it), the next position stays.  Sequences within the budget move whole.
+ * The two caches and states must not overlap, and agree in sequences, heads, head_dim and block; needs the source's weight.
+ *   workspace   pk_fp8_workspace_bytes(cfg, PK_FP8_OP_EVICT, budget, 0) bytes
+ * budget >= 1, keep_first + keep_last <= budget.
+ */
+pk_status pk_fp8_evict(const pk_fp8_config *cfg, const pk_fp8_cache *cache, const int32_t *states, const pk_fp8_config *to_cfg,
+                       const pk_fp8_cache *to, int32_t *to_states, int32_t budget, int32_t keep_first, int32_t keep_last,
+                       void *workspace, size_t workspace_bytes, void *stream);
 
 #ifdef __cplusplus
 }

@@ -1,0 +1,803 @@
+// Attention over the 8-bit cache, and the attention weight of its tokens.
+//
+// A wave takes 64 cached tokens of one stream at a time against RT tiles of 16 query rows (row = query token * r + query head of the
+// group).  S^T = K Q^T with K's codes as fp16 (exact) on the matrix cores: lane 16 g + n gets, for row n, tokens 4g .. 4g+3 of
+// each tile of 16.  Those are the operand positions of the second product O^T = V^T P^T as they stand (the contraction runs over the
+// tokens in whatever order both operands agree on), so softmax numerators go from one product to the other in registers.  Rows of
+// K and V are read as they lie in memory: the contraction over channels takes the quarter row that a lane holds, and V's channels are
+// dealt to the 16 rows of an operand tile so that a lane's bytes of a token are adjacent; pairs of tokens are interleaved by byte
+// permutes before the conversion to fp16.  Block scales are powers of two and stay outside both products.
+#include "pk_fp8.h"
+
+namespace pk {
+
+namespace {
+
+constexpr float kLog2e = 1.44269504088896341f, kLn2 = 0.69314718055994531f;
+constexpr int kWaves = 4, kThreads = 64 * kWaves;
+
+__device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// tanh in binary32.  Below 0.55 the odd Taylor series (the first term left out is 4e-8 of the result at 0.55), above it
+// 1 - 2 / (e^{2x} + 1), whose rounding is no longer magnified there.
+__device__ __forceinline__ float tanh_(float x)
+{
+    const float a = fabsf(x), y = x * x;
+    // coefficients of x^3, x^5, ... of the series: 2^(2k) (2^(2k) - 1) B_2k / (2k)!
+    float s = -929569.f / 638512875.f;
+    s = fmaf(s, y, 21844.f / 6081075.f);
+    s = fmaf(s, y, -1382.f / 155925.f);
+    s = fmaf(s, y, 62.f / 2835.f);
+    s = fmaf(s, y, -17.f / 315.f);
+    s = fmaf(s, y, 2.f / 15.f);
+    s = fmaf(s, y, -1.f / 3.f);
+    float t = fmaf(s * y, x, x);
+    if (__any(!(a < 0.55f))) {
+        const float e = exp2_(fminf(a, 16.f) * (2.f * kLog2e));
+        const float big = 1.f - 2.f * __builtin_amdgcn_rcpf(e + 1.f);
+        t = a < 0.55f ? t : (a != a ? a : copysignf(big, x));
+    }
+    return t;
+}
+
+template <int D>
+struct Shape {
+    static constexpr int kSteps = D / 32;          // products over channels per tile of tokens
+    static constexpr int kTiles = D / 16;          // channel tiles of the output
+    static constexpr int kKWords = D / 16;         // 32-bit words of K per lane and token: a quarter row
+    static constexpr int kVWords = (D + 63) / 64;  // of V: a sixteenth row (96 channels: one word of the first 64, half a word of the rest)
+};
+
+template <int D>
+__device__ __forceinline__ void load_k(uint32_t (&k)[D / 16], const uint8_t *row, int g)
+{
+    if constexpr (D == 96) {
+        const uint2 *p = reinterpret_cast<const uint2 *>(row + g * 24);
+#pragma unroll
+        for (int i = 0; i < 3; ++i) {
+            const uint2 v = p[i];
+            k[2 * i] = v.x;
+            k[2 * i + 1] = v.y;
+        }
+    } else {
+        const uint4 *p = reinterpret_cast<const uint4 *>(row + g * (D / 4));
+#pragma unroll
+        for (int i = 0; i < D / 64; ++i) {
+            const uint4 v = p[i];
+            k[4 * i] = v.x;
+            k[4 * i + 1] = v.y;
+            k[4 * i + 2] = v.z;
+            k[4 * i + 3] = v.w;
+        }
+    }
+}
+template <int D>
+__device__ __forceinline__ void load_v(uint32_t (&v)[Shape<D>::kVWords], const uint8_t *row, int m)
+{
+    if constexpr (D == 64) {
+        v[0] = *reinterpret_cast<const uint32_t *>(row + 4 * m);
+    } else if constexpr (D == 96) {
+        v[0] = *reinterpret_cast<const uint32_t *>(row + 4 * m);
+        v[1] = *reinterpret_cast<const uint16_t *>(row + 64 + 2 * m);
+    } else if constexpr (D == 128) {
+        const uint2 w = *reinterpret_cast<const uint2 *>(row + 8 * m);
+        v[0] = w.x;
+        v[1] = w.y;
+    } else {
+        const uint4 w = *reinterpret_cast<const uint4 *>(row + 16 * m);
+        v[0] = w.x;
+        v[1] = w.y;
+        v[2] = w.z;
+        v[3] = w.w;
+    }
+}
+// Channel of output tile ct and operand row m: the inverse of how load_v deals them.
+template <int D>
+__device__ __forceinline__ int channel_of(int m, int ct)
+{
+    if constexpr (D == 96) return ct < 4 ? 4 * m + ct : 64 + 2 * m + (ct - 4);
+    return m * (D / 16) + ct;
+}
+
+// 8 channels of a query (16-bit) as fp16: as they are, or from bfloat16 times a power of two
+__device__ __forceinline__ half8v query8(const uint4 &v, int bf16, float mul)
+{
+    if (!bf16) return __builtin_bit_cast(half8v, v);
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    half8v h;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float lo, hi;
+        widen(w[i], 1, lo, hi);
+        h[2 * i] = (_Float16)(lo * mul);
+        h[2 * i + 1] = (_Float16)(hi * mul);
+    }
+    return h;
+}
+
+// The query of a row as operands of the products over channels, and the factor that belongs to the products (a power of two).
+template <int D>
+__device__ __forceinline__ void load_query(half8v (&qf)[D / 32], float &factor, const Fp8Queries &a, int seq, int kvh, int row, bool live, int g)
+{
+    uint4 raw[D / 32];
+#pragma unroll
+    for (int s = 0; s < D / 32; ++s) raw[s] = make_uint4(0, 0, 0, 0);
+    if (live) {
+        const int i = row / a.r, h = row - i * a.r;
+        const uint4 *p = reinterpret_cast<const uint4 *>(static_cast<const char *>(a.q) + 2 * (seq * a.qs.seq + i * a.qs.token + (int64_t)(kvh * a.r + h) * a.qs.head)) +
+                         g * (D / 32);
+#pragma unroll
+        for (int s = 0; s < D / 32; ++s) raw[s] = p[s];
+    }
+    float mul = 1.f;
+    factor = 1.f;
+    if (a.bf16) {
+        uint32_t most = 0;
+#pragma unroll
+        for (int s = 0; s < D / 32; ++s) {
+            const uint32_t w[4] = {raw[s].x, raw[s].y, raw[s].z, raw[s].w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t lo = w[i] & 0x7fffu, hi = (w[i] >> 16) & 0x7fffu;
+                most = max(most, max(lo < 0x7f80u ? lo : 0u, hi < 0x7f80u ? hi : 0u));
+            }
+        }
+        const float x[1] = {__builtin_bit_cast(float, most << 16)};
+        const uint32_t all = __builtin_bit_cast(uint32_t, fold_rows(x, MaxF()));
+        // the largest element to [2^14, 2^15), within what a binary32 holds on both sides
+        const int shift = min(max((int)(all >> 23) - 127 - 14, -126), 126);
+        factor = __builtin_bit_cast(float, (uint32_t)(127 + shift) << 23);
+        mul = __builtin_bit_cast(float, (uint32_t)(127 - shift) << 23);
+    }
+#pragma unroll
+    for (int s = 0; s < D / 32; ++s) qf[s] = query8(raw[s], a.bf16, mul);
+}
+
+// Per lane: what its query row sees
+struct Row {
+    int last;       // index of the last token it sees, -1: none
+    int pos;        // its position
+    float slope;    // of its head
+    float factor;   // of its products
+};
+
+template <int D>
+__device__ __forceinline__ half8v k_operand(const uint32_t (&k)[D / 16], int s)
+{
+    const half2v a = codes_lo(k[2 * s]), b = codes_hi(k[2 * s]), c = codes_lo(k[2 * s + 1]), d = codes_hi(k[2 * s + 1]);
+    return half8v{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+// Scores of 4 tokens of a row, t0 + 0 .. 3, in place of their products; masked ones at -inf.  `unit` is what multiplies the product, and
+// what a score is multiplied with: the score is cap * tanh(unit * x / cap) - slope * distance, or unit * x - ....
+template <bool OPT>
+__device__ __forceinline__ void finish_scores(float (&x)[4], float k_scale, const Fp8Queries &a, float post, const Row &row, int t0, const int32_t *pos,
+                                              bool edge, bool windowed)
+{
+    const float f = k_scale * row.factor * a.scale;
+    if constexpr (OPT) {
+        if (a.cap > 0.f) {
+            const float inv = 1.f / a.cap;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = tanh_(x[i] * f * inv) * a.cap;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] *= f;
+        }
+        if (pos) {
+            const int4 p = *reinterpret_cast<const int4 *>(pos + t0);
+            const int back[4] = {row.pos - p.x, row.pos - p.y, row.pos - p.z, row.pos - p.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                x[i] = fmaf(-row.slope, (float)back[i], x[i]);
+                if (windowed && back[i] >= a.window) x[i] = -INFINITY;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] *= post;
+    } else {
+        const float fp = f * post;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] *= fp;
+    }
+    if (edge) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = t0 + i <= row.last ? x[i] : -INFINITY;
+    }
+}
+
+// Where a workgroup's rows and keys are
+struct Place {
+    int stream, seq, kvh, len, next, count;
+};
+// ONE: all lanes of the wave ask for the same stream
+template <bool ONE>
+__device__ __forceinline__ Place place_of(const Fp8Queries &a, int stream)
+{
+    Place p;
+    p.stream = stream;
+    p.seq = stream / a.c.n_kv_heads;
+    p.kvh = stream - p.seq * a.c.n_kv_heads;
+    const int2 st = fp8_state(a.states, p.seq, a.c.t_capacity);
+    const int count = fp8_count(a.counts, p.seq, a.n_query);
+    p.len = ONE ? __builtin_amdgcn_readfirstlane(st.x) : st.x;
+    p.next = ONE ? __builtin_amdgcn_readfirstlane(st.y) : st.y;
+    p.count = ONE ? __builtin_amdgcn_readfirstlane(count) : count;
+    return p;
+}
+__device__ __forceinline__ Row row_of(const Fp8Queries &a, const Place &p, int row)
+{
+    const int i = row / a.r;
+    Row x;
+    x.last = i < p.count ? p.len - p.count + i : -1;
+    x.pos = p.next - p.count + i;
+    x.slope = a.slopes ? a.slopes[p.kvh * a.r + row - i * a.r] : 0.f;
+    x.factor = 1.f;
+    return x;
+}
+// Tokens [lo, hi) that rows first .. last (clamped to the live ones) can see: positions are distinct and grow, so a token that is at most
+// window - 1 positions back is at most as many tokens back.
+__device__ __forceinline__ void key_range(const Fp8Queries &a, const Place &p, int first_row, int last_row, int &lo, int &hi)
+{
+    const int i0 = first_row / a.r, i1 = min(last_row / a.r, p.count - 1);
+    hi = i0 <= i1 ? max(p.len - p.count + i1 + 1, 0) : 0;
+    lo = 0;
+    if (a.window > 0) lo = (int)min(max((int64_t)p.len - p.count + i0 + 1 - a.window, (int64_t)0), (int64_t)hi) & ~63;
+}
+
+template <int D>
+__device__ __forceinline__ void store_row(const Fp8AttentionArgs &a, const Place &p, int row, int c, const float *x, int n)
+{
+    const int i = row / a.in.r, h = row - i * a.in.r;
+    uint32_t *o = reinterpret_cast<uint32_t *>(static_cast<char *>(a.out) + 2 * (p.seq * a.os.seq + i * a.os.token + (int64_t)(p.kvh * a.in.r + h) * a.os.head + c));
+    for (int e = 0; e < n; e += 2) o[e / 2] = narrow(x[e], x[e + 1], a.in.bf16);
+}
+__device__ __forceinline__ void store_lse(const Fp8AttentionArgs &a, const Place &p, int row, float m, float l)
+{
+    if (!a.lse) return;
+    const int i = row / a.in.r, h = row - i * a.in.r;
+    a.lse[((int64_t)p.seq * a.in.c.n_kv_heads * a.in.r + p.kvh * a.in.r + h) * a.in.n_query + i] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+}
+
+// Rows of a workgroup: BY_ROWS, every wave has RT tiles of its own and walks all keys; else the waves share RT tiles and deal the keys
+// out among them, 64 at a time.
+template <int D, int RT, bool BY_ROWS, bool OPT>
+__global__ __launch_bounds__(kThreads, 2) void fp8_attention_kernel(Fp8AttentionArgs a)
+{
+    using S = Shape<D>;
+    const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int N = a.in.n_seq * a.in.c.n_kv_heads;
+    const int rows = a.in.r * a.in.n_query;
+    const int rest = blockIdx.x / N;
+    const Place p = place_of<true>(a.in, blockIdx.x - rest * N);
+    const int split = rest % a.splits, group = rest / a.splits;
+    const int row0 = BY_ROWS ? (group * kWaves + wave) * 16 * RT : group * 16 * RT;
+
+    Row row[RT];
+    half8v qf[RT][S::kSteps];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        const int at = row0 + 16 * rt + n;
+        row[rt] = row_of(a.in, p, at);
+        load_query<D>(qf[rt], row[rt].factor, a.in, p.seq, p.kvh, at, at < p.count * a.in.r, g);
+    }
+    int lo, hi;
+    key_range(a.in, p, row0, min(row0 + 16 * RT, rows) - 1, lo, hi);
+    if (a.splits > 1) {
+        const int per = ((hi - lo + a.splits - 1) / a.splits + 63) & ~63;
+        lo = (int)min((int64_t)lo + (int64_t)split * per, (int64_t)hi);
+        hi = min(lo + per, hi);
+    }
+    // the first token that some live row does not see, and the largest position of a live row
+    const int sees_all = p.len - p.count + min(row0 / a.in.r, max(p.count - 1, 0)) + 1;
+    const int pos_most = p.next - p.count + min((row0 + 16 * RT - 1) / a.in.r, p.count - 1);
+    const int32_t *pos = OPT && (a.in.slopes || a.in.window > 0) ? a.in.c.pos + (int64_t)p.stream * a.in.c.t_capacity : nullptr;
+
+    float m[RT], l[RT];
+    float4v o[RT][S::kTiles];
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        m[rt] = -INFINITY;
+        l[rt] = 0.f;
+#pragma unroll
+        for (int ct = 0; ct < S::kTiles; ++ct) o[rt][ct] = float4v{0.f, 0.f, 0.f, 0.f};
+    }
+    int unit = -1000;   // exponent field of the V scale that o is in units of
+
+    const StreamMap map = a.in.c.map.of(p.stream);
+    const int first = BY_ROWS ? lo : lo + 64 * wave, step = BY_ROWS ? 64 : 64 * kWaves;
+    for (int t0 = first; t0 < hi; t0 += step) {
+        const int64_t at = map.pos(t0);
+        uint32_t kw[4][S::kKWords], vw[16][S::kVWords];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) load_k<D>(kw[j], a.in.c.k_codes + (at + 16 * j + n) * D, g);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) load_v<D>(vw[j], a.in.c.v_codes + (at + 16 * (j >> 2) + 4 * g + (j & 3)) * D, n);
+        const int64_t b0 = at >> a.in.c.log_block, b1 = (at + 32) >> a.in.c.log_block;
+        const float ks[2] = {fabsf(a.in.c.k_scale[b0]), fabsf(a.in.c.k_scale[b1])};
+        const float vs[2] = {a.in.c.v_scale[b0], a.in.c.v_scale[b1]};
+        const bool edge = t0 + 64 > sees_all;
+        const bool windowed = OPT && a.in.window > 0 && (int64_t)pos_most - t0 >= a.in.window;
+
+        float4v s[RT][4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) s[rt][j] = float4v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int q = 0; q < S::kSteps; ++q) {
+                const half8v k = k_operand<D>(kw[j], q);
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) s[rt][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, qf[rt][q], s[rt][j], 0, 0, 0);
+            }
+        }
+        float x[RT][16];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            float most = -INFINITY;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                float y[4] = {s[rt][j][0], s[rt][j][1], s[rt][j][2], s[rt][j][3]};
+                finish_scores<OPT>(y, ks[j >> 1], a.in, kLog2e, row[rt], t0 + 16 * j + 4 * g, pos, edge, windowed);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    x[rt][4 * j + i] = y[i];
+                    most = fmaxf(most, y[i]);
+                }
+            }
+            const float one[1] = {most};
+            most = fold_rows(one, MaxF());
+            // the reference moves when a score is far above it: numerators stay below 2^4 and need no other care
+            if (__any(most > m[rt] + 4.f)) {
+                const float to = fmaxf(most, m[rt]);
+                const float by = to == -INFINITY ? 1.f : exp2_(m[rt] - to);
+                m[rt] = to;
+                l[rt] *= by;
+#pragma unroll
+                for (int ct = 0; ct < S::kTiles; ++ct) o[rt][ct] *= by;
+            }
+        }
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            if (t0 + 32 * half >= hi) break;
+            // Units of o: the largest scale so far.  A block of a scale up to 2^6 smaller enters with numerators that are smaller by as much
+            // (their fp16 keeps 2^-24 of the reference); below that o comes down for it and goes up again.
+            const int field = field_of_scale(vs[half]);
+            int fold = 0, down = 0;
+            if (field > unit) {
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                    for (int ct = 0; ct < S::kTiles; ++ct)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) o[rt][ct][i] = ldexpf(o[rt][ct][i], unit - field);
+                unit = field;
+            } else {
+                fold = unit - field;
+                if (fold > 6) {
+                    down = min(fold, 60);
+                    fold -= down;
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                        for (int ct = 0; ct < S::kTiles; ++ct)
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) o[rt][ct][i] = ldexpf(o[rt][ct][i], down);
+                }
+            }
+            half8v pf[RT];
+#pragma unroll
+            for (int rt = 0; rt < RT; ++rt) {
+                const float ref = (m[rt] == -INFINITY ? 0.f : m[rt]) + (float)fold;
+                float sum = 0.f;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const float e = exp2_(x[rt][8 * half + i] - ref);
+                    sum += e;
+                    pf[rt][i] = (_Float16)e;
+                }
+                l[rt] += ldexpf(sum, fold);
+            }
+            const bool flagged = vs[half] < 0.f;
+            if (edge || windowed || flagged) {
+                // what no row of the wave sees must not reach the product, whatever its codes
+                const bool cut = t0 + 32 * half + 32 > hi;
+                if (cut) {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (t0 + 32 * half + 16 * (j >> 2) + 4 * g + (j & 3) >= hi)
+#pragma unroll
+                            for (int w = 0; w < S::kVWords; ++w) vw[8 * half + j][w] = 0;
+                }
+                if (flagged) {
+                    // NaN codes reach only the rows that see them: a product of their own of marks (1.0 for a NaN) and of who sees whom
+                    half8v see[RT];
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            const int t = t0 + 32 * half + 16 * (j >> 2) + 4 * g + (j & 3);
+                            bool yes = t <= row[rt].last;
+                            if (OPT && a.in.window > 0) yes = yes && (int64_t)row[rt].pos - pos[t] < a.in.window;
+                            see[rt][j] = yes ? (_Float16)1.f : (_Float16)0.f;
+                        }
+#pragma unroll
+                    for (int w = 0; w < S::kVWords; ++w) {
+                        uint32_t mark[8];
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) {
+                            const uint32_t nan = nan_codes(vw[8 * half + j][w]) >> 7;
+                            mark[j] = nan * 0x38u;                      // 0x38: 1.0
+                            vw[8 * half + j][w] &= ~(nan * 0xffu);
+                        }
+                        constexpr int kPer = 4;
+#pragma unroll
+                        for (int c = 0; c < kPer; ++c) {
+                            const int ct = 4 * w + c;
+                            if (ct >= S::kTiles) break;
+                            half8v f;
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) f[j] = (mark[j] >> (8 * c)) & 0xffu ? (_Float16)1.f : (_Float16)0.f;
+#pragma unroll
+                            for (int rt = 0; rt < RT; ++rt) {
+                                const float4v seen = __builtin_amdgcn_mfma_f32_16x16x32_f16(f, see[rt], float4v{0.f, 0.f, 0.f, 0.f}, 0, 0, 0);
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) o[rt][ct][i] = seen[i] > 0.f ? __builtin_nanf("") : o[rt][ct][i];
+                            }
+                        }
+                    }
+                }
+            }
+#pragma unroll
+            for (int w = 0; w < S::kVWords; ++w) {
+                uint32_t even[4], odd[4];   // channels 4w, 4w+1 and 4w+2, 4w+3 of token pairs
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const uint32_t lo2 = vw[8 * half + 2 * q][w], hi2 = vw[8 * half + 2 * q + 1][w];
+                    even[q] = __builtin_amdgcn_perm(hi2, lo2, 0x05010400u);
+                    odd[q] = __builtin_amdgcn_perm(hi2, lo2, 0x07030602u);
+                }
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    const int ct = 4 * w + c;
+                    if (ct >= S::kTiles) break;
+                    half8v f;
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const uint32_t word = c < 2 ? even[q] : odd[q];
+                        const half2v h = c & 1 ? codes_hi(word) : codes_lo(word);
+                        f[2 * q] = h[0];
+                        f[2 * q + 1] = h[1];
+                    }
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) o[rt][ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f, pf[rt], o[rt][ct], 0, 0, 0);
+                }
+            }
+            if (down) {
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+                    for (int ct = 0; ct < S::kTiles; ++ct)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) o[rt][ct][i] = ldexpf(o[rt][ct][i], -down);
+            }
+        }
+    }
+
+    // results of the wave, normalised: o / l * 2^unit
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+        const float one[1] = {l[rt]};
+        l[rt] = fold_rows(one, AddF());
+        const float inv = l[rt] == 0.f ? 0.f : 1.f / l[rt];
+#pragma unroll
+        for (int ct = 0; ct < S::kTiles; ++ct)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[rt][ct][i] = ldexpf(o[rt][ct][i] * inv, max(unit, 1) - 127);
+    }
+    if constexpr (BY_ROWS) {
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+            const int at = row0 + 16 * rt + n;
+            if (at >= p.count * a.in.r) continue;
+            if (a.splits == 1) {
+                if (g == 0) store_lse(a, p, at, m[rt], l[rt]);
+            } else if (g == 0) {
+                float *ml = a.part_ml + (((int64_t)p.stream * a.splits + split) * rows + at) * 2;
+                ml[0] = m[rt];
+                ml[1] = l[rt];
+            }
+            // a lane has the channels of operand rows 4g .. 4g+3: runs of neighbours
+            constexpr int kMain = D == 96 ? 4 : S::kTiles;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float y[S::kTiles];
+#pragma unroll
+                for (int ct = 0; ct < S::kTiles; ++ct) y[ct] = o[rt][ct][i];
+                if (a.splits == 1) {
+                    store_row<D>(a, p, at, channel_of<D>(4 * g + i, 0), y, kMain);
+                    if constexpr (D == 96) store_row<D>(a, p, at, channel_of<D>(4 * g + i, 4), y + 4, 2);
+                } else {
+                    float *to = a.part_o + (((int64_t)p.stream * a.splits + split) * rows + at) * D;
+#pragma unroll
+                    for (int ct = 0; ct < S::kTiles; ++ct) to[channel_of<D>(4 * g + i, ct)] = y[ct];
+                }
+            }
+        }
+    } else {
+        // rows that the waves bring together at a time: 32 to 34 KB of LDS
+        constexpr int kAtOnce = D == 256 ? 8 : 16, kPad = 4;
+        __shared__ float sm_o[kWaves][kAtOnce][D + kPad];
+        __shared__ float sm_m[kWaves][kAtOnce], sm_l[kWaves][kAtOnce];
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+            for (int part = 0; part < 16 / kAtOnce; ++part) {
+                const int from = row0 + 16 * rt + part * kAtOnce, here = min(rows - from, kAtOnce);
+                if (here <= 0) break;
+                if (rt + part > 0) __syncthreads();
+                if (n / kAtOnce == part) {
+                    const int q = n % kAtOnce;
+                    if (g == 0) {
+                        sm_m[wave][q] = m[rt];
+                        sm_l[wave][q] = l[rt];
+                    }
+#pragma unroll
+                    for (int ct = 0; ct < S::kTiles; ++ct)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) sm_o[wave][q][channel_of<D>(4 * g + i, ct)] = o[rt][ct][i];
+                }
+                __syncthreads();
+                for (int e = threadIdx.x; e < here * (D / 4); e += kThreads) {
+                    const int q = e / (D / 4), c = (e % (D / 4)) * 4, at = from + q;
+                    if (at >= p.count * a.in.r) continue;
+                    float top = -INFINITY;
+                    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, sm_m[w][q]);
+                    const float ref = top == -INFINITY ? 0.f : top;
+                    float sum = 0.f, y[4] = {0.f, 0.f, 0.f, 0.f};
+                    for (int w = 0; w < kWaves; ++w) {
+                        const float share = sm_l[w][q] * exp2_(sm_m[w][q] - ref);
+                        sum += share;
+                        for (int i = 0; i < 4; ++i) y[i] = fmaf(share, sm_o[w][q][c + i], y[i]);
+                    }
+                    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+                    for (int i = 0; i < 4; ++i) y[i] *= inv;
+                    if (a.splits == 1) {
+                        store_row<D>(a, p, at, c, y, 4);
+                        if (c == 0) store_lse(a, p, at, top, sum);
+                    } else {
+                        const int64_t slot = ((int64_t)p.stream * a.splits + split) * rows + at;
+                        *reinterpret_cast<float4 *>(a.part_o + slot * D + c) = make_float4(y[0], y[1], y[2], y[3]);
+                        if (c == 0) {
+                            a.part_ml[2 * slot] = top;
+                            a.part_ml[2 * slot + 1] = sum;
+                        }
+                    }
+                }
+            }
+    }
+}
+
+// The splits of a row together: sum_s l_s 2^(m_s - m) o_s / sum_s l_s 2^(m_s - m).  A thread takes two channels of a row.
+template <int D>
+__global__ __launch_bounds__(256) void fp8_merge_kernel(Fp8AttentionArgs a)
+{
+    const int rows = a.in.r * a.in.n_query;
+    const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x, all = (int64_t)a.in.n_seq * a.in.c.n_kv_heads * rows * (D / 2);
+    if (e >= all) return;
+    const int c = (int)(e % (D / 2)) * 2;
+    const int64_t flat = e / (D / 2);
+    const int row = (int)(flat % rows);
+    const Place p = place_of<false>(a.in, (int)(flat / rows));
+    if (row >= p.count * a.in.r) return;
+    float top = -INFINITY;
+    for (int s = 0; s < a.splits; ++s) top = fmaxf(top, a.part_ml[2 * (((int64_t)p.stream * a.splits + s) * rows + row)]);
+    const float ref = top == -INFINITY ? 0.f : top;
+    float sum = 0.f, y[2] = {0.f, 0.f};
+    for (int s = 0; s < a.splits; ++s) {
+        const int64_t slot = ((int64_t)p.stream * a.splits + s) * rows + row;
+        const float part = a.part_ml[2 * slot + 1] * exp2_(a.part_ml[2 * slot] - ref);
+        sum += part;
+        const float2 o = *reinterpret_cast<const float2 *>(a.part_o + slot * D + c);
+        y[0] = fmaf(part, o.x, y[0]);
+        y[1] = fmaf(part, o.y, y[1]);
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    y[0] *= inv;
+    y[1] *= inv;
+    store_row<D>(a, p, row, c, y, 2);
+    if (c == 0) store_lse(a, p, row, top, sum);
+}
+
+// ---- the weight of every token -------------------------------------------------------------------------------------------
+
+// Query operands of up to this many tiles of 16 rows in LDS at a time: 32 KB at 128 channels, 64 at 256
+constexpr int kWeightTiles = 8;
+
+// A wave takes 64 tokens at a time, their K operands in registers, against the rows in LDS; the sums over rows stay in registers
+// until all tiles are done.  More rows than fit go in rounds that add to what the first wrote, each token in the same lane.
+template <int D, bool OPT>
+__global__ __launch_bounds__(kThreads, 2) void fp8_weights_kernel(Fp8WeightsArgs a, int ranges)
+{
+    using S = Shape<D>;
+    __shared__ half8v sm_q[kWeightTiles][S::kSteps][64];
+    __shared__ Row sm_row[kWeightTiles * 16];
+    __shared__ float sm_lse[kWeightTiles * 16];
+    const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int N = a.in.n_seq * a.in.c.n_kv_heads;
+    const int range = blockIdx.x / N;
+    const Place p = place_of<true>(a.in, blockIdx.x - range * N);
+    const int rows = p.count * a.in.r;
+    const int per = ((p.len + ranges - 1) / ranges + 63) & ~63;
+    const int from = (int)min((int64_t)range * per, (int64_t)p.len), to = min(from + per, p.len);
+    if (from >= to) return;
+    const int32_t *pos = OPT && (a.in.slopes || a.in.window > 0) ? a.in.c.pos + (int64_t)p.stream * a.in.c.t_capacity : nullptr;
+    float *weight = a.in.c.weight + (int64_t)p.stream * a.in.c.t_capacity;
+    const StreamMap map = a.in.c.map.of(p.stream);
+    for (int first = 0; first < max(rows, 1); first += 16 * kWeightTiles) {
+        const int tiles = (min(rows - first, 16 * kWeightTiles) + 15) / 16;
+        if (first > 0) __syncthreads();
+        for (int tile = wave; tile < tiles; tile += kWaves) {
+            const int at = first + 16 * tile + n;
+            half8v qf[S::kSteps];
+            Row row = row_of(a.in, p, at);
+            load_query<D>(qf, row.factor, a.in, p.seq, p.kvh, at, at < rows, g);
+#pragma unroll
+            for (int s = 0; s < S::kSteps; ++s) sm_q[tile][s][lane] = qf[s];
+            if (g == 0) {
+                const int i = at / a.in.r, h = at - i * a.in.r;
+                float lse = at < rows ? a.lse[((int64_t)p.seq * a.in.c.n_kv_heads * a.in.r + p.kvh * a.in.r + h) * a.in.n_query + i] : INFINITY;
+                if (lse == -INFINITY) {   // a row that saw nothing adds nothing
+                    lse = INFINITY;
+                    row.last = -1;
+                }
+                sm_lse[16 * tile + n] = lse;
+                sm_row[16 * tile + n] = row;
+            }
+        }
+        __syncthreads();
+        int lo, hi;
+        key_range(a.in, p, first, min(first + 16 * kWeightTiles, rows) - 1, lo, hi);
+        for (int t0 = from + 64 * wave; t0 < to; t0 += 64 * kWaves) {
+            float sum[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sum[i] = 0.f;
+            if (rows > 0 && t0 < hi && t0 + 64 > lo) {
+                const int64_t at = map.pos(t0);
+                uint32_t kw[4][S::kKWords];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) load_k<D>(kw[j], a.in.c.k_codes + (at + 16 * j + n) * D, g);
+                const float ks[2] = {fabsf(a.in.c.k_scale[at >> a.in.c.log_block]), fabsf(a.in.c.k_scale[(at + 32) >> a.in.c.log_block])};
+                half8v kf[4][S::kSteps];
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int s = 0; s < S::kSteps; ++s) kf[j][s] = k_operand<D>(kw[j], s);
+                for (int tile = 0; tile < tiles; ++tile) {
+                    const Row row = sm_row[16 * tile + n];
+                    const float lse = sm_lse[16 * tile + n];
+                    float4v x[4];
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) x[j] = float4v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                    for (int s = 0; s < S::kSteps; ++s) {
+                        const half8v q = sm_q[tile][s][lane];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) x[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[j][s], q, x[j], 0, 0, 0);
+                    }
+                    const bool edge = __any(t0 + 63 > row.last);
+                    const bool windowed = OPT && a.in.window > 0;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        float y[4] = {x[j][0], x[j][1], x[j][2], x[j][3]};
+                        finish_scores<OPT>(y, ks[j >> 1], a.in, 1.f, row, t0 + 16 * j + 4 * g, pos, edge, windowed);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) sum[4 * j + i] += exp2_((y[i] - lse) * kLog2e);
+                    }
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < 16; ++i) sum[i] = row_sum(sum[i]);
+            if (n < 4) {   // lane 16 g + n writes tokens 16 n + 4 g .. + 3
+                float4 v;
+                v.x = n == 0 ? sum[0] : n == 1 ? sum[4] : n == 2 ? sum[8] : sum[12];
+                v.y = n == 0 ? sum[1] : n == 1 ? sum[5] : n == 2 ? sum[9] : sum[13];
+                v.z = n == 0 ? sum[2] : n == 1 ? sum[6] : n == 2 ? sum[10] : sum[14];
+                v.w = n == 0 ? sum[3] : n == 1 ? sum[7] : n == 2 ? sum[11] : sum[15];
+                const int t = t0 + 16 * n + 4 * g;
+                float *w = weight + t;
+                const bool add = a.accumulate || first > 0;
+                if (t + 3 < to) {
+                    float4 old = make_float4(0.f, 0.f, 0.f, 0.f);
+                    if (add) old = *reinterpret_cast<const float4 *>(w);
+                    *reinterpret_cast<float4 *>(w) = make_float4(old.x + v.x, old.y + v.y, old.z + v.z, old.w + v.w);
+                } else {
+                    const float y[4] = {v.x, v.y, v.z, v.w};
+                    for (int i = 0; i < 4; ++i)
+                        if (t + i < to) w[i] = (add ? w[i] : 0.f) + y[i];
+                }
+            }
+        }
+    }
+}
+
+// How many rows a workgroup of the attention takes, and how.
+struct Rows {
+    int tiles;      // per wave (RT)
+    bool by_rows;
+    int per_group;
+};
+Rows rows_of(int64_t rows, int d)
+{
+    Rows x;
+    x.by_rows = rows > 64;
+    x.tiles = d == 256 || rows <= 16 ? 1 : 2;
+    x.per_group = 16 * x.tiles * (x.by_rows ? kWaves : 1);
+    return x;
+}
+
+template <int D, int RT, bool BY_ROWS>
+void launch_rt(const Fp8AttentionArgs &a, uint32_t grid, bool opt, hipStream_t s)
+{
+    if (opt) fp8_attention_kernel<D, RT, BY_ROWS, true><<<grid, kThreads, 0, s>>>(a);
+    else fp8_attention_kernel<D, RT, BY_ROWS, false><<<grid, kThreads, 0, s>>>(a);
+}
+
+template <int D>
+hipError_t launch_d(const Fp8AttentionArgs &a, hipStream_t s)
+{
+    const int64_t rows = (int64_t)a.in.r * a.in.n_query, N = (int64_t)a.in.n_seq * a.in.c.n_kv_heads;
+    const Rows x = rows_of(rows, D);
+    const uint32_t grid = (uint32_t)(N * ((rows + x.per_group - 1) / x.per_group) * a.splits);
+    const bool opt = a.in.cap > 0.f || a.in.slopes || a.in.window > 0;
+    if (x.tiles == 1) {
+        if (x.by_rows) launch_rt<D, 1, true>(a, grid, opt, s);
+        else launch_rt<D, 1, false>(a, grid, opt, s);
+    } else if constexpr (D < 256) {
+        if (x.by_rows) launch_rt<D, 2, true>(a, grid, opt, s);
+        else launch_rt<D, 2, false>(a, grid, opt, s);
+    }
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || a.splits == 1) return e;
+    fp8_merge_kernel<D><<<(uint32_t)((N * rows * (D / 2) + 255) / 256), 256, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+template <int D>
+hipError_t launch_weights_d(const Fp8WeightsArgs &a, hipStream_t s)
+{
+    const int64_t N = (int64_t)a.in.n_seq * a.in.c.n_kv_heads;
+    const int64_t most = ((int64_t)a.bound + 64 * kWaves - 1) / (64 * kWaves), want = (1024 + N - 1) / N;
+    const int ranges = (int)(most < want ? (most < 1 ? 1 : most) : want);
+    if (a.in.cap > 0.f || a.in.slopes || a.in.window > 0) fp8_weights_kernel<D, true><<<(uint32_t)(N * ranges), kThreads, 0, s>>>(a, ranges);
+    else fp8_weights_kernel<D, false><<<(uint32_t)(N * ranges), kThreads, 0, s>>>(a, ranges);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+int fp8_attention_splits(int64_t n_streams, int64_t r, int64_t n_query, int d, int64_t bound)
+{
+    const Rows x = rows_of(r * n_query, d);
+    const int64_t groups = n_streams * ((r * n_query + x.per_group - 1) / x.per_group);
+    const int64_t want = (1024 + groups - 1) / groups, most = (bound + 255) / 256;
+    const int64_t k = want < most ? want : most;
+    return (int)(k < 1 ? 1 : k > 256 ? 256 : k);
+}
+
+hipError_t launch_fp8_attention(const Fp8AttentionArgs &a, hipStream_t s)
+{
+    return a.in.d == 64 ? launch_d<64>(a, s) : a.in.d == 96 ? launch_d<96>(a, s) : a.in.d == 128 ? launch_d<128>(a, s) : launch_d<256>(a, s);
+}
+
+hipError_t launch_fp8_weights(const Fp8WeightsArgs &a, hipStream_t s)
+{
+    return a.in.d == 64    ? launch_weights_d<64>(a, s)
+           : a.in.d == 96  ? launch_weights_d<96>(a, s)
+           : a.in.d == 128 ? launch_weights_d<128>(a, s)
+                           : launch_weights_d<256>(a, s);
+}
+
+}  // namespace pk

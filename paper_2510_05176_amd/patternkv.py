@@ -432,3 +432,243 @@ def pk_dequantize(cfg: Config, cache: Cache, patterns_k: torch.Tensor, patterns_
                             t0, t1, _ptr(k), _ptr(v), _stream())
     _check(st, "pk_dequantize")
     return k, v
+
+
+# ---- the 8-bit cache -------------------------------------------------------------------------------------------------------
+
+DTYPE_FP16, DTYPE_BF16 = 0, 1
+FP8_OP_ATTENTION, FP8_OP_EVICT = 0, 1
+_FP8_ARRAYS = ("k_codes", "v_codes", "k_scale", "v_scale", "pos", "weight")
+_FP8_TYPES = dict(k_codes=torch.uint8, v_codes=torch.uint8, k_scale=torch.float32, v_scale=torch.float32, pos=torch.int32, weight=torch.float32)
+_pack_fp8_config = struct.Struct("@9i").pack
+_pack_fp8_cache = struct.Struct("@7P").pack
+_pack_strides = struct.Struct("@3q").pack
+_pack_fp8_scores = struct.Struct("@ffiP").pack
+
+
+class _Fp8Layout(C.Structure):
+    _fields_ = [(n, C.c_uint64) for n in _FP8_ARRAYS + ("total",)] + [("align", C.c_uint32)]
+
+
+_lib.pk_fp8_cache_layout.restype = C.c_int
+_lib.pk_fp8_cache_layout.argtypes = [C.c_void_p, C.POINTER(_Fp8Layout)]
+_lib.pk_fp8_workspace_bytes.restype = C.c_size_t
+_lib.pk_fp8_workspace_bytes.argtypes = [C.c_void_p, C.c_int, C.c_int64, C.c_int64]
+_lib.pk_fp8_append.restype = C.c_int
+_lib.pk_fp8_append.argtypes = [C.c_void_p] * 8 + [C.c_int32, C.c_void_p, C.c_void_p]
+_lib.pk_fp8_attention.restype = C.c_int
+_lib.pk_fp8_attention.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p,
+                                  C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+_lib.pk_fp8_weights.restype = C.c_int
+_lib.pk_fp8_weights.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p,
+                                C.c_void_p, C.c_int32, C.c_void_p]
+_lib.pk_fp8_evict.restype = C.c_int
+_lib.pk_fp8_evict.argtypes = [C.c_void_p] * 6 + [C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_size_t, C.c_void_p]
+
+
+@dataclass(frozen=True)
+class Fp8Config:
+    n_seq: int = 1
+    n_kv_heads: int = 1
+    n_q_heads: int = 1
+    head_dim: int = 128
+    block: int = 64         # tokens per scale
+    t_capacity: int = 0
+    dtype: int = DTYPE_FP16
+    page_tokens: int = 0    # > 0: the codes and scales are a pool of n_pages pages of this many tokens (all KV heads)
+    n_pages: int = 0
+
+    def __post_init__(self):
+        # what every call of a serving loop asks for is made once
+        values = (self.n_seq, self.n_kv_heads, self.n_q_heads, self.head_dim, self.block, self.t_capacity, self.dtype, self.page_tokens, self.n_pages)
+        object.__setattr__(self, "packed", _pack_fp8_config(*values))
+        object.__setattr__(self, "torch_dtype", torch.bfloat16 if self.dtype == DTYPE_BF16 else torch.float16)
+        object.__setattr__(self, "_workspaces", {})
+
+    @property
+    def n_streams(self) -> int:
+        return self.n_seq * self.n_kv_heads
+
+
+def pk_fp8_cache_layout(cfg: Fp8Config) -> dict:
+    lay = _Fp8Layout()
+    _check(_lib.pk_fp8_cache_layout(cfg.packed, C.byref(lay)), "pk_fp8_cache_layout")
+    return {n: int(getattr(lay, n)) for n, _ in _Fp8Layout._fields_}
+
+
+def pk_fp8_workspace_bytes(cfg: Fp8Config, op: int, a: int, b: int = 0) -> int:
+    key = (op, a, b)
+    if key not in cfg._workspaces:
+        if len(cfg._workspaces) > 4096:
+            cfg._workspaces.clear()
+        cfg._workspaces[key] = int(_lib.pk_fp8_workspace_bytes(cfg.packed, op, a, b))
+    return cfg._workspaces[key]
+
+
+class Fp8Cache:
+    """Device memory of an 8-bit cache: the arrays of pk_fp8_cache_layout (`buf`), `states` int32 [n_seq, 4] (tokens held, next position, 0, 0)
+    and, if paged, `page_table` int32 [n_seq, t_capacity / page_tokens], which the caller fills.  `arrays`, `states` and
+    `page_table` may be tensors that the caller has; they stay the same for the cache's life.  track_weight=False leaves out the
+    attention weights (pk_fp8_weights and pk_fp8_evict need them)."""
+
+    def __init__(self, cfg: Fp8Config, device="cuda", arrays: dict | None = None, states: torch.Tensor | None = None,
+                 page_table: torch.Tensor | None = None, track_weight: bool = True):
+        self.cfg = cfg
+        lay = pk_fp8_cache_layout(cfg)
+        self.bytes = {n: lay[n] for n in _FP8_ARRAYS}
+        if arrays is None:
+            arrays = {n: torch.zeros(lay[n] // _FP8_TYPES[n].itemsize, dtype=_FP8_TYPES[n], device=device)
+                      for n in _FP8_ARRAYS if track_weight or n != "weight"}
+        self.buf = dict(arrays)
+        for n in _FP8_ARRAYS:
+            t = self.buf.get(n)
+            if t is None:
+                assert n == "weight", f"the cache needs {n}"
+                continue
+            assert t.dtype == _FP8_TYPES[n] and t.is_contiguous() and t.numel() * t.element_size() >= lay[n], n
+        if states is None:
+            states = torch.zeros((cfg.n_seq, 4), dtype=torch.int32, device=self.buf["k_codes"].device)
+        assert states.dtype == torch.int32 and tuple(states.shape) == (cfg.n_seq, 4) and states.is_contiguous()
+        self.states = states
+        if cfg.page_tokens > 0:
+            shape = (cfg.n_seq, cfg.t_capacity // cfg.page_tokens)
+            if page_table is None:
+                page_table = torch.zeros(shape, dtype=torch.int32, device=states.device)
+            assert page_table.dtype == torch.int32 and tuple(page_table.shape) == shape and page_table.is_contiguous()
+        else:
+            page_table = None
+        self.page_table = page_table
+        tensors = [self.buf.get(n) for n in _FP8_ARRAYS] + [page_table]
+        self.device = states.device
+        assert all(t is None or t.device == self.device for t in tensors), "the tensors of a cache are on one device"
+        self.packed = _pack_fp8_cache(*[0 if t is None else t.data_ptr() for t in tensors])
+
+    @property
+    def lengths(self) -> torch.Tensor:
+        """Tokens held by every sequence (a view of the states)."""
+        return self.states[:, 0]
+
+
+def _fp8_stream(cache: Fp8Cache):
+    # the launches go to the current device's stream, so the memory has to be that device's
+    if cache.device.index != torch.cuda.current_device():
+        raise ValueError(f"the cache is on {cache.device}, the current device is cuda:{torch.cuda.current_device()}")
+    return torch.cuda.current_stream().cuda_stream
+
+
+def _fp8_vectors(cfg: Fp8Config, cache: Fp8Cache, t: torch.Tensor, heads: int, name: str) -> bytes:
+    """The strides of a [n_seq, heads, tokens, d] tensor of the configuration's type."""
+    shape = t.shape
+    if t.dtype != cfg.torch_dtype or len(shape) != 4 or shape[0] != cfg.n_seq or shape[1] != heads or shape[3] != cfg.head_dim:
+        raise ValueError(f"{name}: expected {cfg.torch_dtype} [{cfg.n_seq}, {heads}, tokens, {cfg.head_dim}], got {t.dtype} {list(shape)}")
+    if t.device != cache.device:
+        raise ValueError(f"{name} is on {t.device}, the cache on {cache.device}")
+    s = t.stride()
+    if s[3] != 1:
+        raise ValueError(f"{name}: the elements of a vector must be adjacent")
+    # strides of dimensions of one element carry no meaning
+    return _pack_strides(s[0] if shape[0] > 1 else 0, s[2] if shape[2] > 1 else 0, s[1] if shape[1] > 1 else 0)
+
+
+def _fp8_counts(cfg: Fp8Config, cache: Fp8Cache, counts):
+    if counts is None:
+        return None
+    if counts.dtype != torch.int32 or tuple(counts.shape) != (cfg.n_seq,) or not counts.is_contiguous() or counts.device != cache.device:
+        raise ValueError(f"counts: expected contiguous int32 [{cfg.n_seq}] on {cache.device}")
+    return counts.data_ptr()
+
+
+def _fp8_scores(cfg: Fp8Config, cache: Fp8Cache, softmax_scale, cap, window, slopes) -> bytes:
+    if slopes is None:
+        return _pack_fp8_scores(softmax_scale, cap, window, 0)
+    if slopes.dtype != torch.float32 or tuple(slopes.shape) != (cfg.n_q_heads,) or not slopes.is_contiguous() or slopes.device != cache.device:
+        raise ValueError(f"slopes: expected contiguous float32 [{cfg.n_q_heads}] on {cache.device}")
+    return _pack_fp8_scores(softmax_scale, cap, window, slopes.data_ptr())
+
+
+def _fp8_lse(cfg: Fp8Config, cache: Fp8Cache, lse: torch.Tensor, n: int):
+    if lse.dtype != torch.float32 or tuple(lse.shape) != (cfg.n_seq, cfg.n_q_heads, n) or not lse.is_contiguous() or lse.device != cache.device:
+        raise ValueError(f"lse: expected contiguous float32 [{cfg.n_seq}, {cfg.n_q_heads}, {n}] on {cache.device}")
+    return lse.data_ptr()
+
+
+def _fp8_workspace(cfg: Fp8Config, cache: Fp8Cache, workspace, op: int, a: int, b: int):
+    if workspace is None:
+        need = pk_fp8_workspace_bytes(cfg, op, a, b)
+        workspace = torch.empty(need, dtype=torch.uint8, device=cache.device) if need else None
+    elif workspace.dtype != torch.uint8 or not workspace.is_contiguous() or workspace.device != cache.device:
+        raise ValueError(f"workspace: expected contiguous uint8 on {cache.device}")
+    return workspace
+
+
+def pk_fp8_append(cfg: Fp8Config, cache: Fp8Cache, k_new: torch.Tensor, v_new: torch.Tensor, counts: torch.Tensor | None = None,
+                  states_out: torch.Tensor | None = None):
+    """Append k_new, v_new [n_seq, n_kv_heads, n_new, d] (any strides that are multiples of 8; elements of a vector adjacent) behind the
+    tokens held.  counts int32 [n_seq] on the device: how many of the n_new each sequence takes.  The new states go to the
+    cache's, or to states_out, in which case the cache's stay as they are."""
+    ks, vs = _fp8_vectors(cfg, cache, k_new, cfg.n_kv_heads, "k_new"), _fp8_vectors(cfg, cache, v_new, cfg.n_kv_heads, "v_new")
+    if k_new.shape != v_new.shape:
+        raise ValueError("k_new and v_new differ in shape")
+    out = cache.states if states_out is None else states_out
+    if out is not cache.states and (out.dtype != torch.int32 or tuple(out.shape) != (cfg.n_seq, 4) or not out.is_contiguous() or out.device != cache.device):
+        raise ValueError(f"states_out: expected contiguous int32 [{cfg.n_seq}, 4] on {cache.device}")
+    _check(_lib.pk_fp8_append(cfg.packed, cache.packed, cache.states.data_ptr(), out.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), ks, vs,
+                              k_new.shape[2], _fp8_counts(cfg, cache, counts), _fp8_stream(cache)), "pk_fp8_append")
+    return out
+
+
+def pk_fp8_attention(cfg: Fp8Config, cache: Fp8Cache, q: torch.Tensor, softmax_scale: float, cap: float = 0.0, window: int = 0,
+                     slopes: torch.Tensor | None = None, counts: torch.Tensor | None = None, bound: int | None = None,
+                     out: torch.Tensor | None = None, lse: torch.Tensor | None = None, workspace: torch.Tensor | None = None):
+    """Attention of the last n tokens of every sequence, q [n_seq, n_q_heads, n, d] (or [n_seq, n_q_heads, d] for one), over the
+    tokens that the cache holds -> out, the same shape and type.  Strides as in pk_fp8_append.  cap, window, slopes [n_q_heads]: see
+    include/patternkv.h.  counts int32 [n_seq]: the sequence's queries are the first counts[i] (rows behind them are left as they
+    were).  bound: no sequence holds more tokens than this (default: the capacity); sizes the launch.
+    lse float32 [n_seq, n_q_heads, n] receives the log-sum-exp."""
+    one = q.dim() == 3
+    if one:
+        q = q.unsqueeze(2)
+    qs = _fp8_vectors(cfg, cache, q, cfg.n_q_heads, "q")
+    n = q.shape[2]
+    if out is None:
+        # a token's heads next to each other, as the projection that follows takes them; rows that are not written are zero
+        new = torch.empty if counts is None else torch.zeros
+        o = new((cfg.n_seq, n, cfg.n_q_heads, cfg.head_dim), dtype=q.dtype, device=q.device).transpose(1, 2)
+    else:
+        o = out.unsqueeze(2) if one and out.dim() == 3 else out
+        if o.shape != q.shape:
+            raise ValueError(f"out: expected {list(q.shape)}, got {list(o.shape)}")
+    os_ = _fp8_vectors(cfg, cache, o, cfg.n_q_heads, "out")
+    bound = cfg.t_capacity if bound is None else bound
+    workspace = _fp8_workspace(cfg, cache, workspace, FP8_OP_ATTENTION, n, bound)
+    _check(_lib.pk_fp8_attention(cfg.packed, cache.packed, cache.states.data_ptr(), bound, q.data_ptr(), qs, n, _fp8_counts(cfg, cache, counts),
+                                 _fp8_scores(cfg, cache, softmax_scale, cap, window, slopes), o.data_ptr(), os_,
+                                 None if lse is None else _fp8_lse(cfg, cache, lse, n), None if workspace is None else workspace.data_ptr(),
+                                 0 if workspace is None else workspace.numel(), _fp8_stream(cache)), "pk_fp8_attention")
+    return out if out is not None else o.squeeze(2) if one else o
+
+
+def pk_fp8_weights(cfg: Fp8Config, cache: Fp8Cache, q: torch.Tensor, lse: torch.Tensor, softmax_scale: float, cap: float = 0.0, window: int = 0,
+                   slopes: torch.Tensor | None = None, counts: torch.Tensor | None = None, bound: int | None = None, accumulate: bool = True):
+    """Add (accumulate=False: set) the attention weight that every cached token got from the queries of a pk_fp8_attention call, whose
+    arguments and lse these are, in cache.buf["weight"] [n_seq, n_kv_heads, t_capacity]."""
+    if q.dim() == 3:
+        q = q.unsqueeze(2)
+    qs = _fp8_vectors(cfg, cache, q, cfg.n_q_heads, "q")
+    n = q.shape[2]
+    bound = cfg.t_capacity if bound is None else bound
+    _check(_lib.pk_fp8_weights(cfg.packed, cache.packed, cache.states.data_ptr(), bound, q.data_ptr(), qs, n, _fp8_counts(cfg, cache, counts),
+                               _fp8_scores(cfg, cache, softmax_scale, cap, window, slopes), _fp8_lse(cfg, cache, lse, n), 1 if accumulate else 0,
+                               _fp8_stream(cache)), "pk_fp8_weights")
+
+
+def pk_fp8_evict(cfg: Fp8Config, cache: Fp8Cache, to_cfg: Fp8Config, to: Fp8Cache, budget: int, keep_first: int = 0, keep_last: int = 0,
+                 workspace: torch.Tensor | None = None):
+    """Bring every sequence down to `budget` tokens in another cache: the first keep_first, the last keep_last, and of the others those
+    with the largest weight."""
+    if to.device != cache.device:
+        raise ValueError(f"the caches are on {cache.device} and {to.device}")
+    workspace = _fp8_workspace(cfg, cache, workspace, FP8_OP_EVICT, budget, 0)
+    _check(_lib.pk_fp8_evict(cfg.packed, cache.packed, cache.states.data_ptr(), to_cfg.packed, to.packed, to.states.data_ptr(), budget, keep_first,
+                             keep_last, None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.numel(),
+                             _fp8_stream(cache)), "pk_fp8_evict")

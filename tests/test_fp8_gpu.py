@@ -1,0 +1,483 @@
+"""The 8-bit cache on the GPU against its definition in 64 bits.
+
+Codes, scales, positions and the choice of an eviction are exact.  A score of magnitude sum S = scale * sum |q k| + |bias| is off by at most
+(d + 8) roundings of binary32 relative to S (d products into a binary32 accumulator, then factor, cap, bias, reference);
+a softmax weight by twice that, its numerator by fp16's half step 2^-11 on top, and by half of fp16's smallest step, 2^-25, relative to the largest
+numerator (kept up to 2^6 smaller where V scales differ); an output by half a step of its own type on top.
+"""
+import math
+
+import numpy as np
+import pytest
+
+import fp8_reference as ref
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+
+@pytest.fixture(scope="module")
+def pk():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2510_05176_amd import patternkv
+    return patternkv
+
+
+EPS = {torch.float16: 2.0 ** -11, torch.bfloat16: 2.0 ** -8}
+
+
+class Pair:
+    """A cache on the GPU and the same sequences in 64 bits."""
+
+    def __init__(self, pk, seed, n_seq=2, hkv=2, r=4, d=128, block=64, cap=1024, bf16=False, page=0, extra_pages=3, spread=1.0):
+        self.pk, self.rng, self.spread = pk, np.random.default_rng(seed), spread
+        n_pages = n_seq * (cap // page) + extra_pages if page else 0
+        self.cfg = pk.Fp8Config(n_seq=n_seq, n_kv_heads=hkv, n_q_heads=hkv * r, head_dim=d, block=block, t_capacity=cap,
+                                dtype=pk.DTYPE_BF16 if bf16 else pk.DTYPE_FP16, page_tokens=page, n_pages=n_pages)
+        self.cache = self.new_cache(self.cfg)
+        self.seqs = [ref.Sequence(hkv, block, d) for _ in range(n_seq)]
+        self.dtype = self.cfg.torch_dtype
+
+    def new_cache(self, cfg):
+        cache = self.pk.Fp8Cache(cfg)
+        for n in ("k_codes", "v_codes"):   # what lies behind the tokens held is anything, NaN codes included
+            cache.buf[n].copy_(torch.from_numpy(self.rng.integers(0, 256, cache.buf[n].numel()).astype(np.uint8)))
+        for n in ("k_scale", "v_scale", "weight"):
+            cache.buf[n].fill_(math.nan)
+        if cfg.page_tokens:
+            cache.page_table.copy_(torch.from_numpy(self.rng.permutation(cfg.n_pages)[:cache.page_table.numel()].astype(np.int32)).view(cache.page_table.shape))
+        return cache
+
+    def rows(self, cfg, cache, seq, head):
+        cap, page = cfg.t_capacity, cfg.page_tokens
+        t = np.arange(cap)
+        if page:
+            table = cache.page_table[seq].cpu().numpy().astype(np.int64)
+            return (table[t // page] * cfg.n_kv_heads + head) * page + t % page
+        return (seq * cfg.n_kv_heads + head) * cap + t
+
+    def vectors(self, n, heads, scale=1.0):
+        """[n_seq][heads][n][d] of the 16-bit type, a view of a wider tensor; and in 64 bits"""
+        cfg = self.cfg
+        x = self.rng.standard_normal((cfg.n_seq, n, heads, cfg.head_dim)) * scale
+        x *= np.exp(self.spread * self.rng.standard_normal((cfg.n_seq, n, 1, 1)))
+        wide = torch.zeros((cfg.n_seq, n, heads + 1, cfg.head_dim + 8), dtype=self.dtype, device="cuda")
+        t = wide[:, :, :heads, :cfg.head_dim].transpose(1, 2)
+        t.copy_(torch.from_numpy(x).transpose(1, 2).to(self.dtype))
+        return t, t.double().cpu().numpy()
+
+    def append(self, n, counts=None, k=None, v=None, **kw):
+        (kt, kn), (vt, vn) = k or self.vectors(n, self.cfg.n_kv_heads), v or self.vectors(n, self.cfg.n_kv_heads)
+        c = None if counts is None else torch.tensor(counts, dtype=torch.int32, device="cuda")
+        got = self.pk.pk_fp8_append(self.cfg, self.cache, kt, vt, counts=c, **kw)
+        for b, s in enumerate(self.seqs):
+            m = n if counts is None else counts[b]
+            m = min(m, self.cfg.t_capacity - s.length)
+            s.append(kn[b][:, :m], vn[b][:, :m])
+        return got
+
+    def check(self, cfg=None, cache=None, seqs=None, weights=True):
+        cfg, cache, seqs = cfg or self.cfg, cache or self.cache, seqs or self.seqs
+        d, B = cfg.head_dim, cfg.block
+        codes = {n: cache.buf[n + "_codes"].cpu().numpy().reshape(-1, d) for n in "kv"}
+        scale = {n: cache.buf[n + "_scale"].cpu().numpy() for n in "kv"}
+        pos = cache.buf["pos"].cpu().numpy().reshape(cfg.n_seq, cfg.n_kv_heads, -1)
+        weight = cache.buf["weight"].cpu().numpy().reshape(pos.shape)
+        states = cache.states.cpu().numpy()
+        for b, s in enumerate(seqs):
+            assert list(states[b]) == [s.length, s.next, 0, 0], b
+            for h in range(cfg.n_kv_heads):
+                at = self.rows(cfg, cache, b, h)[:s.length]
+                assert np.array_equal(pos[b, h, :s.length], s.pos[h])
+                if weights:
+                    assert np.array_equal(weight[b, h, :s.length], s.weight[h].astype(np.float32), equal_nan=True)
+                for n, want in (("k", s.k[h]), ("v", s.v[h])):
+                    nan = np.isnan(ref.VALUES[want.codes])
+                    have = codes[n][at]
+                    assert np.array_equal((have & 127) == 127, nan), (b, h, n)
+                    assert np.array_equal(np.where(nan, 0, have), np.where(nan, 0, want.codes)), (b, h, n)
+                    sc = scale[n][at[::B] // B]
+                    assert np.array_equal(np.abs(sc), 2.0 ** np.array(want.exp, float)), (b, h, n)
+                    assert np.array_equal(np.signbit(sc), np.array(want.flag, bool)), (b, h, n)
+
+    def attend(self, n, counts=None, scale=None, cap=0.0, window=0, slopes=False, weights=None, bound=None, q=None, **kw):
+        """A call against the definition; weights: None, or whether they accumulate"""
+        cfg = self.cfg
+        scale = cfg.head_dim ** -0.5 if scale is None else scale
+        qt, qn = q or self.vectors(n, cfg.n_q_heads)
+        c = None if counts is None else torch.tensor(counts, dtype=torch.int32, device="cuda")
+        sl = torch.exp2(-torch.arange(1, cfg.n_q_heads + 1, device="cuda").float()) if slopes else None
+        lse = torch.full((cfg.n_seq, cfg.n_q_heads, n), 7.0, device="cuda")
+        out = torch.full((cfg.n_seq, cfg.n_q_heads, n, cfg.head_dim), 7.0, dtype=self.dtype, device="cuda")
+        self.pk.pk_fp8_attention(cfg, self.cache, qt, scale, cap=cap, window=window, slopes=sl, counts=c, bound=bound, out=out, lse=lse, **kw)
+        before = self.cache.buf["weight"].cpu().numpy().reshape(cfg.n_seq, cfg.n_kv_heads, -1).copy()
+        if weights is not None:
+            self.pk.pk_fp8_weights(cfg, self.cache, qt, lse, scale, cap=cap, window=window, slopes=sl, counts=c, bound=bound, accumulate=weights)
+        got, got_lse = out.double().cpu().numpy(), lse.double().cpu().numpy()
+        after = self.cache.buf["weight"].cpu().numpy().reshape(before.shape)
+        r = cfg.n_q_heads // cfg.n_kv_heads
+        for b, s in enumerate(self.seqs):
+            m = n if counts is None else counts[b]
+            assert (got[b, :, m:] == 7.0).all() and (got_lse[b, :, m:] == 7.0).all()   # rows behind the sequence's
+            if m:
+                want, want_lse, soft, mag, size = s.attention(qn[b][:, :m], scale, cap=cap, window=window, slopes=None if sl is None else sl.double().cpu().numpy())
+                off = (cfg.head_dim + 8) * 2.0 ** -24 * size          # of a score
+                nan = np.isnan(want)
+                top = max([np.nanmax(np.abs(x.values()), initial=0.0) for x in s.v] + [0.0])
+                tol = EPS[self.dtype] * np.abs(want) + (2.0 ** -11 + 2 * off[..., None]) * mag + s.length * 2.0 ** -25 * 2 * top + 2.0 ** -25
+                assert np.array_equal(np.isnan(got[b, :, :m]), nan), b
+                bad = ~nan & ~(np.abs(got[b, :, :m] - want) <= tol)
+                assert not bad.any(), (b, np.argwhere(bad)[:4], (np.abs(got[b, :, :m] - want) / tol)[bad][:4])
+                empty = want_lse == -np.inf
+                assert np.array_equal(got_lse[b, :, :m] == -np.inf, empty) and (got[b, :, :m][empty] == 0).all()
+                ok = ~empty & ~np.isnan(want_lse)
+                assert np.array_equal(np.isnan(got_lse[b, :, :m]), np.isnan(want_lse))
+                far = np.abs(got_lse[b, :, :m] - want_lse)[ok]
+                assert (far <= (off + s.length * 2.0 ** -24 + 2.0 ** -22 * (np.abs(want_lse) + 2))[ok]).all()
+            if weights is not None:
+                soft = soft if m else np.zeros((cfg.n_q_heads, 0, s.length))
+                rel = (2 * off + s.length * 2.0 ** -24 + 2.0 ** -21 * (np.abs(np.where(empty, 0.0, want_lse)) + 4))[..., None] if m else 0.0
+                for h in range(cfg.n_kv_heads):
+                    mine = soft[h * r:(h + 1) * r]
+                    want_w, tol_w = mine.sum((0, 1)), (mine * rel[h * r:(h + 1) * r]).sum((0, 1)) if m else 0.0
+                    old = before[b, h, :s.length].astype(np.float64) if weights else 0.0
+                    total = want_w + old
+                    room = tol_w + 2.0 ** -24 * (np.abs(total) + (r * m + 4) * want_w) + 1e-37
+                    assert (np.abs(after[b, h, :s.length] - total) <= room).all(), (b, h)
+                    assert np.array_equal(after[b, h, s.length:], before[b, h, s.length:], equal_nan=True)
+                    s.weight[h] = after[b, h, :s.length].astype(np.float64)
+        return out, lse
+
+
+APPENDS = [  # d, block, bf16, page
+    (128, 64, False, 0), (128, 64, True, 128), (64, 32, True, 0), (96, 32, False, 256), (96, 64, True, 0), (256, 128, False, 0), (256, 32, True, 128), (64, 128, False, 0)]
+
+
+@pytest.mark.parametrize("d,block,bf16,page", APPENDS)
+def test_append(pk, d, block, bf16, page):
+    """In pieces of every kind: prompts, single tokens into begun blocks, unequal counts, nothing; vectors grow, so that begun blocks get
+    larger scales."""
+    p = Pair(pk, 1, n_seq=3, hkv=2, d=d, block=block, cap=512, bf16=bf16, page=page)
+    p.append(70, counts=[70, 1, 0])
+    p.check()
+    for step in range(4):
+        big = 4.0 ** step
+        p.append(1, k=p.vectors(1, 2, big), v=p.vectors(1, 2, big))
+    p.check()
+    p.append(130, counts=[0, 130, 65])
+    p.append(33)
+    p.append(3, counts=[3, 2, 1], k=p.vectors(3, 2, 2.0 ** -14), v=p.vectors(3, 2, 0.0))
+    p.check()
+
+
+def test_append_stops_at_the_capacity(pk):
+    p = Pair(pk, 2, n_seq=2, cap=128, block=64)
+    p.append(100, counts=[100, 60])
+    p.append(50)
+    p.check()
+    assert p.cache.lengths.tolist() == [128, 110]
+    p.append(1)
+    p.append(128)
+    p.check()
+    assert p.cache.lengths.tolist() == [128, 128]
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+def test_append_of_extreme_values(pk, bf16):
+    """Zeros, the type's largest and smallest values, infinities and NaN, which leave the rest of their block alone."""
+    p = Pair(pk, 3, n_seq=1, hkv=2, d=64, block=32, cap=256, bf16=bf16)
+    info = torch.finfo(p.dtype)
+    x = p.rng.standard_normal((1, 100, 2, 64))
+    x[0, :5] = 0.0
+    x[0, 33, 0, 3], x[0, 34, 1, 0] = math.inf, math.nan
+    x[0, 64:96, 1] = -math.inf
+    x[0, 40:64, 1] *= info.max / 8
+    x[0, 70, 0] = info.smallest_normal
+    x[0, 96:, 0] = info.tiny / 4
+    x[0, 96:, 1] = info.max
+    x = np.clip(x, -info.max, info.max, out=x, where=np.isfinite(x))
+    t = torch.from_numpy(x).to(p.dtype).cuda().transpose(1, 2)
+    n = t.double().cpu().numpy()
+    half = (t[:, :, :50], n[:, :, :50])
+    rest = (t[:, :, 50:], n[:, :, 50:])
+    p.append(50, k=half, v=half)
+    p.append(50, k=rest, v=rest)
+    p.check()
+
+
+def test_append_beside_the_old_states(pk):
+    """states_out leaves the cache's own states: drafts are appended, dropped, and others take their place."""
+    p = Pair(pk, 4, n_seq=2, d=128, cap=256)
+    p.append(61)
+    old = p.cache.states.clone()
+    out = torch.full_like(old, 9)
+    k, v = p.vectors(5, 2), p.vectors(5, 2)
+    assert p.pk.pk_fp8_append(p.cfg, p.cache, k[0], v[0], states_out=out) is out
+    assert torch.equal(p.cache.states, old) and out.tolist() == [[66, 66, 0, 0]] * 2
+    p.append(5, k=k, v=v)     # the same ones again, for good: the begun block's scale is there already
+    p.check()
+    none = torch.zeros(2, dtype=torch.int32, device="cuda")
+    p.pk.pk_fp8_append(p.cfg, p.cache, k[0], v[0], counts=none, states_out=out)
+    assert torch.equal(out, p.cache.states)
+    p.check()
+
+
+ATTENDS = [
+    # lengths, n, r, d, block, bf16, page, options
+    ([1, 5, 64, 65], 1, 4, 128, 64, False, 0, {}),
+    ([1, 333, 1000, 517], 1, 1, 128, 32, True, 128, {}),
+    ([130, 700, 2, 1024], 1, 7, 256, 128, True, 0, {}),
+    ([130, 700, 2, 1024], 1, 16, 96, 64, False, 256, {}),
+    ([130, 700, 25, 1024], 1, 24, 64, 32, True, 0, {}),
+    ([130, 700, 25, 1024], 1, 64, 128, 64, False, 0, {}),
+    ([9, 700, 64, 1000], 5, 4, 128, 32, False, 128, {}),
+    ([9, 700, 64, 1000], 5, 5, 128, 64, True, 0, dict(cap=20.0)),
+    ([100, 333, 65, 1000], 37, 2, 64, 64, False, 0, {}),
+    ([100, 333, 65, 1000], 65, 3, 96, 32, True, 128, dict(cap=5.0)),
+    ([200, 333, 129, 1000], 129, 4, 128, 64, True, 0, {}),
+    ([200, 333, 129, 1000], 129, 2, 256, 64, False, 0, {}),
+    ([9, 700, 64, 1000], 3, 4, 128, 64, False, 0, dict(window=1)),
+    ([9, 700, 64, 1000], 3, 4, 128, 64, False, 256, dict(window=100, slopes=True)),
+    ([200, 333, 129, 1000], 100, 4, 64, 128, True, 0, dict(window=90)),
+    ([200, 333, 129, 1000], 100, 1, 128, 64, False, 0, dict(window=64, slopes=True, cap=10.0)),
+    ([9, 700, 64, 1000], 1, 4, 256, 32, True, 128, dict(slopes=True)),
+    ([9, 700, 64, 1000], 2, 4, 96, 64, True, 0, dict(window=33, cap=30.0)),
+]
+
+
+@pytest.mark.parametrize("lengths,n,r,d,block,bf16,page,how", ATTENDS)
+def test_attention_and_weights(pk, lengths, n, r, d, block, bf16, page, how):
+    p = Pair(pk, 5, n_seq=4, hkv=2, r=r, d=d, block=block, cap=1024, bf16=bf16, page=page, spread=0.5)
+    p.append(max(lengths), counts=lengths)
+    p.attend(n, weights=False, **how)
+    p.attend(n, weights=True, **how)
+    p.attend(n, counts=[n, n // 2, 0, max(n - 1, 0)], weights=True, bound=64, **how)   # a bound below the lengths costs time only
+
+
+def test_empty_sequences(pk):
+    """Nothing held, and more queries than tokens: no row sees anything, or only the last do."""
+    p = Pair(pk, 6, n_seq=3, cap=256)
+    p.attend(1, weights=True)
+    p.attend(4, weights=False)
+    p.append(3, counts=[0, 3, 1])
+    for n in (1, 2, 5, 70):
+        p.attend(n, weights=False)
+        p.attend(n, weights=False, counts=[n, 0, min(n, 2)], window=2)
+
+
+def test_few_heads_and_queries_share_tiles(pk):
+    """Every number of rows around the tile sizes."""
+    p = Pair(pk, 7, n_seq=1, hkv=1, r=1, d=64, cap=320)
+    p.append(300)
+    for n in (15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 300):
+        p.attend(n, weights=False)
+
+
+@pytest.mark.parametrize("n,how", [(1, {}), (1, dict(window=40)), (6, {}), (6, dict(window=40)), (150, {}), (150, dict(window=100))])
+@pytest.mark.parametrize("d,block", [(128, 64), (96, 32), (256, 128)])
+def test_masked_values_do_not_reach_a_row(pk, n, how, d, block):
+    """NaN in K and V at tokens that some rows see and others do not, and in whole blocks; and behind the tokens held (every
+    cache of these tests starts with NaN codes and scales there)."""
+    p = Pair(pk, 8, n_seq=2, hkv=1, r=2, d=d, block=block, cap=512)
+    k, v = p.vectors(300, 1), p.vectors(300, 1)
+    for t, c in ((298, 5), (297, 70 % d), (220, d - 1), (150, 0)):
+        v[0][0, 0, t, c] = math.nan
+    v[0][1, 0, 10:90] = math.inf
+    k[0][1, 0, 20, 3] = math.nan
+    k[0][0, 0, 170, 1] = -math.inf
+    k, v = (k[0], k[0].double().cpu().numpy()), (v[0], v[0].double().cpu().numpy())
+    p.append(300, counts=[300, 299], k=k, v=v)
+    p.check()
+    p.attend(n, **how)
+
+
+def test_scores_of_any_size(pk):
+    """Queries and keys that make scores of thousands, of nothing, and of both signs; negative scale."""
+    p = Pair(pk, 9, n_seq=1, hkv=1, r=4, d=128, cap=512)
+    p.append(400, k=p.vectors(400, 1, 30.0))
+    q = p.vectors(2, 4, 60.0)
+    p.attend(2, q=q)
+    p.attend(2, q=q, scale=-0.01, weights=False)
+    p.attend(2, q=q, cap=40.0)
+    p.attend(2, q=q, scale=0.0, weights=False)
+    q[0].zero_()
+    p.attend(2, q=(q[0], q[1] * 0.0), weights=False)
+
+
+@pytest.mark.parametrize("bf16", [False, True])
+def test_value_scales_of_every_size(pk, bf16):
+    """Blocks whose V scales differ by up to 2^24 (bfloat16: 2^70) in both orders, the large ones with little softmax weight: the rest of
+    the result keeps its precision."""
+    p = Pair(pk, 10, n_seq=1, hkv=1, r=2, d=64, block=32, cap=512, bf16=bf16, spread=0.0)
+    k, v = p.vectors(512, 1), p.vectors(512, 1)
+    sizes = [0, 3, -4, 10, 2, -9, 12, 1, 0, 5, -3, 8, 4, 0, 11, 2] if not bf16 else [0, 3, -40, 30, 2, -9, 12, 1, 0, 25, -35, 8, 4, 0, 11, 2]
+    for i, e in enumerate(sizes):
+        v[0][0, 0, 32 * i:32 * i + 32] *= 2.0 ** e
+    q = p.vectors(1, 2, 4.0)
+    for i in (3, 6, 9, 14):       # the keys of the large blocks point away from both queries
+        k[0][0, 0, 32 * i:32 * i + 32] -= (q[0][0, 0, 0] + q[0][0, 1, 0]) * 0.5
+    p.append(512, k=(k[0], k[0].double().cpu().numpy()), v=(v[0], v[0].double().cpu().numpy()))
+    p.attend(1, q=q)
+
+
+EVICTS = [(128, 64, 0, 0, 100, 4, 16), (64, 32, 128, 0, 64, 0, 0), (96, 32, 0, 128, 77, 0, 77), (256, 128, 256, 128, 129, 1, 0), (128, 64, 0, 0, 1, 0, 0), (64, 64, 0, 0, 63, 31, 32)]
+
+
+@pytest.mark.parametrize("d,block,page,to_page,budget,first,last", EVICTS)
+def test_evict(pk, d, block, page, to_page, budget, first, last):
+    """Unequal lengths on both sides of the budget; equal weights, zeros of both signs, infinite and NaN ones; NaN codes move along."""
+    p = Pair(pk, 11, n_seq=4, hkv=2, d=d, block=block, cap=512, page=page)
+    k = p.vectors(500, 2)
+    k[0][1, 0, 450, 2] = math.nan
+    p.append(500, counts=[500, 499, 0, budget], k=(k[0], k[0].double().cpu().numpy()))
+    w = p.cache.buf["weight"].view(4, 2, -1)
+    for b, s in enumerate(p.seqs):
+        for h in range(2):
+            x = p.rng.random(s.length).astype(np.float32) ** 4
+            if h == 1:
+                x = np.float32(p.rng.integers(0, 3, s.length))   # many ties
+                x[x == 0] *= np.float32(-1.0) ** np.arange((x == 0).sum())
+            if b == 1 and s.length > 60:
+                x[20:40], x[50] = math.nan, math.inf
+            s.weight[h] = x.astype(np.float64)
+            w[b, h, :s.length] = torch.from_numpy(x).cuda()
+    n_pages = 4 * (256 // to_page) + 2 if to_page else 0
+    to_cfg = pk.Fp8Config(n_seq=4, n_kv_heads=2, n_q_heads=8, head_dim=d, block=block, t_capacity=256, page_tokens=to_page, n_pages=n_pages)
+    to = p.new_cache(to_cfg)
+    before = {n: t.clone() for n, t in p.cache.buf.items()}
+    pk.pk_fp8_evict(p.cfg, p.cache, to_cfg, to, budget, keep_first=first, keep_last=last)
+    p.check(to_cfg, to, [s.evict(budget, first, last) for s in p.seqs])
+    assert all(torch.equal(before[n].view(torch.uint8), p.cache.buf[n].view(torch.uint8)) for n in before)
+
+
+def test_evict_larger_budget_than_the_cache(pk):
+    p = Pair(pk, 12, n_seq=2, cap=128)
+    p.append(128, counts=[128, 5])
+    to_cfg = pk.Fp8Config(n_seq=2, n_kv_heads=2, n_q_heads=8, t_capacity=1024)
+    to = p.new_cache(to_cfg)
+    pk.pk_fp8_evict(p.cfg, p.cache, to_cfg, to, 1024)
+    p.check(to_cfg, to, [s.evict(1024, 0, 0) for s in p.seqs])
+
+
+def test_evict_long(pk):
+    """More tokens than the selection's workgroup has threads, every weight from few values."""
+    p = Pair(pk, 13, n_seq=1, hkv=1, r=1, d=64, block=128, cap=8192)
+    p.append(8191)
+    x = np.float32(p.rng.integers(0, 50, 8191) / 7.0)
+    p.seqs[0].weight[0] = x.astype(np.float64)
+    p.cache.buf["weight"][:8191] = torch.from_numpy(x).cuda()
+    to_cfg = pk.Fp8Config(n_seq=1, n_kv_heads=1, n_q_heads=1, head_dim=64, block=128, t_capacity=4096)
+    to = p.new_cache(to_cfg)
+    pk.pk_fp8_evict(p.cfg, p.cache, to_cfg, to, 3001, keep_first=3, keep_last=100)
+    p.check(to_cfg, to, [p.seqs[0].evict(3001, 3, 100)])
+
+
+@pytest.mark.parametrize("bf16,page", [(False, 0), (True, 128)])
+def test_a_serving_loop(pk, bf16, page):
+    """Prompts, generation steps with weights, eviction, further steps with window and distance bias over the gaps, drafts, eviction
+    back."""
+    p = Pair(pk, 14, n_seq=2, hkv=2, r=4, d=128, block=32, cap=512, bf16=bf16, page=page, spread=0.5)
+    p.append(300, counts=[300, 170])
+    p.attend(32, weights=False)
+    for _ in range(3):
+        p.append(1)
+        p.attend(1, weights=True)
+    first_cfg, first = p.cfg, p.cache
+    to_cfg = pk.Fp8Config(n_seq=2, n_kv_heads=2, n_q_heads=8, head_dim=128, block=32, t_capacity=256, dtype=p.cfg.dtype)
+    to = p.new_cache(to_cfg)
+    pk.pk_fp8_evict(p.cfg, p.cache, to_cfg, to, 150, keep_first=4, keep_last=20)
+    p.cfg, p.cache, p.seqs = to_cfg, to, [s.evict(150, 4, 20) for s in p.seqs]
+    p.check()
+    for _ in range(3):
+        p.append(1)
+        p.attend(1, weights=True, window=60, slopes=True)
+    p.append(5)
+    p.attend(5, weights=True, window=200, slopes=True, cap=20.0)
+    p.check()
+    first.states.zero_()
+    pk.pk_fp8_evict(p.cfg, p.cache, first_cfg, first, 64, keep_first=1, keep_last=30)
+    p.cfg, p.cache, p.seqs = first_cfg, first, [s.evict(64, 1, 30) for s in p.seqs]
+    p.append(1)
+    p.attend(1, slopes=True)
+    p.check()
+
+
+def test_replayed_graph_grows_the_sequences(pk):
+    """A generation step (append in place, attention, weights) captured once and replayed with new tokens, eager work and waits in
+    between, against the same steps without a graph."""
+    a, b = (Pair(pk, 15, n_seq=3, hkv=2, r=4, cap=1024) for _ in range(2))
+    a.append(200, counts=[200, 63, 0])
+    b.append(200, counts=[200, 63, 0])
+    new = [(a.vectors(1, 2)[0], a.vectors(1, 2)[0], a.vectors(1, 8)[0]) for _ in range(6)]
+    k, v, q = (t.clone() for t in new[0])
+    out, lse = torch.zeros(3, 8, 1, 128, dtype=torch.float16, device="cuda"), torch.zeros(3, 8, 1, device="cuda")
+
+    def step(p, k, v, q, out, lse):
+        pk.pk_fp8_append(p.cfg, p.cache, k, v)
+        pk.pk_fp8_attention(p.cfg, p.cache, q, 0.09, out=out, lse=lse)
+        pk.pk_fp8_weights(p.cfg, p.cache, q, lse, 0.09)
+
+    step(a, k, v, q, out, lse)       # everything the launches need is loaded before the capture
+    step(b, k, v, q, out, lse)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(a, k, v, q, out, lse)
+    for kk, vv, qq in new[1:]:
+        k.copy_(kk), v.copy_(vv), q.copy_(qq)
+        graph.replay()
+        out2, lse2 = torch.zeros_like(out), torch.zeros_like(lse)
+        step(b, kk, vv, qq, out2, lse2)
+        torch.cuda.synchronize()
+        assert torch.equal(out, out2) and torch.equal(lse, lse2) and torch.equal(a.cache.states, b.cache.states)
+        held = b.cache.lengths.max().item()
+        for n in ("pos", "weight"):
+            for s, have in enumerate(b.cache.lengths.tolist()):
+                assert torch.equal(a.cache.buf[n].view(3, 2, -1)[s, :, :have], b.cache.buf[n].view(3, 2, -1)[s, :, :have])
+        assert held > 200
+
+
+def test_another_stream(pk):
+    p = Pair(pk, 16, n_seq=2, cap=1024)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        p.append(700)
+        p.attend(1, weights=False)
+    s.synchronize()
+    p.check()
+
+
+def test_many_appends_in_place_count_once(pk):
+    """The state moves once per call, however many workgroups an append has."""
+    p = Pair(pk, 17, n_seq=1, hkv=4, r=1, d=64, block=32, cap=8192)
+    t = torch.randn(1, 4, 1000, 64, device="cuda").half()
+    for i in range(1, 9):
+        pk.pk_fp8_append(p.cfg, p.cache, t, t)
+        assert p.cache.states.tolist() == [[min(1000 * i, 8192), min(1000 * i, 8192), 0, 0]]
+
+
+def test_a_stream_of_more_than_4_gib(pk):
+    """Byte offsets inside a stream that need more than 32 bits: the same tokens at the end of a long stream and in a short one."""
+    cap = 1 << 25
+    long_cfg = pk.Fp8Config(n_seq=1, n_kv_heads=1, n_q_heads=4, head_dim=256, t_capacity=cap)
+    short_cfg = pk.Fp8Config(n_seq=1, n_kv_heads=1, n_q_heads=4, head_dim=256, t_capacity=512)
+    long, short = pk.Fp8Cache(long_cfg), pk.Fp8Cache(short_cfg)
+    start = cap - 448
+    long.states.copy_(torch.tensor([[start, start, 0, 0]]))
+    g = torch.Generator().manual_seed(3)
+    k, v, q = (torch.randn(1, h, n, 256, generator=g).half().cuda() for h, n in ((1, 448), (1, 448), (4, 2)))
+    got = []
+    for cfg, cache in ((long_cfg, long), (short_cfg, short)):
+        pk.pk_fp8_append(cfg, cache, k, v)
+        lse = torch.zeros(1, 4, 2, device="cuda")
+        out = pk.pk_fp8_attention(cfg, cache, q, 0.1, window=440, lse=lse, bound=512)
+        pk.pk_fp8_weights(cfg, cache, q, lse, 0.1, window=440, accumulate=False)
+        got.append((out, lse))
+    assert long.states.tolist() == [[cap, cap, 0, 0]]
+    assert torch.equal(long.buf["k_codes"][start * 256:], short.buf["k_codes"][:448 * 256])
+    assert torch.equal(long.buf["v_codes"][start * 256:], short.buf["v_codes"][:448 * 256])
+    assert torch.equal(long.buf["weight"][start:], short.buf["weight"][:448])
+    assert torch.equal(got[0][1], got[1][1]) and torch.equal(got[0][0], got[1][0])
