@@ -48,22 +48,22 @@ struct Shape {
     static constexpr int kVWords = (D + 63) / 64;  // of V: a sixteenth row (96 channels: one word of the first 64, half a word of the rest)
 };
 
+// A lane's part of a row: `tile` points to a tile's first row and is the same for all lanes, `off` is the lane's own offset, so that an
+// address takes no vector registers beyond that.
 template <int D>
-__device__ __forceinline__ void load_k(uint32_t (&k)[D / 16], const uint8_t *row, int g)
+__device__ __forceinline__ void load_k(uint32_t (&k)[D / 16], const uint8_t *tile, uint32_t off)
 {
     if constexpr (D == 96) {
-        const uint2 *p = reinterpret_cast<const uint2 *>(row + g * 24);
 #pragma unroll
         for (int i = 0; i < 3; ++i) {
-            const uint2 v = p[i];
+            const uint2 v = *reinterpret_cast<const uint2 *>(tile + off + 8 * i);
             k[2 * i] = v.x;
             k[2 * i + 1] = v.y;
         }
     } else {
-        const uint4 *p = reinterpret_cast<const uint4 *>(row + g * (D / 4));
 #pragma unroll
         for (int i = 0; i < D / 64; ++i) {
-            const uint4 v = p[i];
+            const uint4 v = *reinterpret_cast<const uint4 *>(tile + off + 16 * i);
             k[4 * i] = v.x;
             k[4 * i + 1] = v.y;
             k[4 * i + 2] = v.z;
@@ -71,20 +71,21 @@ __device__ __forceinline__ void load_k(uint32_t (&k)[D / 16], const uint8_t *row
         }
     }
 }
+// n: which sixteenth of the row, off: its offset
 template <int D>
-__device__ __forceinline__ void load_v(uint32_t (&v)[Shape<D>::kVWords], const uint8_t *row, int m)
+__device__ __forceinline__ void load_v(uint32_t (&v)[Shape<D>::kVWords], const uint8_t *row, uint32_t off, uint32_t n)
 {
     if constexpr (D == 64) {
-        v[0] = *reinterpret_cast<const uint32_t *>(row + 4 * m);
+        v[0] = *reinterpret_cast<const uint32_t *>(row + off);
     } else if constexpr (D == 96) {
-        v[0] = *reinterpret_cast<const uint32_t *>(row + 4 * m);
-        v[1] = *reinterpret_cast<const uint16_t *>(row + 64 + 2 * m);
+        v[0] = *reinterpret_cast<const uint32_t *>(row + off);
+        v[1] = *reinterpret_cast<const uint16_t *>(row + (off + 64 - 2 * n));
     } else if constexpr (D == 128) {
-        const uint2 w = *reinterpret_cast<const uint2 *>(row + 8 * m);
+        const uint2 w = *reinterpret_cast<const uint2 *>(row + off);
         v[0] = w.x;
         v[1] = w.y;
     } else {
-        const uint4 w = *reinterpret_cast<const uint4 *>(row + 16 * m);
+        const uint4 w = *reinterpret_cast<const uint4 *>(row + off);
         v[0] = w.x;
         v[1] = w.y;
         v[2] = w.z;
@@ -274,14 +275,25 @@ __global__ __launch_bounds__(kThreads, 2) void fp8_attention_kernel(Fp8Attention
     const int split = rest % a.splits, group = rest / a.splits;
     const int row0 = BY_ROWS ? (group * kWaves + wave) * 16 * RT : group * 16 * RT;
 
+    // queries: in registers for one tile of up to 128 channels, else in LDS (the registers then hold two tiles' results or 256 channels' of one)
+    constexpr bool kQueriesInLds = RT > 1 || D == 256;
+    __shared__ half8v sm_q[kQueriesInLds ? kWaves : 1][kQueriesInLds ? RT : 1][kQueriesInLds ? S::kSteps : 1][64];
     Row row[RT];
-    half8v qf[RT][S::kSteps];
+    half8v q_reg[S::kSteps];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
         const int at = row0 + 16 * rt + n;
         row[rt] = row_of(a.in, p, at);
-        load_query<D>(qf[rt], row[rt].factor, a.in, p.seq, p.kvh, at, at < p.count * a.in.r, g);
+        load_query<D>(q_reg, row[rt].factor, a.in, p.seq, p.kvh, at, at < p.count * a.in.r, g);
+        if constexpr (kQueriesInLds)   // of the wave's own: nothing to wait for but its own stores
+#pragma unroll
+            for (int s = 0; s < S::kSteps; ++s) sm_q[wave][rt][s][lane] = q_reg[s];
     }
+    int q_lane = lane;
+    const auto query = [&](int rt, int s) -> half8v {
+        if constexpr (kQueriesInLds) return sm_q[wave][rt][s][q_lane];
+        else return q_reg[s];
+    };
     int lo, hi;
     key_range(a.in, p, row0, min(row0 + 16 * RT, rows) - 1, lo, hi);
     if (a.splits > 1) {
@@ -303,23 +315,25 @@ __global__ __launch_bounds__(kThreads, 2) void fp8_attention_kernel(Fp8Attention
 #pragma unroll
         for (int ct = 0; ct < S::kTiles; ++ct) o[rt][ct] = float4v{0.f, 0.f, 0.f, 0.f};
     }
-    int unit = -1000;   // exponent field of the V scale that o is in units of
+    int unit = 0, unit_most = 0;   // exponent field of the V scale that o is in units of, and the largest one (0: none yet, o = 0)
 
+    const uint32_t k_off = n * D + g * (D / 4), v_off = 4 * g * D + n * (D == 96 ? 4 : D / 16);
     const StreamMap map = a.in.c.map.of(p.stream);
     const int first = BY_ROWS ? lo : lo + 64 * wave, step = BY_ROWS ? 64 : 64 * kWaves;
     for (int t0 = first; t0 < hi; t0 += step) {
         const int64_t at = map.pos(t0);
         uint32_t kw[4][S::kKWords], vw[16][S::kVWords];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) load_k<D>(kw[j], a.in.c.k_codes + (at + 16 * j + n) * D, g);
+        for (int j = 0; j < 4; ++j) load_k<D>(kw[j], a.in.c.k_codes + at * D + 16 * j * D, k_off);
 #pragma unroll
-        for (int j = 0; j < 16; ++j) load_v<D>(vw[j], a.in.c.v_codes + (at + 16 * (j >> 2) + 4 * g + (j & 3)) * D, n);
+        for (int j = 0; j < 16; ++j) load_v<D>(vw[j], a.in.c.v_codes + at * D + (16 * (j >> 2) + (j & 3)) * D, v_off, n);
         const int64_t b0 = at >> a.in.c.log_block, b1 = (at + 32) >> a.in.c.log_block;
         const float ks[2] = {fabsf(a.in.c.k_scale[b0]), fabsf(a.in.c.k_scale[b1])};
         const float vs[2] = {a.in.c.v_scale[b0], a.in.c.v_scale[b1]};
         const bool edge = t0 + 64 > sees_all;
         const bool windowed = OPT && a.in.window > 0 && (int64_t)pos_most - t0 >= a.in.window;
 
+        if constexpr (kQueriesInLds) asm volatile("" : "+v"(q_lane));   // read again every time, not kept in registers
         float4v s[RT][4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
@@ -329,10 +343,11 @@ __global__ __launch_bounds__(kThreads, 2) void fp8_attention_kernel(Fp8Attention
             for (int q = 0; q < S::kSteps; ++q) {
                 const half8v k = k_operand<D>(kw[j], q);
 #pragma unroll
-                for (int rt = 0; rt < RT; ++rt) s[rt][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, qf[rt][q], s[rt][j], 0, 0, 0);
+                for (int rt = 0; rt < RT; ++rt) s[rt][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, query(rt, q), s[rt][j], 0, 0, 0);
             }
         }
-        float x[RT][16];
+        float x[RT][16], by[RT];
+        bool moved = false;
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
             float most = -INFINITY;
@@ -349,41 +364,35 @@ __global__ __launch_bounds__(kThreads, 2) void fp8_attention_kernel(Fp8Attention
             const float one[1] = {most};
             most = fold_rows(one, MaxF());
             // the reference moves when a score is far above it: numerators stay below 2^4 and need no other care
-            if (__any(most > m[rt] + 4.f)) {
-                const float to = fmaxf(most, m[rt]);
-                const float by = to == -INFINITY ? 1.f : exp2_(m[rt] - to);
-                m[rt] = to;
-                l[rt] *= by;
-#pragma unroll
-                for (int ct = 0; ct < S::kTiles; ++ct) o[rt][ct] *= by;
+            by[rt] = 1.f;
+            if (most > m[rt] + 4.f) {
+                by[rt] = exp2_(m[rt] - most);
+                m[rt] = most;
+                l[rt] *= by[rt];
             }
+            moved |= by[rt] != 1.f;
         }
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
             if (t0 + 32 * half >= hi) break;
-            // Units of o: the largest scale so far.  A block of a scale up to 2^6 smaller enters with numerators that are smaller by as much
-            // (their fp16 keeps 2^-24 of the reference); below that o comes down for it and goes up again.
+            // o is in units of a block's scale.  Blocks of a scale up to 2^6 smaller enter with numerators that are smaller by as much (their
+            // fp16 keeps 2^-24 of the reference); others bring o to their unit, up or down, but no further down from the largest scale so far
+            // than a binary32 has room for (2^80, beside 2^38 for the sum itself).
             const int field = field_of_scale(vs[half]);
-            int fold = 0, down = 0;
-            if (field > unit) {
+            int shift = 0;
+            if (field > unit || field < unit - 6) {
+                unit_most = max(unit_most, field);
+                const int to = max(field, unit_most - 80);
+                shift = unit - to;
+                unit = to;
+            }
+            const int fold = min(unit - field, 60);   // from 29 on fp16 leaves nothing of the numerators
+            if (half == 0 ? shift != 0 || __any(moved) : shift != 0) {
 #pragma unroll
-                for (int rt = 0; rt < RT; ++rt)
+                for (int rt = 0; rt < RT; ++rt) {
+                    const float f = ldexpf(half == 0 ? by[rt] : 1.f, shift);
 #pragma unroll
-                    for (int ct = 0; ct < S::kTiles; ++ct)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) o[rt][ct][i] = ldexpf(o[rt][ct][i], unit - field);
-                unit = field;
-            } else {
-                fold = unit - field;
-                if (fold > 6) {
-                    down = min(fold, 60);
-                    fold -= down;
-#pragma unroll
-                    for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-                        for (int ct = 0; ct < S::kTiles; ++ct)
-#pragma unroll
-                            for (int i = 0; i < 4; ++i) o[rt][ct][i] = ldexpf(o[rt][ct][i], down);
+                    for (int ct = 0; ct < S::kTiles; ++ct) o[rt][ct] *= f;
                 }
             }
             half8v pf[RT];
@@ -473,14 +482,6 @@ __global__ __launch_bounds__(kThreads, 2) void fp8_attention_kernel(Fp8Attention
 #pragma unroll
                     for (int rt = 0; rt < RT; ++rt) o[rt][ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f, pf[rt], o[rt][ct], 0, 0, 0);
                 }
-            }
-            if (down) {
-#pragma unroll
-                for (int rt = 0; rt < RT; ++rt)
-#pragma unroll
-                    for (int ct = 0; ct < S::kTiles; ++ct)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) o[rt][ct][i] = ldexpf(o[rt][ct][i], -down);
             }
         }
     }
@@ -635,6 +636,7 @@ __global__ __launch_bounds__(kThreads, 2) void fp8_weights_kernel(Fp8WeightsArgs
     if (from >= to) return;
     const int32_t *pos = OPT && (a.in.slopes || a.in.window > 0) ? a.in.c.pos + (int64_t)p.stream * a.in.c.t_capacity : nullptr;
     float *weight = a.in.c.weight + (int64_t)p.stream * a.in.c.t_capacity;
+    const uint32_t k_off = n * D + g * (D / 4);
     const StreamMap map = a.in.c.map.of(p.stream);
     for (int first = 0; first < max(rows, 1); first += 16 * kWeightTiles) {
         const int tiles = (min(rows - first, 16 * kWeightTiles) + 15) / 16;
@@ -668,7 +670,7 @@ __global__ __launch_bounds__(kThreads, 2) void fp8_weights_kernel(Fp8WeightsArgs
                 const int64_t at = map.pos(t0);
                 uint32_t kw[4][S::kKWords];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) load_k<D>(kw[j], a.in.c.k_codes + (at + 16 * j + n) * D, g);
+                for (int j = 0; j < 4; ++j) load_k<D>(kw[j], a.in.c.k_codes + at * D + 16 * j * D, k_off);
                 const float ks[2] = {fabsf(a.in.c.k_scale[at >> a.in.c.log_block]), fabsf(a.in.c.k_scale[(at + 32) >> a.in.c.log_block])};
                 half8v kf[4][S::kSteps];
 #pragma unroll
