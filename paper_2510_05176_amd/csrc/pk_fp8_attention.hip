@@ -18,27 +18,38 @@ constexpr int kWaves = 4, kThreads = 64 * kWaves;
 
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// tanh in binary32.  Below 0.55 the odd Taylor series (the first term left out is 4e-8 of the result at 0.55), above it
-// 1 - 2 / (e^{2x} + 1), whose rounding is no longer magnified there.
-__device__ __forceinline__ float tanh_(float x)
+// tanh in binary32, of N values.  Below 0.55 the odd Taylor series (the first term left out is 4e-8 of the result at 0.55), above it
+// 1 - 2 / (e^{2x} + 1), whose rounding is no longer magnified there; a wave without such a value does not compute it.
+template <int N>
+__device__ __forceinline__ void tanh_all(float (&x)[N])
 {
-    const float a = fabsf(x), y = x * x;
-    // coefficients of x^3, x^5, ... of the series: 2^(2k) (2^(2k) - 1) B_2k / (2k)!
-    float s = -929569.f / 638512875.f;
-    s = fmaf(s, y, 21844.f / 6081075.f);
-    s = fmaf(s, y, -1382.f / 155925.f);
-    s = fmaf(s, y, 62.f / 2835.f);
-    s = fmaf(s, y, -17.f / 315.f);
-    s = fmaf(s, y, 2.f / 15.f);
-    s = fmaf(s, y, -1.f / 3.f);
-    float t = fmaf(s * y, x, x);
-    if (__any(!(a < 0.55f))) {
-        const float e = exp2_(fminf(a, 16.f) * (2.f * kLog2e));
-        const float big = 1.f - 2.f * __builtin_amdgcn_rcpf(e + 1.f);
-        t = a < 0.55f ? t : (a != a ? a : copysignf(big, x));
+    float most = 0.f;
+#pragma unroll
+    for (int i = 0; i < N; ++i) most = fmaxf(most, fabsf(x[i]));   // (a NaN does not count and comes out of the series as one)
+    const bool far = __any(most >= 0.55f);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const float y = x[i] * x[i];
+        // coefficients of x^3, x^5, ...: 2^(2k) (2^(2k) - 1) B_2k / (2k)!
+        float s = -929569.f / 638512875.f;
+        s = fmaf(s, y, 21844.f / 6081075.f);
+        s = fmaf(s, y, -1382.f / 155925.f);
+        s = fmaf(s, y, 62.f / 2835.f);
+        s = fmaf(s, y, -17.f / 315.f);
+        s = fmaf(s, y, 2.f / 15.f);
+        s = fmaf(s, y, -1.f / 3.f);
+        float t = fmaf(s * y, x[i], x[i]);
+        if (far) {
+            const float a = fabsf(x[i]), e = exp2_(fminf(a, 16.f) * (2.f * kLog2e));
+            const float big = copysignf(1.f - 2.f * __builtin_amdgcn_rcpf(e + 1.f), x[i]);
+            t = a >= 0.55f ? big : t;
+        }
+        x[i] = t;
     }
-    return t;
 }
+
+// The same value for all lanes, through the scalar path; nothing writes it while the kernel runs
+__device__ __forceinline__ float scalar_load(const float *p) { return *(const __attribute__((address_space(4))) float *)(uintptr_t)p; }
 
 template <int D>
 struct Shape {
@@ -130,6 +141,8 @@ __device__ __forceinline__ void load_query(half8v (&qf)[D / 32], float &factor, 
 #pragma unroll
         for (int s = 0; s < D / 32; ++s) raw[s] = p[s];
     }
+    // the products take the scale's sign, so that what multiplies them later is positive
+    const bool negative = a.scale < 0.f;
     float mul = 1.f;
     factor = 1.f;
     if (a.bf16) {
@@ -148,7 +161,10 @@ __device__ __forceinline__ void load_query(half8v (&qf)[D / 32], float &factor, 
         // the largest element to [2^14, 2^15), within what a binary32 holds on both sides
         const int shift = min(max((int)(all >> 23) - 127 - 14, -126), 126);
         factor = __builtin_bit_cast(float, (uint32_t)(127 + shift) << 23);
-        mul = __builtin_bit_cast(float, (uint32_t)(127 - shift) << 23);
+        mul = __builtin_bit_cast(float, ((uint32_t)(127 - shift) << 23) | (negative ? 0x80000000u : 0u));
+    } else if (negative) {
+#pragma unroll
+        for (int s = 0; s < D / 32; ++s) raw[s] = make_uint4(raw[s].x ^ 0x80008000u, raw[s].y ^ 0x80008000u, raw[s].z ^ 0x80008000u, raw[s].w ^ 0x80008000u);
     }
 #pragma unroll
     for (int s = 0; s < D / 32; ++s) qf[s] = query8(raw[s], a.bf16, mul);
@@ -169,41 +185,49 @@ __device__ __forceinline__ half8v k_operand(const uint32_t (&k)[D / 16], int s)
     return half8v{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
 
-// Scores of 4 tokens of a row, t0 + 0 .. 3, in place of their products; masked ones at -inf.  `unit` is what multiplies the product, and
-// what a score is multiplied with: the score is cap * tanh(unit * x / cap) - slope * distance, or unit * x - ....
+// From the products of 16 tokens of a row (4 each of the tiles at t, t + 16, t + 32, t + 48) to its scores times `post`: score = x * f of the
+// token's half.  Without options x stays the product and f takes scale and units in, so that the factor costs nothing where the caller
+// subtracts something anyway; f is never 0, so that a masked x = -inf stays one.
 template <bool OPT>
-__device__ __forceinline__ void finish_scores(float (&x)[4], float k_scale, const Fp8Queries &a, float post, const Row &row, int t0, const int32_t *pos,
-                                              bool edge, bool windowed)
+__device__ __forceinline__ void to_scores(float (&x)[16], float (&f)[2], const float (&ks)[2], const Fp8Queries &a, float post, const Row &row, int t,
+                                          const int32_t *pos, bool edge, bool windowed)
 {
-    const float f = k_scale * row.factor * a.scale;
+    const float c = row.factor * fabsf(a.scale);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) f[h] = ks[h] * c;
     if constexpr (OPT) {
         if (a.cap > 0.f) {
             const float inv = 1.f / a.cap;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = tanh_(x[i] * f * inv) * a.cap;
+            for (int i = 0; i < 16; ++i) x[i] *= f[i >> 3] * inv;
+            tanh_all(x);
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[i] *= a.cap * post;
         } else {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] *= f;
+            for (int i = 0; i < 16; ++i) x[i] *= f[i >> 3] * post;
         }
         if (pos) {
-            const int4 p = *reinterpret_cast<const int4 *>(pos + t0);
-            const int back[4] = {row.pos - p.x, row.pos - p.y, row.pos - p.z, row.pos - p.w};
+            const float slope = row.slope * post;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                x[i] = fmaf(-row.slope, (float)back[i], x[i]);
-                if (windowed && back[i] >= a.window) x[i] = -INFINITY;
+            for (int j = 0; j < 4; ++j) {
+                const int4 p = *reinterpret_cast<const int4 *>(pos + t + 16 * j);
+                const int back[4] = {row.pos - p.x, row.pos - p.y, row.pos - p.z, row.pos - p.w};
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    x[4 * j + i] = fmaf(-slope, (float)back[i], x[4 * j + i]);
+                    if (windowed && back[i] >= a.window) x[4 * j + i] = -INFINITY;
+                }
             }
         }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] *= post;
+        f[0] = f[1] = 1.f;
     } else {
-        const float fp = f * post;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] *= fp;
+        for (int h = 0; h < 2; ++h) f[h] = fmaxf(f[h] * post, 0x1p-126f);
     }
     if (edge) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = t0 + i <= row.last ? x[i] : -INFINITY;
+        for (int i = 0; i < 16; ++i) x[i] = t + 16 * (i >> 2) + (i & 3) <= row.last ? x[i] : -INFINITY;
     }
 }
 
@@ -328,8 +352,8 @@ __global__ __launch_bounds__(kThreads, 2) void fp8_attention_kernel(Fp8Attention
 #pragma unroll
         for (int j = 0; j < 16; ++j) load_v<D>(vw[j], a.in.c.v_codes + at * D + (16 * (j >> 2) + (j & 3)) * D, v_off, n);
         const int64_t b0 = at >> a.in.c.log_block, b1 = (at + 32) >> a.in.c.log_block;
-        const float ks[2] = {fabsf(a.in.c.k_scale[b0]), fabsf(a.in.c.k_scale[b1])};
-        const float vs[2] = {a.in.c.v_scale[b0], a.in.c.v_scale[b1]};
+        const float ks[2] = {fabsf(scalar_load(a.in.c.k_scale + b0)), fabsf(scalar_load(a.in.c.k_scale + b1))};
+        const float vs[2] = {scalar_load(a.in.c.v_scale + b0), scalar_load(a.in.c.v_scale + b1)};
         const bool edge = t0 + 64 > sees_all;
         const bool windowed = OPT && a.in.window > 0 && (int64_t)pos_most - t0 >= a.in.window;
 
@@ -346,20 +370,20 @@ __global__ __launch_bounds__(kThreads, 2) void fp8_attention_kernel(Fp8Attention
                 for (int rt = 0; rt < RT; ++rt) s[rt][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, query(rt, q), s[rt][j], 0, 0, 0);
             }
         }
-        float x[RT][16], by[RT];
+        float x[RT][16], f[RT][2], by[RT];
         bool moved = false;
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) x[rt][i] = s[rt][i >> 2][i & 3];
+            to_scores<OPT>(x[rt], f[rt], ks, a.in, kLog2e, row[rt], t0 + 4 * g, pos, edge, windowed);
             float most = -INFINITY;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                float y[4] = {s[rt][j][0], s[rt][j][1], s[rt][j][2], s[rt][j][3]};
-                finish_scores<OPT>(y, ks[j >> 1], a.in, kLog2e, row[rt], t0 + 16 * j + 4 * g, pos, edge, windowed);
+            for (int h = 0; h < 2; ++h) {
+                float top = x[rt][8 * h];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    x[rt][4 * j + i] = y[i];
-                    most = fmaxf(most, y[i]);
-                }
+                for (int i = 1; i < 8; ++i) top = fmaxf(top, x[rt][8 * h + i]);
+                most = fmaxf(most, top * f[rt][h]);
             }
             const float one[1] = {most};
             most = fold_rows(one, MaxF());
@@ -388,6 +412,7 @@ __global__ __launch_bounds__(kThreads, 2) void fp8_attention_kernel(Fp8Attention
             }
             const int fold = min(unit - field, 60);   // from 29 on fp16 leaves nothing of the numerators
             if (half == 0 ? shift != 0 || __any(moved) : shift != 0) {
+                asm volatile("");   // a branch: most blocks leave o as it is
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) {
                     const float f = ldexpf(half == 0 ? by[rt] : 1.f, shift);
@@ -402,7 +427,7 @@ __global__ __launch_bounds__(kThreads, 2) void fp8_attention_kernel(Fp8Attention
                 float sum = 0.f;
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const float e = exp2_(x[rt][8 * half + i] - ref);
+                    const float e = exp2_(fmaf(x[rt][8 * half + i], f[rt][half], -ref));
                     sum += e;
                     pf[rt][i] = (_Float16)e;
                 }
@@ -671,7 +696,7 @@ __global__ __launch_bounds__(kThreads, 2) void fp8_weights_kernel(Fp8WeightsArgs
                 uint32_t kw[4][S::kKWords];
 #pragma unroll
                 for (int j = 0; j < 4; ++j) load_k<D>(kw[j], a.in.c.k_codes + at * D + 16 * j * D, k_off);
-                const float ks[2] = {fabsf(a.in.c.k_scale[at >> a.in.c.log_block]), fabsf(a.in.c.k_scale[(at + 32) >> a.in.c.log_block])};
+                const float ks[2] = {fabsf(scalar_load(a.in.c.k_scale + (at >> a.in.c.log_block))), fabsf(scalar_load(a.in.c.k_scale + ((at + 32) >> a.in.c.log_block)))};
                 half8v kf[4][S::kSteps];
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
@@ -691,13 +716,12 @@ __global__ __launch_bounds__(kThreads, 2) void fp8_weights_kernel(Fp8WeightsArgs
                     }
                     const bool edge = __any(t0 + 63 > row.last);
                     const bool windowed = OPT && a.in.window > 0;
+                    float y[16], f[2];
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        float y[4] = {x[j][0], x[j][1], x[j][2], x[j][3]};
-                        finish_scores<OPT>(y, ks[j >> 1], a.in, 1.f, row, t0 + 16 * j + 4 * g, pos, edge, windowed);
+                    for (int i = 0; i < 16; ++i) y[i] = x[i >> 2][i & 3];
+                    to_scores<OPT>(y, f, ks, a.in, 1.f, row, t0 + 4 * g, pos, edge, windowed);
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) sum[4 * j + i] += exp2_((y[i] - lse) * kLog2e);
-                    }
+                    for (int i = 0; i < 16; ++i) sum[i] += exp2_(fmaf(y[i], f[i >> 3], -lse) * kLog2e);
                 }
             }
 #pragma unroll
@@ -725,6 +749,9 @@ __global__ __launch_bounds__(kThreads, 2) void fp8_weights_kernel(Fp8WeightsArgs
     }
 }
 
+#ifndef TARGET
+#define TARGET 512
+#endif
 // How many rows a workgroup of the attention takes, and how.
 struct Rows {
     int tiles;      // per wave (RT)
@@ -784,7 +811,7 @@ int fp8_attention_splits(int64_t n_streams, int64_t r, int64_t n_query, int d, i
 {
     const Rows x = rows_of(r * n_query, d);
     const int64_t groups = n_streams * ((r * n_query + x.per_group - 1) / x.per_group);
-    const int64_t want = (1024 + groups - 1) / groups, most = (bound + 255) / 256;
+    const int64_t want = (TARGET + groups - 1) / groups, most = (bound + 255) / 256;
     const int64_t k = want < most ? want : most;
     return (int)(k < 1 ? 1 : k > 256 ? 256 : k);
 }
