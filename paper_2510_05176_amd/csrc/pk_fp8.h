@@ -47,12 +47,14 @@ struct Fp8AttentionArgs {
     void *out;
     pk_strides os;
     float *lse;               // or null
-    float *part_o, *part_ml;  // splits > 1: [N][splits][rows][d] normalised results, [N][splits][rows][2] reference and sum
-    int32_t splits;
+    float *part_o, *part_ml;  // parts > 0: results of the slots, [slots][kv heads][rows][d] normalised, [slots][kv heads][rows][2] reference and sum
+    int32_t parts;            // work items that the keys of a KV head and a group of rows are dealt out in, 0: one per sequence
+    int32_t groups;           // of rows (set by the launch)
 };
-// How the keys of a call are split over workgroups, from host values alone.
-int fp8_attention_splits(int64_t n_streams, int64_t r, int64_t n_query, int d, int64_t bound);
-hipError_t launch_fp8_attention(const Fp8AttentionArgs &a, hipStream_t s);
+// Both from host values alone.
+int64_t fp8_attention_parts(int64_t n_seq, int64_t n_kv_heads, int64_t r, int64_t n_query, int d, int64_t bound);
+inline int64_t fp8_attention_slots(int64_t n_seq, int64_t parts) { return n_seq + parts; }
+hipError_t launch_fp8_attention(Fp8AttentionArgs &a, hipStream_t s);
 
 struct Fp8WeightsArgs {
     Fp8Queries in;

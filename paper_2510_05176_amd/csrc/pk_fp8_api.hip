@@ -88,19 +88,19 @@ uint64_t kept_bytes(const pk_fp8_config *c, int64_t budget)
 }
 
 struct AttentionPlan {
-    int splits;
+    int64_t parts;
     uint64_t o_bytes, ml_bytes;
 };
 AttentionPlan plan_attention(const pk_fp8_config *c, int64_t n_query, int64_t bound)
 {
-    const int64_t N = (int64_t)c->n_seq * c->n_kv_heads, r = c->n_q_heads / c->n_kv_heads;
-    AttentionPlan p = {1, 0, 0};
+    const int64_t r = c->n_q_heads / c->n_kv_heads;
+    AttentionPlan p = {0, 0, 0};
     if (n_query < 1) return p;
-    p.splits = fp8_attention_splits(N, r, n_query, c->head_dim, bound);
-    if (p.splits > 1) {
-        const uint64_t slots = (uint64_t)N * p.splits * r * n_query;
-        p.o_bytes = round_up(slots * c->head_dim * 4, 256);
-        p.ml_bytes = round_up(slots * 2 * 4, 256);
+    p.parts = fp8_attention_parts(c->n_seq, c->n_kv_heads, r, n_query, c->head_dim, bound);
+    if (p.parts > 0) {
+        const uint64_t results = (uint64_t)fp8_attention_slots(c->n_seq, p.parts) * c->n_kv_heads * r * n_query;
+        p.o_bytes = round_up(results * c->head_dim * 4, 256);
+        p.ml_bytes = round_up(results * 2 * 4, 256);
     }
     return p;
 }
@@ -215,15 +215,16 @@ pk_status pk_fp8_attention(const pk_fp8_config *cfg, const pk_fp8_cache *cache, 
     if (!aligned16(out) || !aligned16(lse) || !aligned16(workspace)) return PK_ERR_ALIGNMENT;
     if (n_query == 0) return PK_OK;
     const AttentionPlan p = plan_attention(cfg, n_query, bound);
-    const int64_t N = (int64_t)cfg->n_seq * cfg->n_kv_heads, rows = (int64_t)a.in.r * n_query;
-    // groups of at least 16 rows, and the merge's threads
-    if (N * ((rows + 15) / 16) * p.splits > kMostGroups || (p.splits > 1 && N * rows * (cfg->head_dim / 2) / 256 + 1 > kMostGroups))
+    // groups of at least 16 rows, and the merge's of at least 2
+    const int64_t rows = (int64_t)a.in.r * n_query, slots = fp8_attention_slots(cfg->n_seq, p.parts) * cfg->n_kv_heads;
+    if (slots * ((rows + 15) / 16) > kMostGroups || (p.parts > 0 && (int64_t)cfg->n_seq * cfg->n_kv_heads * ((rows + 1) / 2) > kMostGroups))
         return PK_ERR_UNSUPPORTED;
-    if (p.splits > 1 && (!workspace || workspace_bytes < p.o_bytes + p.ml_bytes)) return PK_ERR_WORKSPACE;
+    if (p.parts > 0 && (!workspace || workspace_bytes < p.o_bytes + p.ml_bytes)) return PK_ERR_WORKSPACE;
     a.out = out;
     a.os = *os;
     a.lse = lse;
-    a.splits = p.splits;
+    a.parts = (int32_t)p.parts;
+    a.groups = 0;
     a.part_o = static_cast<float *>(workspace);
     a.part_ml = reinterpret_cast<float *>(static_cast<char *>(workspace) + p.o_bytes);
     return launch_fp8_attention(a, static_cast<hipStream_t>(stream)) == hipSuccess ? PK_OK : PK_ERR_DEVICE;

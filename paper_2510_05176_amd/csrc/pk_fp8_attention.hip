@@ -270,6 +270,41 @@ __device__ __forceinline__ void key_range(const Fp8Queries &a, const Place &p, i
     if (a.window > 0) lo = (int)min(max((int64_t)p.len - p.count + i0 + 1 - a.window, (int64_t)0), (int64_t)hi) & ~63;
 }
 
+// How the keys of a call are dealt out: the units of 64 visible tokens of all sequences (one at least of each), laid end to end, in
+// `parts` runs of equal length (at least kLeastUnits), whatever the lengths of the sequences.  A run is one workgroup's; where it crosses
+// from one sequence into the next it goes on with that.  The piece of sequence b in run i has slot i + b: they grow from piece to
+// piece, so no two are alike and n_seq + parts are enough.  parts == 0: a workgroup per sequence.
+constexpr int kMostSeqs = 256, kLeastUnits = 4;
+__device__ __forceinline__ int first_visible(const Fp8Queries &a, int len, int count)   // a multiple of 64
+{
+    return a.window > 0 ? (int)min(max((int64_t)len - count + 1 - a.window, (int64_t)0), (int64_t)len) & ~63 : 0;
+}
+// Ends of the sequences' units, lane's sequences 64 i + lane; returns all of them.
+__device__ __forceinline__ int ends_of(const Fp8Queries &a, int (&end)[kMostSeqs / 64])
+{
+    const int lane = threadIdx.x & 63;
+    int before = 0;
+#pragma unroll
+    for (int i = 0; i < kMostSeqs / 64; ++i) {
+        end[i] = 0;
+        if (64 * i >= a.n_seq) continue;
+        const int seq = 64 * i + lane;
+        int units = 0;
+        if (seq < a.n_seq) {
+            const int len = fp8_state(a.states, seq, a.c.t_capacity).x, count = fp8_count(a.counts, seq, a.n_query);
+            units = count > 0 ? max((len - first_visible(a, len, count) + 63) >> 6, 1) : 1;
+        }
+        for (int o = 1; o < 64; o <<= 1) {
+            const int v = __shfl_up(units, o);
+            if (lane >= o) units += v;
+        }
+        end[i] = units + before;
+        before = __shfl(end[i], 63);
+    }
+    return before;
+}
+__device__ __forceinline__ int run_length(int all, int parts) { return max((all + parts - 1) / parts, kLeastUnits); }
+
 template <int D>
 __device__ __forceinline__ void store_row(const Fp8AttentionArgs &a, const Place &p, int row, int c, const float *x, int n)
 {
@@ -292,11 +327,33 @@ __global__ __launch_bounds__(kThreads, 2) void fp8_attention_kernel(Fp8Attention
     using S = Shape<D>;
     const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int N = a.in.n_seq * a.in.c.n_kv_heads;
-    const int rows = a.in.r * a.in.n_query;
-    const int rest = blockIdx.x / N;
-    const Place p = place_of<true>(a.in, blockIdx.x - rest * N);
-    const int split = rest % a.splits, group = rest / a.splits;
+    const int rows = a.in.r * a.in.n_query, hkv = a.in.c.n_kv_heads;
+    // heads next to each other: with eight of them every XCD has one head's keys in its cache
+    const int kvh = blockIdx.x % hkv, rest = blockIdx.x / hkv;
+    const int group = rest % a.groups, run = rest / a.groups;
+    __shared__ int sm_end[kMostSeqs];
+    int seq = run, seq_from = 0, seq_to = 0, at_unit = 0, stop = 0, per = 0;
+    if (a.parts > 0) {
+        int end[kMostSeqs / 64];
+        const int all = __builtin_amdgcn_readfirstlane(ends_of(a.in, end));
+        per = run_length(all, a.parts);
+        at_unit = run * per;
+        stop = min(at_unit + per, all);
+        if (at_unit >= stop) return;
+#pragma unroll
+        for (int i = kMostSeqs / 64 - 1; i >= 0; --i) {
+            if (64 * i + lane < a.in.n_seq && wave == 0) sm_end[64 * i + lane] = end[i];
+            const uint64_t behind = __ballot(64 * i + lane < a.in.n_seq && end[i] > at_unit);
+            if (behind) seq = 64 * i + __ffsll((unsigned long long)behind) - 1;
+        }
+        __syncthreads();
+        seq_from = seq > 0 ? __builtin_amdgcn_readfirstlane(sm_end[seq - 1]) : 0;
+    }
+    for (;; seq_from = seq_to, ++seq) {   // the pieces of the run
+    if (a.parts > 0) seq_to = __builtin_amdgcn_readfirstlane(sm_end[seq]);
+    const bool whole = a.parts == 0 || (at_unit <= seq_from && seq_to <= stop);   // the sequence is this piece
+    const Place p = place_of<true>(a.in, seq * hkv + kvh);
+    const int64_t part0 = ((int64_t)(run + seq) * hkv + kvh) * rows;   // where partial results of the rows go
     const int row0 = BY_ROWS ? (group * kWaves + wave) * 16 * RT : group * 16 * RT;
 
     // queries: in registers for one tile of up to 128 channels, else in LDS (the registers then hold two tiles' results or 256 channels' of one)
@@ -320,10 +377,10 @@ __global__ __launch_bounds__(kThreads, 2) void fp8_attention_kernel(Fp8Attention
     };
     int lo, hi;
     key_range(a.in, p, row0, min(row0 + 16 * RT, rows) - 1, lo, hi);
-    if (a.splits > 1) {
-        const int per = ((hi - lo + a.splits - 1) / a.splits + 63) & ~63;
-        lo = (int)min((int64_t)lo + (int64_t)split * per, (int64_t)hi);
-        hi = min(lo + per, hi);
+    if (!whole) {
+        const int64_t from = first_visible(a.in, p.len, p.count);
+        lo = (int)max(from + (int64_t)(max(at_unit, seq_from) - seq_from) * 64, (int64_t)lo);
+        hi = (int)min(from + (int64_t)(min(stop, seq_to) - seq_from) * 64, (int64_t)hi);
     }
     // the first token that some live row does not see, and the largest position of a live row
     const int sees_all = p.len - p.count + min(row0 / a.in.r, max(p.count - 1, 0)) + 1;
@@ -527,10 +584,10 @@ __global__ __launch_bounds__(kThreads, 2) void fp8_attention_kernel(Fp8Attention
         for (int rt = 0; rt < RT; ++rt) {
             const int at = row0 + 16 * rt + n;
             if (at >= p.count * a.in.r) continue;
-            if (a.splits == 1) {
+            if (whole) {
                 if (g == 0) store_lse(a, p, at, m[rt], l[rt]);
             } else if (g == 0) {
-                float *ml = a.part_ml + (((int64_t)p.stream * a.splits + split) * rows + at) * 2;
+                float *ml = a.part_ml + (part0 + at) * 2;
                 ml[0] = m[rt];
                 ml[1] = l[rt];
             }
@@ -541,11 +598,11 @@ __global__ __launch_bounds__(kThreads, 2) void fp8_attention_kernel(Fp8Attention
                 float y[S::kTiles];
 #pragma unroll
                 for (int ct = 0; ct < S::kTiles; ++ct) y[ct] = o[rt][ct][i];
-                if (a.splits == 1) {
+                if (whole) {
                     store_row<D>(a, p, at, channel_of<D>(4 * g + i, 0), y, kMain);
                     if constexpr (D == 96) store_row<D>(a, p, at, channel_of<D>(4 * g + i, 4), y + 4, 2);
                 } else {
-                    float *to = a.part_o + (((int64_t)p.stream * a.splits + split) * rows + at) * D;
+                    float *to = a.part_o + (part0 + at) * D;
 #pragma unroll
                     for (int ct = 0; ct < S::kTiles; ++ct) to[channel_of<D>(4 * g + i, ct)] = y[ct];
                 }
@@ -589,11 +646,11 @@ __global__ __launch_bounds__(kThreads, 2) void fp8_attention_kernel(Fp8Attention
                     }
                     const float inv = sum == 0.f ? 0.f : 1.f / sum;
                     for (int i = 0; i < 4; ++i) y[i] *= inv;
-                    if (a.splits == 1) {
+                    if (whole) {
                         store_row<D>(a, p, at, c, y, 4);
                         if (c == 0) store_lse(a, p, at, top, sum);
                     } else {
-                        const int64_t slot = ((int64_t)p.stream * a.splits + split) * rows + at;
+                        const int64_t slot = part0 + at;
                         *reinterpret_cast<float4 *>(a.part_o + slot * D + c) = make_float4(y[0], y[1], y[2], y[3]);
                         if (c == 0) {
                             a.part_ml[2 * slot] = top;
@@ -603,26 +660,40 @@ __global__ __launch_bounds__(kThreads, 2) void fp8_attention_kernel(Fp8Attention
                 }
             }
     }
+    if (a.parts == 0 || seq_to >= stop) break;
+    if constexpr (!BY_ROWS) __syncthreads();   // before the next piece's results take these places
+    }
 }
 
-// The splits of a row together: sum_s l_s 2^(m_s - m) o_s / sum_s l_s 2^(m_s - m).  A thread takes two channels of a row.
+// The pieces of a row together: sum_s l_s 2^(m_s - m) o_s / sum_s l_s 2^(m_s - m).  A workgroup takes some rows of a (sequence, KV head)
+// that was split, a thread two channels of a row.
 template <int D>
 __global__ __launch_bounds__(256) void fp8_merge_kernel(Fp8AttentionArgs a)
 {
-    const int rows = a.in.r * a.in.n_query;
-    const int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x, all = (int64_t)a.in.n_seq * a.in.c.n_kv_heads * rows * (D / 2);
-    if (e >= all) return;
-    const int c = (int)(e % (D / 2)) * 2;
-    const int64_t flat = e / (D / 2);
-    const int row = (int)(flat % rows);
-    const Place p = place_of<false>(a.in, (int)(flat / rows));
-    if (row >= p.count * a.in.r) return;
+    constexpr int kRows = 256 / (D / 2);
+    const int rows = a.in.r * a.in.n_query, hkv = a.in.c.n_kv_heads, groups = (rows + kRows - 1) / kRows;
+    const int kvh = blockIdx.x % hkv, rest = blockIdx.x / hkv, row = rest % groups * kRows + (int)threadIdx.x / (D / 2);
+    const int seq = rest / groups;
+    int end[kMostSeqs / 64], from = 0, to = 0;
+    const int all = __builtin_amdgcn_readfirstlane(ends_of(a.in, end)), per = run_length(all, a.parts);
+#pragma unroll
+    for (int i = 0; i < kMostSeqs / 64; ++i) {
+        const int before = __shfl(end[i], (seq - 1) & 63), here = __shfl(end[i], seq & 63);
+        if (seq > 0 && (seq - 1) / 64 == i) from = before;
+        if (seq / 64 == i) to = here;
+    }
+    const int first_run = from / per, pieces = (to - 1) / per - first_run + 1;
+    if (pieces == 1) return;   // written already
+    const Place p = place_of<true>(a.in, seq * hkv + kvh);
+    if ((int)threadIdx.x >= kRows * (D / 2) || row >= p.count * a.in.r) return;
+    const int c = (int)threadIdx.x % (D / 2) * 2;
+    const int64_t first = ((int64_t)(first_run + seq) * hkv + kvh) * rows + row, step = (int64_t)hkv * rows;
     float top = -INFINITY;
-    for (int s = 0; s < a.splits; ++s) top = fmaxf(top, a.part_ml[2 * (((int64_t)p.stream * a.splits + s) * rows + row)]);
+    for (int s = 0; s < pieces; ++s) top = fmaxf(top, a.part_ml[2 * (first + s * step)]);
     const float ref = top == -INFINITY ? 0.f : top;
     float sum = 0.f, y[2] = {0.f, 0.f};
-    for (int s = 0; s < a.splits; ++s) {
-        const int64_t slot = ((int64_t)p.stream * a.splits + s) * rows + row;
+    for (int s = 0; s < pieces; ++s) {
+        const int64_t slot = first + s * step;
         const float part = a.part_ml[2 * slot + 1] * exp2_(a.part_ml[2 * slot] - ref);
         sum += part;
         const float2 o = *reinterpret_cast<const float2 *>(a.part_o + slot * D + c);
@@ -749,8 +820,9 @@ __global__ __launch_bounds__(kThreads, 2) void fp8_weights_kernel(Fp8WeightsArgs
     }
 }
 
-#ifndef TARGET
-#define TARGET 512
+#ifndef R1
+#define R1 512
+#define R2 512
 #endif
 // How many rows a workgroup of the attention takes, and how.
 struct Rows {
@@ -775,11 +847,12 @@ void launch_rt(const Fp8AttentionArgs &a, uint32_t grid, bool opt, hipStream_t s
 }
 
 template <int D>
-hipError_t launch_d(const Fp8AttentionArgs &a, hipStream_t s)
+hipError_t launch_d(Fp8AttentionArgs &a, hipStream_t s)
 {
-    const int64_t rows = (int64_t)a.in.r * a.in.n_query, N = (int64_t)a.in.n_seq * a.in.c.n_kv_heads;
+    const int64_t rows = (int64_t)a.in.r * a.in.n_query;
     const Rows x = rows_of(rows, D);
-    const uint32_t grid = (uint32_t)(N * ((rows + x.per_group - 1) / x.per_group) * a.splits);
+    a.groups = (int)((rows + x.per_group - 1) / x.per_group);
+    const uint32_t grid = (uint32_t)((a.parts > 0 ? a.parts : a.in.n_seq) * a.in.c.n_kv_heads * a.groups);
     const bool opt = a.in.cap > 0.f || a.in.slopes || a.in.window > 0;
     if (x.tiles == 1) {
         if (x.by_rows) launch_rt<D, 1, true>(a, grid, opt, s);
@@ -788,9 +861,10 @@ hipError_t launch_d(const Fp8AttentionArgs &a, hipStream_t s)
         if (x.by_rows) launch_rt<D, 2, true>(a, grid, opt, s);
         else launch_rt<D, 2, false>(a, grid, opt, s);
     }
-    hipError_t e = hipGetLastError();
-    if (e != hipSuccess || a.splits == 1) return e;
-    fp8_merge_kernel<D><<<(uint32_t)((N * rows * (D / 2) + 255) / 256), 256, 0, s>>>(a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess || a.parts == 0) return e;
+    constexpr int kRows = 256 / (D / 2);
+    fp8_merge_kernel<D><<<(uint32_t)((int64_t)a.in.n_seq * a.in.c.n_kv_heads * ((rows + kRows - 1) / kRows)), 256, 0, s>>>(a);
     return hipGetLastError();
 }
 
@@ -807,16 +881,20 @@ hipError_t launch_weights_d(const Fp8WeightsArgs &a, hipStream_t s)
 
 }  // namespace
 
-int fp8_attention_splits(int64_t n_streams, int64_t r, int64_t n_query, int d, int64_t bound)
+int64_t fp8_attention_parts(int64_t n_seq, int64_t n_kv_heads, int64_t r, int64_t n_query, int d, int64_t bound)
 {
     const Rows x = rows_of(r * n_query, d);
-    const int64_t groups = n_streams * ((r * n_query + x.per_group - 1) / x.per_group);
-    const int64_t want = (TARGET + groups - 1) / groups, most = (bound + 255) / 256;
-    const int64_t k = want < most ? want : most;
-    return (int)(k < 1 ? 1 : k > 256 ? 256 : k);
+    const int64_t across = n_kv_heads * ((r * n_query + x.per_group - 1) / x.per_group);   // workgroups per run
+    const int64_t resident = x.tiles == 1 && d < 256 ? R1 : R2;
+    int64_t parts = resident / across;
+    if (parts < 1) parts = 1;
+    if (n_seq > kMostSeqs || n_seq >= 4 * parts) return 0;
+    const int64_t most = n_seq * ((bound + 64 * kLeastUnits - 1) / (64 * kLeastUnits));
+    if (parts > most) parts = most;
+    return parts <= 1 && n_seq == 1 ? 0 : parts;
 }
 
-hipError_t launch_fp8_attention(const Fp8AttentionArgs &a, hipStream_t s)
+hipError_t launch_fp8_attention(Fp8AttentionArgs &a, hipStream_t s)
 {
     return a.in.d == 64 ? launch_d<64>(a, s) : a.in.d == 96 ? launch_d<96>(a, s) : a.in.d == 128 ? launch_d<128>(a, s) : launch_d<256>(a, s);
 }

@@ -549,11 +549,16 @@ class Fp8Cache:
         return self.states[:, 0]
 
 
+# The current stream's handle without the object around it (torch.cuda.current_stream() took 3.2 of a short call's 9 us).
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
+
+
 def _fp8_stream(cache: Fp8Cache):
     # the launches go to the current device's stream, so the memory has to be that device's
-    if cache.device.index != torch.cuda.current_device():
-        raise ValueError(f"the cache is on {cache.device}, the current device is cuda:{torch.cuda.current_device()}")
-    return torch.cuda.current_stream().cuda_stream
+    index = cache.device.index
+    if index is None or index != torch.cuda.current_device():
+        raise ValueError(f"the cache is on {cache.device}, which is not the current device")
+    return _raw_stream(index)
 
 
 def _fp8_vectors(cfg: Fp8Config, cache: Fp8Cache, t: torch.Tensor, heads: int, name: str) -> bytes:
