@@ -50,6 +50,7 @@ struct Fp8AttentionArgs {
     float *part_o, *part_ml;  // parts > 0: results of the slots, [slots][kv heads][rows][d] normalised, [slots][kv heads][rows][2] reference and sum
     int32_t parts;            // work items that the keys of a KV head and a group of rows are dealt out in, 0: one per sequence
     int32_t groups;           // of rows (set by the launch)
+    int32_t bound;            // the caller's, of the tokens held
 };
 // Both from host values alone.
 int64_t fp8_attention_parts(int64_t n_seq, int64_t n_kv_heads, int64_t r, int64_t n_query, int d, int64_t bound);

@@ -225,6 +225,7 @@ pk_status pk_fp8_attention(const pk_fp8_config *cfg, const pk_fp8_cache *cache, 
     a.lse = lse;
     a.parts = (int32_t)p.parts;
     a.groups = 0;
+    a.bound = bound;
     a.part_o = static_cast<float *>(workspace);
     a.part_ml = reinterpret_cast<float *>(static_cast<char *>(workspace) + p.o_bytes);
     return launch_fp8_attention(a, static_cast<hipStream_t>(stream)) == hipSuccess ? PK_OK : PK_ERR_DEVICE;

@@ -294,12 +294,12 @@ __device__ __forceinline__ int ends_of(const Fp8Queries &a, int (&end)[kMostSeqs
             const int len = fp8_state(a.states, seq, a.c.t_capacity).x, count = fp8_count(a.counts, seq, a.n_query);
             units = count > 0 ? max((len - first_visible(a, len, count) + 63) >> 6, 1) : 1;
         }
-        for (int o = 1; o < 64; o <<= 1) {
+        for (int o = 1; o < min(a.n_seq, 64); o <<= 1) {
             const int v = __shfl_up(units, o);
             if (lane >= o) units += v;
         }
         end[i] = units + before;
-        before = __shfl(end[i], 63);
+        before = __shfl(end[i], min(a.n_seq - 1 - 64 * i, 63));
     }
     return before;
 }
@@ -321,8 +321,8 @@ __device__ __forceinline__ void store_lse(const Fp8AttentionArgs &a, const Place
 
 // Rows of a workgroup: BY_ROWS, every wave has RT tiles of its own and walks all keys; else the waves share RT tiles and deal the keys
 // out among them, 64 at a time.
-template <int D, int RT, bool BY_ROWS, bool OPT>
-__global__ __launch_bounds__(kThreads, 2) void fp8_attention_kernel(Fp8AttentionArgs a)
+template <int D, int RT, int NW, bool BY_ROWS, bool OPT>
+__global__ __launch_bounds__(64 * NW, 2) void fp8_attention_kernel(Fp8AttentionArgs a)
 {
     using S = Shape<D>;
     const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
@@ -354,11 +354,12 @@ __global__ __launch_bounds__(kThreads, 2) void fp8_attention_kernel(Fp8Attention
     const bool whole = a.parts == 0 || (at_unit <= seq_from && seq_to <= stop);   // the sequence is this piece
     const Place p = place_of<true>(a.in, seq * hkv + kvh);
     const int64_t part0 = ((int64_t)(run + seq) * hkv + kvh) * rows;   // where partial results of the rows go
-    const int row0 = BY_ROWS ? (group * kWaves + wave) * 16 * RT : group * 16 * RT;
+    const int row0 = BY_ROWS ? (group * NW + wave) * 16 * RT : group * 16 * RT;
 
     // queries: in registers for one tile of up to 128 channels, else in LDS (the registers then hold two tiles' results or 256 channels' of one)
     constexpr bool kQueriesInLds = RT > 1 || D == 256;
-    __shared__ half8v sm_q[kQueriesInLds ? kWaves : 1][kQueriesInLds ? RT : 1][kQueriesInLds ? S::kSteps : 1][64];
+    constexpr int kOwn = BY_ROWS ? NW : 1;   // sets of queries
+    __shared__ half8v sm_q[kQueriesInLds ? kOwn : 1][kQueriesInLds ? RT : 1][kQueriesInLds ? S::kSteps : 1][64];
     Row row[RT];
     half8v q_reg[S::kSteps];
 #pragma unroll
@@ -366,13 +367,16 @@ __global__ __launch_bounds__(kThreads, 2) void fp8_attention_kernel(Fp8Attention
         const int at = row0 + 16 * rt + n;
         row[rt] = row_of(a.in, p, at);
         load_query<D>(q_reg, row[rt].factor, a.in, p.seq, p.kvh, at, at < p.count * a.in.r, g);
-        if constexpr (kQueriesInLds)   // of the wave's own: nothing to wait for but its own stores
+        if constexpr (kQueriesInLds) {
+            if (BY_ROWS || wave == 0)
 #pragma unroll
-            for (int s = 0; s < S::kSteps; ++s) sm_q[wave][rt][s][lane] = q_reg[s];
+                for (int s = 0; s < S::kSteps; ++s) sm_q[BY_ROWS ? wave : 0][rt][s][lane] = q_reg[s];
+        }
     }
+    if constexpr (kQueriesInLds && !BY_ROWS) __syncthreads();
     int q_lane = lane;
     const auto query = [&](int rt, int s) -> half8v {
-        if constexpr (kQueriesInLds) return sm_q[wave][rt][s][q_lane];
+        if constexpr (kQueriesInLds) return sm_q[BY_ROWS ? wave : 0][rt][s][q_lane];
         else return q_reg[s];
     };
     int lo, hi;
@@ -400,7 +404,7 @@ __global__ __launch_bounds__(kThreads, 2) void fp8_attention_kernel(Fp8Attention
 
     const uint32_t k_off = n * D + g * (D / 4), v_off = 4 * g * D + n * (D == 96 ? 4 : D / 16);
     const StreamMap map = a.in.c.map.of(p.stream);
-    const int first = BY_ROWS ? lo : lo + 64 * wave, step = BY_ROWS ? 64 : 64 * kWaves;
+    const int first = BY_ROWS ? lo : lo + 64 * wave, step = BY_ROWS ? 64 : 64 * NW;
     for (int t0 = first; t0 < hi; t0 += step) {
         const int64_t at = map.pos(t0);
         uint32_t kw[4][S::kKWords], vw[16][S::kVWords];
@@ -610,9 +614,9 @@ __global__ __launch_bounds__(kThreads, 2) void fp8_attention_kernel(Fp8Attention
         }
     } else {
         // rows that the waves bring together at a time: 32 to 34 KB of LDS
-        constexpr int kAtOnce = D == 256 ? 8 : 16, kPad = 4;
-        __shared__ float sm_o[kWaves][kAtOnce][D + kPad];
-        __shared__ float sm_m[kWaves][kAtOnce], sm_l[kWaves][kAtOnce];
+        constexpr int kAtOnce = (D == 256 ? 8 : 16) * 4 / NW, kPad = 4;
+        __shared__ float sm_o[NW][kAtOnce][D + kPad];
+        __shared__ float sm_m[NW][kAtOnce], sm_l[NW][kAtOnce];
 #pragma unroll
         for (int rt = 0; rt < RT; ++rt)
 #pragma unroll
@@ -632,14 +636,14 @@ __global__ __launch_bounds__(kThreads, 2) void fp8_attention_kernel(Fp8Attention
                         for (int i = 0; i < 4; ++i) sm_o[wave][q][channel_of<D>(4 * g + i, ct)] = o[rt][ct][i];
                 }
                 __syncthreads();
-                for (int e = threadIdx.x; e < here * (D / 4); e += kThreads) {
+                for (int e = threadIdx.x; e < here * (D / 4); e += 64 * NW) {
                     const int q = e / (D / 4), c = (e % (D / 4)) * 4, at = from + q;
                     if (at >= p.count * a.in.r) continue;
                     float top = -INFINITY;
-                    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, sm_m[w][q]);
+                    for (int w = 0; w < NW; ++w) top = fmaxf(top, sm_m[w][q]);
                     const float ref = top == -INFINITY ? 0.f : top;
                     float sum = 0.f, y[4] = {0.f, 0.f, 0.f, 0.f};
-                    for (int w = 0; w < kWaves; ++w) {
+                    for (int w = 0; w < NW; ++w) {
                         const float share = sm_l[w][q] * exp2_(sm_m[w][q] - ref);
                         sum += share;
                         for (int i = 0; i < 4; ++i) y[i] = fmaf(share, sm_o[w][q][c + i], y[i]);
@@ -665,15 +669,18 @@ __global__ __launch_bounds__(kThreads, 2) void fp8_attention_kernel(Fp8Attention
     }
 }
 
-// The pieces of a row together: sum_s l_s 2^(m_s - m) o_s / sum_s l_s 2^(m_s - m).  A workgroup takes some rows of a (sequence, KV head)
-// that was split, a thread two channels of a row.
+// The pieces of a row together: sum_s l_s 2^(m_s - m) o_s / sum_s l_s 2^(m_s - m).  A wave takes a row of a (sequence, KV head) that was
+// cut: the factors of 64 pieces in its lanes, then the pieces' results one after the other, a lane D / 64 channels (two of 48 lanes at
+// 96), with several loads in flight.  (A thread that read every piece's factors itself took 20 us for the 64 pieces of one sequence of 32k.)
+constexpr int kMergeRows = 4;
 template <int D>
-__global__ __launch_bounds__(256) void fp8_merge_kernel(Fp8AttentionArgs a)
+__global__ __launch_bounds__(64 * kMergeRows) void fp8_merge_kernel(Fp8AttentionArgs a)
 {
-    constexpr int kRows = 256 / (D / 2);
-    const int rows = a.in.r * a.in.n_query, hkv = a.in.c.n_kv_heads, groups = (rows + kRows - 1) / kRows;
-    const int kvh = blockIdx.x % hkv, rest = blockIdx.x / hkv, row = rest % groups * kRows + (int)threadIdx.x / (D / 2);
-    const int seq = rest / groups;
+    constexpr int kPer = D <= 128 ? 2 : 4;   // channels per lane
+    const int rows = a.in.r * a.in.n_query, hkv = a.in.c.n_kv_heads, groups = (rows + kMergeRows - 1) / kMergeRows;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int kvh = blockIdx.x % hkv, rest = blockIdx.x / hkv, row = rest % groups * kMergeRows + wave, seq = rest / groups;
+    const Place p = place_of<false>(a.in, seq * hkv + kvh);   // (requested before the rest)
     int end[kMostSeqs / 64], from = 0, to = 0;
     const int all = __builtin_amdgcn_readfirstlane(ends_of(a.in, end)), per = run_length(all, a.parts);
 #pragma unroll
@@ -682,29 +689,54 @@ __global__ __launch_bounds__(256) void fp8_merge_kernel(Fp8AttentionArgs a)
         if (seq > 0 && (seq - 1) / 64 == i) from = before;
         if (seq / 64 == i) to = here;
     }
+    from = __builtin_amdgcn_readfirstlane(from);
+    to = __builtin_amdgcn_readfirstlane(to);
     const int first_run = from / per, pieces = (to - 1) / per - first_run + 1;
     if (pieces == 1) return;   // written already
-    const Place p = place_of<true>(a.in, seq * hkv + kvh);
-    if ((int)threadIdx.x >= kRows * (D / 2) || row >= p.count * a.in.r) return;
-    const int c = (int)threadIdx.x % (D / 2) * 2;
+    if (row >= p.count * a.in.r) return;
     const int64_t first = ((int64_t)(first_run + seq) * hkv + kvh) * rows + row, step = (int64_t)hkv * rows;
-    float top = -INFINITY;
-    for (int s = 0; s < pieces; ++s) top = fmaxf(top, a.part_ml[2 * (first + s * step)]);
-    const float ref = top == -INFINITY ? 0.f : top;
-    float sum = 0.f, y[2] = {0.f, 0.f};
-    for (int s = 0; s < pieces; ++s) {
-        const int64_t slot = first + s * step;
-        const float part = a.part_ml[2 * slot + 1] * exp2_(a.part_ml[2 * slot] - ref);
-        sum += part;
-        const float2 o = *reinterpret_cast<const float2 *>(a.part_o + slot * D + c);
-        y[0] = fmaf(part, o.x, y[0]);
-        y[1] = fmaf(part, o.y, y[1]);
+    const int c = min(lane * kPer, D - kPer);
+    float top = -INFINITY, sum = 0.f, y[kPer];
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) y[i] = 0.f;
+    for (int s0 = 0; s0 < pieces; s0 += 64) {
+        float2 ml = make_float2(-INFINITY, 0.f);
+        if (s0 + lane < pieces) ml = *reinterpret_cast<const float2 *>(a.part_ml + 2 * (first + (s0 + lane) * step));
+        const float most_of_row[1] = {row_max(ml.x)};
+        const float most = fold_rows(most_of_row, MaxF());
+        if (most > top) {
+            const float by = exp2_(top - most);
+            top = most;
+            sum *= by;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) y[i] *= by;
+        }
+        const float share = ml.y * exp2_(ml.x - (top == -INFINITY ? 0.f : top));
+        const float sum_of_row[1] = {row_sum(share)};
+        sum += fold_rows(sum_of_row, AddF());
+        const int here = min(pieces - s0, 64);
+#pragma unroll 8
+        for (int s = 0; s < here; ++s) {
+            const float w = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, share), s));
+            const float *o = a.part_o + (first + (s0 + s) * step) * D + c;
+            if constexpr (kPer == 2) {
+                const float2 v = *reinterpret_cast<const float2 *>(o);
+                y[0] = fmaf(w, v.x, y[0]);
+                y[1] = fmaf(w, v.y, y[1]);
+            } else {
+                const float4 v = *reinterpret_cast<const float4 *>(o);
+                y[0] = fmaf(w, v.x, y[0]);
+                y[1] = fmaf(w, v.y, y[1]);
+                y[2] = fmaf(w, v.z, y[2]);
+                y[3] = fmaf(w, v.w, y[3]);
+            }
+        }
     }
     const float inv = sum == 0.f ? 0.f : 1.f / sum;
-    y[0] *= inv;
-    y[1] *= inv;
-    store_row<D>(a, p, row, c, y, 2);
-    if (c == 0) store_lse(a, p, row, top, sum);
+#pragma unroll
+    for (int i = 0; i < kPer; ++i) y[i] *= inv;
+    if (lane * kPer < D) store_row<D>(a, p, row, c, y, kPer);
+    if (lane == 0) store_lse(a, p, row, top, sum);
 }
 
 // ---- the weight of every token -------------------------------------------------------------------------------------------
@@ -820,10 +852,6 @@ __global__ __launch_bounds__(kThreads, 2) void fp8_weights_kernel(Fp8WeightsArgs
     }
 }
 
-#ifndef R1
-#define R1 512
-#define R2 512
-#endif
 // How many rows a workgroup of the attention takes, and how.
 struct Rows {
     int tiles;      // per wave (RT)
@@ -839,11 +867,20 @@ Rows rows_of(int64_t rows, int d)
     return x;
 }
 
-template <int D, int RT, bool BY_ROWS>
+// Workgroups of eight waves that share a sequence's rows, instead of four:
+// few workgroups over short caches, where nothing is then left to merge (8 heads, 32 query heads of 128 channels, one token: 1.1k tokens 14.7 us
+// against 18.7 with runs, merged; 2k 17.7 and 19.4; 3k 22.3 and 19.3), and
+bool eight_waves(int64_t workgroups, int64_t bound) { return workgroups <= 256 && bound <= 2048; }
+// long runs, which make half as many pieces then (16 sequences x 32k tokens 185.6 -> 181.4 us, 8 of them with 256 channels 201 -> 186); shorter
+// ones change from sequence to sequence more often, where eight waves wait for each other (32 sequences of 700 to 6000 tokens, five
+// queries: 72.5 -> 77.5).
+bool long_runs(int64_t n_seq, int64_t across, int64_t bound) { return n_seq * ((bound + 63) / 64) * across >= 128 * 256; }
+
+template <int D, int RT, int NW, bool BY_ROWS>
 void launch_rt(const Fp8AttentionArgs &a, uint32_t grid, bool opt, hipStream_t s)
 {
-    if (opt) fp8_attention_kernel<D, RT, BY_ROWS, true><<<grid, kThreads, 0, s>>>(a);
-    else fp8_attention_kernel<D, RT, BY_ROWS, false><<<grid, kThreads, 0, s>>>(a);
+    if (opt) fp8_attention_kernel<D, RT, NW, BY_ROWS, true><<<grid, 64 * NW, 0, s>>>(a);
+    else fp8_attention_kernel<D, RT, NW, BY_ROWS, false><<<grid, 64 * NW, 0, s>>>(a);
 }
 
 template <int D>
@@ -854,17 +891,19 @@ hipError_t launch_d(Fp8AttentionArgs &a, hipStream_t s)
     a.groups = (int)((rows + x.per_group - 1) / x.per_group);
     const uint32_t grid = (uint32_t)((a.parts > 0 ? a.parts : a.in.n_seq) * a.in.c.n_kv_heads * a.groups);
     const bool opt = a.in.cap > 0.f || a.in.slopes || a.in.window > 0;
+    const bool wide = a.parts > 0 ? long_runs(a.in.n_seq, (int64_t)a.in.c.n_kv_heads * a.groups, a.bound) : eight_waves(grid, a.bound);
     if (x.tiles == 1) {
-        if (x.by_rows) launch_rt<D, 1, true>(a, grid, opt, s);
-        else launch_rt<D, 1, false>(a, grid, opt, s);
+        if (x.by_rows) launch_rt<D, 1, 4, true>(a, grid, opt, s);
+        else if (wide) launch_rt<D, 1, 8, false>(a, grid, opt, s);
+        else launch_rt<D, 1, 4, false>(a, grid, opt, s);
     } else if constexpr (D < 256) {
-        if (x.by_rows) launch_rt<D, 2, true>(a, grid, opt, s);
-        else launch_rt<D, 2, false>(a, grid, opt, s);
+        if (x.by_rows) launch_rt<D, 2, 4, true>(a, grid, opt, s);
+        else if (wide) launch_rt<D, 2, 8, false>(a, grid, opt, s);
+        else launch_rt<D, 2, 4, false>(a, grid, opt, s);
     }
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.parts == 0) return e;
-    constexpr int kRows = 256 / (D / 2);
-    fp8_merge_kernel<D><<<(uint32_t)((int64_t)a.in.n_seq * a.in.c.n_kv_heads * ((rows + kRows - 1) / kRows)), 256, 0, s>>>(a);
+    fp8_merge_kernel<D><<<(uint32_t)((int64_t)a.in.n_seq * a.in.c.n_kv_heads * ((rows + kMergeRows - 1) / kMergeRows)), 64 * kMergeRows, 0, s>>>(a);
     return hipGetLastError();
 }
 
@@ -885,10 +924,9 @@ int64_t fp8_attention_parts(int64_t n_seq, int64_t n_kv_heads, int64_t r, int64_
 {
     const Rows x = rows_of(r * n_query, d);
     const int64_t across = n_kv_heads * ((r * n_query + x.per_group - 1) / x.per_group);   // workgroups per run
-    const int64_t resident = x.tiles == 1 && d < 256 ? R1 : R2;
-    int64_t parts = resident / across;
+    int64_t parts = (!x.by_rows && long_runs(n_seq, across, bound) ? 256 : 512) / across;
     if (parts < 1) parts = 1;
-    if (n_seq > kMostSeqs || n_seq >= 4 * parts) return 0;
+    if (n_seq > kMostSeqs || n_seq >= 4 * parts || (!x.by_rows && eight_waves(n_seq * across, bound))) return 0;
     const int64_t most = n_seq * ((bound + 64 * kLeastUnits - 1) / (64 * kLeastUnits));
     if (parts > most) parts = most;
     return parts <= 1 && n_seq == 1 ? 0 : parts;
