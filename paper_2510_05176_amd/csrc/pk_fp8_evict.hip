@@ -1,9 +1,8 @@
 // Eviction from the 8-bit cache, in two launches: which tokens stay (one workgroup per stream, into the workspace), and their
 // move into the other cache (one workgroup per new block of a stream, K and V).
 //
-// The choice is a radix selection over the weights as ordered integers: three histograms of 11, 11 and 10 bits find the weight of
-// the last token that stays, then every wave counts and writes its own run of tokens, so that ties go to the earlier ones and
-// the order is kept.  It reads the weights five times, from the caches but for the first.
+// Weights are chosen among as integers in the same order: the weight of the last token that stays, then which tokens are above it, and of
+// the equal ones the first, so that the order is kept and ties go to the earlier ones.
 #include "pk_fp8.h"
 
 namespace pk {
@@ -20,7 +19,103 @@ __device__ __forceinline__ uint32_t order_of(float w)
     return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
 
+// What both selections end with: the tokens that are kept whatever their weight
+__device__ __forceinline__ void keep_ends(const Fp8EvictArgs &a, int32_t *kept, int hi)
+{
+    for (int i = threadIdx.x; i < a.keep_first; i += kSelThreads) kept[i] = i;
+    for (int i = threadIdx.x; i < a.keep_last; i += kSelThreads) kept[a.budget - a.keep_last + i] = hi + i;
+}
+
+// Up to K * kSelThreads candidates, their weights in registers (token lo + 1024 i + thread in the i-th): the largest integer that at
+// least `need` of them reach, bit by bit from the top, counted by ballots; done as soon as exactly `need` reach it.  A pass is K comparisons
+// and one barrier: of 256 streams of 16k tokens 33 us with the histograms below, KK with this.
+template <int K>
 __global__ __launch_bounds__(kSelThreads) void fp8_select_kernel(Fp8EvictArgs a)
+{
+    __shared__ uint32_t sm_count[2][kSelWaves];
+    __shared__ uint32_t sm_above[K * kSelWaves], sm_equal[K * kSelWaves];
+    const int stream = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int len = __builtin_amdgcn_readfirstlane(fp8_state(a.states, stream / a.from.n_kv_heads, a.from.t_capacity).x);
+    if (len <= a.budget) return;   // the move takes such a sequence whole
+    int32_t *kept = a.kept + (int64_t)stream * a.budget;
+    const int lo = a.keep_first, hi = len - a.keep_last;   // candidates; more of them than the budget has room for
+    const float *w = a.from.weight + (int64_t)stream * a.from.t_capacity;
+    uint32_t need = (uint32_t)(a.budget - a.keep_first - a.keep_last);
+    uint32_t u[K];
+#pragma unroll
+    for (int i = 0; i < K; ++i) {
+        const int t = lo + i * kSelThreads + tid;
+        u[i] = t < hi ? order_of(w[t]) : 0;
+    }
+    keep_ends(a, kept, hi);
+    if (need == 0) return;
+    uint32_t floor = 0;   // kept: above it, and the first of those equal to it
+    bool exact = false;
+    for (int bit = 31; bit >= 0 && !exact; --bit) {
+        const uint32_t to = floor | (1u << bit);
+        uint32_t mine = 0;
+#pragma unroll
+        for (int i = 0; i < K; ++i) mine += __popcll(__ballot(u[i] >= to));
+        if (lane == 0) sm_count[bit & 1][wave] = mine;
+        __syncthreads();   // (the other half is free: every wave is past the pass that read it)
+        uint32_t all = 0;
+#pragma unroll
+        for (int i = 0; i < kSelWaves; ++i) all += sm_count[bit & 1][i];
+        if (all >= need) floor = to;
+        exact = all == need;
+    }
+    if (exact) floor -= 1;   // `need` of them reach it: all are above this, and no equal ones are taken
+    // places in the order of the tokens
+    uint64_t above[K], equal[K];
+#pragma unroll
+    for (int i = 0; i < K; ++i) {
+        const bool here = lo + i * kSelThreads + tid < hi;
+        above[i] = __ballot(here && u[i] > floor);
+        equal[i] = __ballot(here && !exact && u[i] == floor);
+        if (lane == 0) {
+            sm_above[i * kSelWaves + wave] = __popcll(above[i]);
+            sm_equal[i * kSelWaves + wave] = __popcll(equal[i]);
+        }
+    }
+    __syncthreads();
+    if (wave == 0) {   // exclusive sums, K * kSelWaves / 64 neighbours per lane
+        constexpr int kPer = K * kSelWaves / 64;
+        uint32_t x[kPer], y[kPer], sx = 0, sy = 0;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            x[i] = sx;
+            y[i] = sy;
+            sx += sm_above[lane * kPer + i];
+            sy += sm_equal[lane * kPer + i];
+        }
+        uint32_t ex = sx, ey = sy;
+        for (int o = 1; o < 64; o <<= 1) {
+            const uint32_t vx = __shfl_up(ex, o), vy = __shfl_up(ey, o);
+            if (lane >= o) {
+                ex += vx;
+                ey += vy;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            sm_above[lane * kPer + i] = ex - sx + x[i];
+            sm_equal[lane * kPer + i] = ey - sy + y[i];
+        }
+        if (lane == 63) sm_count[0][0] = ex;
+    }
+    __syncthreads();
+    need -= sm_count[0][0];   // of the equal ones
+    const uint64_t below = (1ull << lane) - 1;
+#pragma unroll
+    for (int i = 0; i < K; ++i) {
+        const uint32_t n_above = sm_above[i * kSelWaves + wave] + __popcll(above[i] & below), n_equal = sm_equal[i * kSelWaves + wave] + __popcll(equal[i] & below);
+        const bool gt = (above[i] >> lane) & 1, eq = (equal[i] >> lane) & 1;
+        if (gt || (eq && n_equal < need)) kept[lo + n_above + min(n_equal, need)] = lo + i * kSelThreads + tid;
+    }
+}
+
+// Any number of candidates: three histograms of 11, 11 and 10 bits over the memory (or its caches), then every wave's own run of tokens.
+__global__ __launch_bounds__(kSelThreads) void fp8_select_long_kernel(Fp8EvictArgs a)
 {
     __shared__ uint32_t hist[kBins];
     __shared__ uint32_t sm_prefix, sm_need, sm_wave[kSelWaves][2];
@@ -105,110 +200,122 @@ __global__ __launch_bounds__(kSelThreads) void fp8_select_kernel(Fp8EvictArgs a)
             equal_before += __popcll(m_eq);
         }
     }
-    for (int i = tid; i < a.keep_first; i += kSelThreads) kept[i] = i;
-    for (int i = tid; i < a.keep_last; i += kSelThreads) kept[a.budget - a.keep_last + i] = hi + i;
+    keep_ends(a, kept, hi);
 }
 
 constexpr int kMoveThreads = 256;
 
-template <int D>
+// Magnitudes as binary32 bits with the scale's exponent added to theirs, which no exponent is too large or small for (a code may
+// stand for up to 2^128); the most negative integer stands for zero.
+__device__ __forceinline__ int size_of_codes(const uint4 &v, int field, bool &bad)
+{
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    // e4m3 codes without their sign are ordered like what they stand for: the largest byte that is no NaN
+    uint32_t most = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const uint32_t b = (w[j] >> (8 * k)) & 0x7fu;
+            bad |= b == 0x7fu;
+            most = max(most, b == 0x7fu ? 0u : b);
+        }
+    return most ? __builtin_bit_cast(int, (float)codes_lo(most)[0]) + ((field - 127) << 23) : INT32_MIN;
+}
+__device__ __forceinline__ uint4 rescaled(const uint4 &v, int shift)
+{
+    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    uint32_t o[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const half2v lo = codes_lo(w[j]), hi = codes_hi(w[j]);
+        const float y[4] = {ldexpf((float)lo[0], shift), ldexpf((float)lo[1], shift), ldexpf((float)hi[0], shift), ldexpf((float)hi[1], shift)};
+        o[j] = codes4(y, 1.f);
+    }
+    return make_uint4(o[0], o[1], o[2], o[3]);
+}
+
+// K and V of a block together: where their tokens are is looked up once, and twice as much is on its way (of 256 streams of 1024 tokens
+// kept 38.5 us with a workgroup each, MM with this).
+template <int D, int B>
 __global__ __launch_bounds__(kMoveThreads) void fp8_move_kernel(Fp8EvictArgs a)
 {
-    constexpr int kPerRow = D / 16;
-    constexpr int kMost = (128 * kPerRow + kMoveThreads - 1) / kMoveThreads;   // pieces of 16 codes per thread, largest block
-    __shared__ int sm_max[kMoveThreads / 64], sm_bad[kMoveThreads / 64], sm_row[128], sm_field[128];
+    constexpr int kPerRow = D / 16;                                              // pieces of 16 codes
+    constexpr int kMost = (B * kPerRow + kMoveThreads - 1) / kMoveThreads;       // per thread
+    __shared__ int sm_max[2][kMoveThreads / 64], sm_bad[2][kMoveThreads / 64], sm_field[2][B];
+    __shared__ int64_t sm_row[B];
     const int tid = threadIdx.x, hkv = a.from.n_kv_heads;
     const int stream = blockIdx.y, seq = stream / hkv;
-    const int B = 1 << a.from.log_block;
     const int2 st = fp8_state(a.states, seq, a.from.t_capacity);
-    const int held = min(st.x, a.budget);
-    const bool whole = st.x <= a.budget;
-    const bool is_v = blockIdx.x & 1;
-    const int t0 = (int)(blockIdx.x >> 1) * B, n = min(held - t0, B);
+    const int held = min(st.x, a.budget), t0 = (int)blockIdx.x * B, n = min(held - t0, B);
     if (tid == 0 && stream % hkv == 0 && blockIdx.x == 0) *reinterpret_cast<int4 *>(a.to_states + 4 * (int64_t)seq) = make_int4(held, st.y, 0, 0);
     if (n <= 0) return;
     const StreamMap from = a.from.map.of(stream);
     if (tid < n) {
         // an index from the workspace is one that the selection wrote, below the sequence's length
-        const int t = whole ? t0 + tid : a.kept[(int64_t)stream * a.budget + t0 + tid];
-        int64_t row;
-        if (from.pages) {
-            const int page = min(max(from.pages[t >> from.shift], 0), from.n_pages - 1);
-            row = from.pos_in(page, t);
-        } else {
-            row = from.base + t;
-        }
-        sm_row[tid] = t;
-        sm_field[tid] = field_of_scale((is_v ? a.from.v_scale : a.from.k_scale)[row >> a.from.log_block]);
-        if (!is_v) {
-            const int64_t x = (int64_t)stream * a.from.t_capacity + t, y = (int64_t)stream * a.to.t_capacity + t0 + tid;
-            a.to.pos[y] = a.from.pos[x];
-            if (a.to.weight) a.to.weight[y] = a.from.weight[x];
-        }
+        const int t = st.x <= a.budget ? t0 + tid : a.kept[(int64_t)stream * a.budget + t0 + tid];
+        const int page = from.pages ? min(max(from.pages[t >> from.shift], 0), from.n_pages - 1) : 0;
+        const int64_t row = from.pos_in(page, t);
+        sm_row[tid] = row;
+        sm_field[0][tid] = field_of_scale(a.from.k_scale[row >> a.from.log_block]);
+        sm_field[1][tid] = field_of_scale(a.from.v_scale[row >> a.from.log_block]);
+        const int64_t x = (int64_t)stream * a.from.t_capacity + t, y = (int64_t)stream * a.to.t_capacity + t0 + tid;
+        a.to.pos[y] = a.from.pos[x];
+        if (a.to.weight) a.to.weight[y] = a.from.weight[x];
     }
     __syncthreads();
-    const uint8_t *src = is_v ? a.from.v_codes : a.from.k_codes;
-    uint4 raw[kMost];
+    uint4 raw[2][kMost];
 #pragma unroll
     for (int i = 0; i < kMost; ++i) {
         const int p = tid + i * kMoveThreads;
-        raw[i] = make_uint4(0, 0, 0, 0);
+        raw[0][i] = raw[1][i] = make_uint4(0, 0, 0, 0);
         if (p < n * kPerRow) {
-            const int t = sm_row[p / kPerRow];
-            const int64_t row = from.pages ? from.pos_in(min(max(from.pages[t >> from.shift], 0), from.n_pages - 1), t) : from.base + t;
-            raw[i] = *reinterpret_cast<const uint4 *>(src + row * D + (p % kPerRow) * 16);
+            const int64_t at = sm_row[p / kPerRow] * D + (p % kPerRow) * 16;
+            raw[0][i] = *reinterpret_cast<const uint4 *>(a.from.k_codes + at);
+            raw[1][i] = *reinterpret_cast<const uint4 *>(a.from.v_codes + at);
         }
     }
-    // Magnitudes as binary32 bits with the scale's exponent added to theirs, which no exponent is too large or small for (a code may
-    // stand for up to 2^128); the most negative integer stands for zero.
-    int amax = INT32_MIN;
-    bool bad = false;
+    int most[2] = {INT32_MIN, INT32_MIN};
+    bool bad[2] = {false, false};
 #pragma unroll
     for (int i = 0; i < kMost; ++i) {
-        const int p = tid + i * kMoveThreads;
-        if (p >= n * kPerRow) continue;
-        const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
-        // e4m3 codes without their sign are ordered like what they stand for: the largest byte that is no NaN
-        uint32_t most = 0;
+        const int token = min((tid + i * kMoveThreads) / kPerRow, n - 1);   // (past the block: zeros, which do not count)
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                const uint32_t b = (w[j] >> (8 * k)) & 0x7fu;
-                bad |= b == 0x7fu;
-                most = max(most, b == 0x7fu ? 0u : b);
-            }
-        if (most) amax = max(amax, __builtin_bit_cast(int, (float)codes_lo(most)[0]) + ((sm_field[p / kPerRow] - 127) << 23));
+        for (int s = 0; s < 2; ++s) most[s] = max(most[s], size_of_codes(raw[s][i], sm_field[s][token], bad[s]));
     }
-    for (int o = 1; o < 64; o <<= 1) amax = max(amax, __shfl_xor(amax, o));
-    const bool any_bad = __any(bad);
-    if ((tid & 63) == 0) {
-        sm_max[tid >> 6] = amax;
-        sm_bad[tid >> 6] = any_bad;
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+        for (int o = 1; o < 64; o <<= 1) most[s] = max(most[s], __shfl_xor(most[s], o));
+        const bool any = __any(bad[s]);
+        if ((tid & 63) == 0) {
+            sm_max[s][tid >> 6] = most[s];
+            sm_bad[s][tid >> 6] = any;
+        }
     }
     __syncthreads();
-    amax = max(max(sm_max[0], sm_max[1]), max(sm_max[2], sm_max[3]));
-    const int flagged = sm_bad[0] | sm_bad[1] | sm_bad[2] | sm_bad[3];
-    const int field = max((amax >> 23) - 8 + ((amax & 0x7fffff) > 0x600000 ? 1 : 0), 1);
     const int64_t row0 = a.to.map.of(stream).pos(t0);
-    uint8_t *dst = (is_v ? a.to.v_codes : a.to.k_codes) + row0 * D;
 #pragma unroll
-    for (int i = 0; i < kMost; ++i) {
-        const int p = tid + i * kMoveThreads;
-        if (p >= n * kPerRow) continue;
-        const int shift = sm_field[p / kPerRow] - field;
-        const uint32_t w[4] = {raw[i].x, raw[i].y, raw[i].z, raw[i].w};
-        uint32_t o[4];
+    for (int s = 0; s < 2; ++s) {
+        const int size = max(max(sm_max[s][0], sm_max[s][1]), max(sm_max[s][2], sm_max[s][3]));
+        const int flagged = sm_bad[s][0] | sm_bad[s][1] | sm_bad[s][2] | sm_bad[s][3];
+        const int field = max((size >> 23) - 8 + ((size & 0x7fffff) > 0x600000 ? 1 : 0), 1);
+        uint8_t *dst = (s ? a.to.v_codes : a.to.k_codes) + row0 * D;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const half2v lo = codes_lo(w[j]), hi = codes_hi(w[j]);
-            const float y[4] = {ldexpf((float)lo[0], shift), ldexpf((float)lo[1], shift), ldexpf((float)hi[0], shift), ldexpf((float)hi[1], shift)};
-            o[j] = codes4(y, 1.f);
+        for (int i = 0; i < kMost; ++i) {
+            const int p = tid + i * kMoveThreads;
+            if (p < n * kPerRow) *reinterpret_cast<uint4 *>(dst + (int64_t)p * 16) = rescaled(raw[s][i], sm_field[s][p / kPerRow] - field);
         }
-        *reinterpret_cast<uint4 *>(dst + (int64_t)p * 16) = make_uint4(o[0], o[1], o[2], o[3]);
+        if (tid == 0)
+            (s ? a.to.v_scale : a.to.k_scale)[row0 >> a.to.log_block] = __builtin_bit_cast(float, ((uint32_t)field << 23) | ((uint32_t)flagged << 31));
     }
-    if (tid == 0)
-        (is_v ? a.to.v_scale : a.to.k_scale)[row0 >> a.to.log_block] = __builtin_bit_cast(float, ((uint32_t)field << 23) | ((uint32_t)flagged << 31));
+}
+
+template <int D>
+void launch_move(const Fp8EvictArgs &a, const dim3 &grid, hipStream_t s)
+{
+    if (a.from.log_block == 5) fp8_move_kernel<D, 32><<<grid, kMoveThreads, 0, s>>>(a);
+    else if (a.from.log_block == 6) fp8_move_kernel<D, 64><<<grid, kMoveThreads, 0, s>>>(a);
+    else fp8_move_kernel<D, 128><<<grid, kMoveThreads, 0, s>>>(a);
 }
 
 }  // namespace
@@ -216,15 +323,24 @@ __global__ __launch_bounds__(kMoveThreads) void fp8_move_kernel(Fp8EvictArgs a)
 hipError_t launch_fp8_evict(const Fp8EvictArgs &a, hipStream_t s)
 {
     const int N = a.n_seq * a.from.n_kv_heads, B = 1 << a.from.log_block;
-    fp8_select_kernel<<<N, kSelThreads, 0, s>>>(a);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    const dim3 grid(2 * (uint32_t)(((int64_t)a.budget + B - 1) / B), N);
+    // what a sequence can have to choose from, by the cache's capacity
+    const int64_t most = (int64_t)a.from.t_capacity - a.keep_first - a.keep_last;
+    if (a.budget < a.from.t_capacity) {
+        if (most <= 4 * kSelThreads) fp8_select_kernel<4><<<N, kSelThreads, 0, s>>>(a);
+        else if (most <= 16 * kSelThreads) fp8_select_kernel<16><<<N, kSelThreads, 0, s>>>(a);
+        else if (most <= 32 * kSelThreads) fp8_select_kernel<32><<<N, kSelThreads, 0, s>>>(a);
+        else fp8_select_long_kernel<<<N, kSelThreads, 0, s>>>(a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    // no sequence holds more than the capacity: blocks beyond it have nothing
+    const int64_t kept = a.budget < a.from.t_capacity ? a.budget : a.from.t_capacity;
+    const dim3 grid((uint32_t)((kept + B - 1) / B), N);
     switch (a.d) {
-    case 64: fp8_move_kernel<64><<<grid, kMoveThreads, 0, s>>>(a); break;
-    case 96: fp8_move_kernel<96><<<grid, kMoveThreads, 0, s>>>(a); break;
-    case 128: fp8_move_kernel<128><<<grid, kMoveThreads, 0, s>>>(a); break;
-    default: fp8_move_kernel<256><<<grid, kMoveThreads, 0, s>>>(a);
+    case 64: launch_move<64>(a, grid, s); break;
+    case 96: launch_move<96>(a, grid, s); break;
+    case 128: launch_move<128>(a, grid, s); break;
+    default: launch_move<256>(a, grid, s);
     }
     return hipGetLastError();
 }

@@ -374,6 +374,34 @@ def test_evict_long(pk):
     p.check(to_cfg, to, [p.seqs[0].evict(3001, 3, 100)])
 
 
+@pytest.mark.parametrize("cap,held,budget,first,last", [
+    (4096, 4000, 1000, 0, 0), (4224, 4223, 4000, 100, 60), (16384, 16380, 64, 1, 1), (32768, 32768, 20000, 0, 5), (32832, 32832, 32000, 40, 24), (65536, 40000, 333, 0, 0)])
+@pytest.mark.parametrize("kind", ["distinct", "few", "equal"])
+def test_evict_chooses_the_largest(pk, cap, held, budget, first, last, kind):
+    """Every way of choosing, by the capacity; weights that are all different, from few values, all the same."""
+    p = Pair(pk, 18, n_seq=1, hkv=2, r=1, d=64, block=64, cap=cap)
+    p.cache.states.copy_(torch.tensor([[held, held, 0, 0]]))
+    p.cache.buf["k_codes"].fill_(8)      # what the tokens hold is not looked at here
+    p.cache.buf["v_codes"].fill_(8)
+    p.cache.buf["k_scale"].fill_(1.0)
+    p.cache.buf["v_scale"].fill_(1.0)
+    pos = np.arange(cap, dtype=np.int32)
+    p.cache.buf["pos"].copy_(torch.from_numpy(np.concatenate([pos, pos])))
+    w = np.stack([np.float32(p.rng.permutation(cap) + 1) * 1e-3, np.float32(p.rng.permutation(cap) + 1) * -1e20])
+    w = w if kind == "distinct" else np.float32(p.rng.integers(0, 4, (2, cap)) * 0.1) if kind == "few" else np.full((2, cap), 0.7, np.float32)
+    p.cache.buf["weight"].copy_(torch.from_numpy(w.reshape(-1)))
+    to_cap = -(-budget // 64) * 64
+    to_cfg = pk.Fp8Config(n_seq=1, n_kv_heads=2, n_q_heads=2, head_dim=64, t_capacity=to_cap)
+    to = p.new_cache(to_cfg)
+    pk.pk_fp8_evict(p.cfg, p.cache, to_cfg, to, budget, keep_first=first, keep_last=last)
+    got = to.buf["pos"].cpu().numpy().reshape(2, -1)[:, :budget]
+    for h in range(2):
+        middle = np.arange(first, held - last)
+        order = middle[np.argsort(-w[h, middle].astype(np.float64), kind="stable")][:budget - first - last]
+        assert np.array_equal(got[h], np.sort(np.concatenate([np.arange(first), order, np.arange(held - last, held)])))
+    assert to.states.tolist() == [[budget, held, 0, 0]]
+
+
 @pytest.mark.parametrize("bf16,page", [(False, 0), (True, 128)])
 def test_a_serving_loop(pk, bf16, page):
     """Prompts, generation steps with weights, eviction, further steps with window and distance bias over the gaps, drafts, eviction
