@@ -19,21 +19,29 @@ __device__ __forceinline__ uint32_t order_of(float w)
     return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
 
-// What both selections end with: the tokens that are kept whatever their weight
+// What both selections write besides: the tokens that are kept whatever their weight
 __device__ __forceinline__ void keep_ends(const Fp8EvictArgs &a, int32_t *kept, int hi)
 {
-    for (int i = threadIdx.x; i < a.keep_first; i += kSelThreads) kept[i] = i;
-    for (int i = threadIdx.x; i < a.keep_last; i += kSelThreads) kept[a.budget - a.keep_last + i] = hi + i;
+    for (int i = threadIdx.x; i < a.keep_first; i += blockDim.x) kept[i] = i;
+    for (int i = threadIdx.x; i < a.keep_last; i += blockDim.x) kept[a.budget - a.keep_last + i] = hi + i;
 }
 
-// Up to K * kSelThreads candidates, their weights in registers (token lo + 1024 i + thread in the i-th): the largest integer that at
-// least `need` of them reach, bit by bit from the top, counted by ballots; done as soon as exactly `need` reach it.  A pass is K comparisons
-// and one barrier: of 256 streams of 16k tokens 33 us with the histograms below, KK with this.
+// Up to 4 K tokens per thread, their weights in registers (four neighbours at a time: token 4 (threads i + thread) + j): the largest integer that
+// at least `need` of them reach, bit by bit from the top; a pass is 4 K comparisons, a sum over the workgroup and one barrier.  Once at most
+// kRanked are left between what is kept for certain and what is not, they go to LDS and are ranked against each other; it ends earlier where
+// exactly `need` reach a bound.  (256 streams of 16k tokens to 1024: 33 us with the histograms below, 18.6 with this; 19.8 with eight waves, 27 with
+// four, which do not cover each other's latencies.)
+constexpr int kRegThreads = 1024, kRegWaves = kRegThreads / 64, kRanked = 64;
+
+// set bits of the mask below the lane
+__device__ __forceinline__ uint32_t below_lane(uint64_t mask) { return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0)); }
+
 template <int K>
-__global__ __launch_bounds__(kSelThreads) void fp8_select_kernel(Fp8EvictArgs a)
+__global__ __launch_bounds__(kRegThreads) void fp8_select_kernel(Fp8EvictArgs a)
 {
-    __shared__ uint32_t sm_count[2][kSelWaves];
-    __shared__ uint32_t sm_above[K * kSelWaves], sm_equal[K * kSelWaves];
+    __shared__ float sm_count[2][kRegWaves];
+    __shared__ uint32_t sm_above[K * kRegWaves], sm_equal[K * kRegWaves];   // of four neighbours of a wave
+    __shared__ uint32_t sm_left[kRanked], sm_n_left, sm_floor, sm_ties, sm_all_above;
     const int stream = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int len = __builtin_amdgcn_readfirstlane(fp8_state(a.states, stream / a.from.n_kv_heads, a.from.t_capacity).x);
     if (len <= a.budget) return;   // the move takes such a sequence whole
@@ -41,52 +49,111 @@ __global__ __launch_bounds__(kSelThreads) void fp8_select_kernel(Fp8EvictArgs a)
     const int lo = a.keep_first, hi = len - a.keep_last;   // candidates; more of them than the budget has room for
     const float *w = a.from.weight + (int64_t)stream * a.from.t_capacity;
     uint32_t need = (uint32_t)(a.budget - a.keep_first - a.keep_last);
-    uint32_t u[K];
+    // All loads on their way before the first is looked at (left to itself the compiler puts each into a branch with a wait of its own).
+    // 0: no candidate, or a NaN; the capacity is a multiple of 64.
+    uint32_t u[4 * K];
+    {
+        float4 x[K];
 #pragma unroll
-    for (int i = 0; i < K; ++i) {
-        const int t = lo + i * kSelThreads + tid;
-        u[i] = t < hi ? order_of(w[t]) : 0;
+        for (int i = 0; i < K; ++i) x[i] = *reinterpret_cast<const float4 *>(w + min(4 * (i * kRegThreads + tid), a.from.t_capacity - 4));
+#pragma unroll
+        for (int i = 0; i < K; ++i) asm volatile("" : "+v"(x[i].x), "+v"(x[i].y), "+v"(x[i].z), "+v"(x[i].w));
+#pragma unroll
+        for (int i = 0; i < K; ++i) {
+            const float y[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int t = 4 * (i * kRegThreads + tid) + j;
+                u[4 * i + j] = t >= lo && t < hi ? order_of(y[j]) : 0;
+            }
+        }
     }
+    if (tid == 0) sm_n_left = 0;
     keep_ends(a, kept, hi);
     if (need == 0) return;
     uint32_t floor = 0;   // kept: above it, and the first of those equal to it
-    bool exact = false;
-    for (int bit = 31; bit >= 0 && !exact; --bit) {
+    uint32_t n_floor = hi - lo, n_certain = 0;   // that reach the floor; that reach the lowest bound found too high
+    bool exact = false, ranked = false;   // exact: all that reach the floor are kept
+    for (int bit = 31; bit >= 0 && !exact && !ranked; --bit) {
         const uint32_t to = floor | (1u << bit);
-        uint32_t mine = 0;
+        uint32_t some[4] = {0, 0, 0, 0};
 #pragma unroll
-        for (int i = 0; i < K; ++i) mine += __popcll(__ballot(u[i] >= to));
-        if (lane == 0) sm_count[bit & 1][wave] = mine;
+        for (int i = 0; i < 4 * K; ++i) some[i & 3] += u[i] >= to;
+        const float of_row[1] = {row_sum((float)(some[0] + some[1] + some[2] + some[3]))};   // (whole numbers below 2^24)
+        const float of_wave = fold_rows(of_row, AddF());
+        if (lane == 0) sm_count[bit & 1][wave] = of_wave;
         __syncthreads();   // (the other half is free: every wave is past the pass that read it)
-        uint32_t all = 0;
+        float sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < kSelWaves; ++i) all += sm_count[bit & 1][i];
-        if (all >= need) floor = to;
+        for (int i = 0; i < kRegWaves; ++i) sum += sm_count[bit & 1][i];
+        const uint32_t all = __builtin_amdgcn_readfirstlane((uint32_t)sum);
+        if (all >= need) {
+            floor = to;
+            n_floor = all;
+        } else {
+            n_certain = all;
+        }
         exact = all == need;
+        ranked = !exact && floor > 0 && bit > 0 && n_floor - n_certain <= kRanked;
+        if (ranked) {
+            // those in [floor, floor + 2^bit)
+            const uint32_t span = 1u << bit;
+#pragma unroll
+            for (int i = 0; i < 4 * K; ++i)
+                if (u[i] - floor < span) sm_left[atomicAdd(&sm_n_left, 1u)] = u[i];
+            __syncthreads();
+            const int n_left = n_floor - n_certain;
+            const uint32_t wanted = need - n_certain;
+            if (wave == 0) {
+                const uint32_t v = sm_left[lane];
+                uint32_t over = 0, same = 0;
+                for (int i = 0; i < n_left; ++i) {   // (lanes past them have whatever is there)
+                    const uint32_t other = (uint32_t)__builtin_amdgcn_readlane((int)v, i);
+                    over += other > v;
+                    same += other == v;
+                }
+                if (lane < n_left && over < wanted && wanted <= over + same) {   // whoever has this value writes the same
+                    sm_floor = v;
+                    sm_ties = over + same != wanted;
+                }
+            }
+            __syncthreads();
+            floor = __builtin_amdgcn_readfirstlane(sm_floor);
+            exact = __builtin_amdgcn_readfirstlane(sm_ties) == 0;
+        }
     }
-    if (exact) floor -= 1;   // `need` of them reach it: all are above this, and no equal ones are taken
-    // places in the order of the tokens
-    uint64_t above[K], equal[K];
+    // Places in the order of the tokens: how many of every four neighbours of a wave are above (with `exact`: reach the floor) or equal, sums of
+    // these, then the lanes' own.
+    const uint32_t above_at = exact ? floor : floor + 1;   // (a floor of 0xffffffff would be a NaN's, which is 0)
+    const auto is_equal = [&](int i) {
+        const int t = 4 * ((i >> 2) * kRegThreads + tid) + (i & 3);
+        return u[i] == floor && t >= lo && t < hi;
+    };
 #pragma unroll
     for (int i = 0; i < K; ++i) {
-        const bool here = lo + i * kSelThreads + tid < hi;
-        above[i] = __ballot(here && u[i] > floor);
-        equal[i] = __ballot(here && !exact && u[i] == floor);
+        uint32_t n = 0, m = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) n += __popcll(__ballot(u[4 * i + j] >= above_at));
+        if (!exact)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) m += __popcll(__ballot(is_equal(4 * i + j)));
         if (lane == 0) {
-            sm_above[i * kSelWaves + wave] = __popcll(above[i]);
-            sm_equal[i * kSelWaves + wave] = __popcll(equal[i]);
+            sm_above[i * kRegWaves + wave] = n;
+            sm_equal[i * kRegWaves + wave] = m;
         }
     }
     __syncthreads();
-    if (wave == 0) {   // exclusive sums, K * kSelWaves / 64 neighbours per lane
-        constexpr int kPer = K * kSelWaves / 64;
+    if (wave == 0) {   // exclusive sums; K * kRegWaves are 16, 64 or 128 of them
+        constexpr int kAll = K * kRegWaves, kPer = (kAll + 63) / 64;
         uint32_t x[kPer], y[kPer], sx = 0, sy = 0;
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             x[i] = sx;
             y[i] = sy;
-            sx += sm_above[lane * kPer + i];
-            sy += sm_equal[lane * kPer + i];
+            if (lane * kPer + i < kAll) {
+                sx += sm_above[lane * kPer + i];
+                sy += sm_equal[lane * kPer + i];
+            }
         }
         uint32_t ex = sx, ey = sy;
         for (int o = 1; o < 64; o <<= 1) {
@@ -97,20 +164,37 @@ __global__ __launch_bounds__(kSelThreads) void fp8_select_kernel(Fp8EvictArgs a)
             }
         }
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            sm_above[lane * kPer + i] = ex - sx + x[i];
-            sm_equal[lane * kPer + i] = ey - sy + y[i];
-        }
-        if (lane == 63) sm_count[0][0] = ex;
+        for (int i = 0; i < kPer; ++i)
+            if (lane * kPer + i < kAll) {
+                sm_above[lane * kPer + i] = ex - sx + x[i];
+                sm_equal[lane * kPer + i] = ey - sy + y[i];
+            }
+        if (lane == 63) sm_all_above = ex;
     }
     __syncthreads();
-    need -= sm_count[0][0];   // of the equal ones
-    const uint64_t below = (1ull << lane) - 1;
+    need -= sm_all_above;   // of the equal ones
 #pragma unroll
     for (int i = 0; i < K; ++i) {
-        const uint32_t n_above = sm_above[i * kSelWaves + wave] + __popcll(above[i] & below), n_equal = sm_equal[i * kSelWaves + wave] + __popcll(equal[i] & below);
-        const bool gt = (above[i] >> lane) & 1, eq = (equal[i] >> lane) & 1;
-        if (gt || (eq && n_equal < need)) kept[lo + n_above + min(n_equal, need)] = lo + i * kSelThreads + tid;
+        const int t = 4 * (i * kRegThreads + tid);
+        uint32_t n = sm_above[i * kRegWaves + wave];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) n += below_lane(__ballot(u[4 * i + j] >= above_at));
+        if (exact) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (u[4 * i + j] >= above_at) kept[lo + n++] = t + j;
+        } else {
+            uint32_t m = sm_equal[i * kRegWaves + wave];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) m += below_lane(__ballot(is_equal(4 * i + j)));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const bool gt = u[4 * i + j] >= above_at, eq = is_equal(4 * i + j);
+                if (gt || (eq && m < need)) kept[lo + n + min(m, need)] = t + j;
+                n += gt;
+                m += eq;
+            }
+        }
     }
 }
 
@@ -236,7 +320,7 @@ __device__ __forceinline__ uint4 rescaled(const uint4 &v, int shift)
 }
 
 // K and V of a block together: where their tokens are is looked up once, and twice as much is on its way (of 256 streams of 1024 tokens
-// kept 38.5 us with a workgroup each, MM with this).
+// kept 38.5 us with a workgroup each, 33 with this).
 template <int D, int B>
 __global__ __launch_bounds__(kMoveThreads) void fp8_move_kernel(Fp8EvictArgs a)
 {
@@ -324,11 +408,11 @@ hipError_t launch_fp8_evict(const Fp8EvictArgs &a, hipStream_t s)
 {
     const int N = a.n_seq * a.from.n_kv_heads, B = 1 << a.from.log_block;
     // what a sequence can have to choose from, by the cache's capacity
-    const int64_t most = (int64_t)a.from.t_capacity - a.keep_first - a.keep_last;
+    const int64_t most = (int64_t)a.from.t_capacity - a.keep_last;
     if (a.budget < a.from.t_capacity) {
-        if (most <= 4 * kSelThreads) fp8_select_kernel<4><<<N, kSelThreads, 0, s>>>(a);
-        else if (most <= 16 * kSelThreads) fp8_select_kernel<16><<<N, kSelThreads, 0, s>>>(a);
-        else if (most <= 32 * kSelThreads) fp8_select_kernel<32><<<N, kSelThreads, 0, s>>>(a);
+        if (most <= 4096) fp8_select_kernel<1024 / kRegThreads><<<N, kRegThreads, 0, s>>>(a);
+        else if (most <= 16384) fp8_select_kernel<4096 / kRegThreads><<<N, kRegThreads, 0, s>>>(a);
+        else if (most <= 32768) fp8_select_kernel<8192 / kRegThreads><<<N, kRegThreads, 0, s>>>(a);
         else fp8_select_long_kernel<<<N, kSelThreads, 0, s>>>(a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
