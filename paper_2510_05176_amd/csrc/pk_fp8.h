@@ -61,8 +61,9 @@ struct Fp8WeightsArgs {
     Fp8Queries in;
     const float *lse;
     int32_t accumulate, bound;
+    int32_t parts;            // as for the attention (set by the launch)
 };
-hipError_t launch_fp8_weights(const Fp8WeightsArgs &a, hipStream_t s);
+hipError_t launch_fp8_weights(Fp8WeightsArgs &a, hipStream_t s);
 
 struct Fp8EvictArgs {
     Fp8View from, to;

@@ -244,6 +244,7 @@ pk_status pk_fp8_weights(const pk_fp8_config *cfg, const pk_fp8_cache *cache, co
     a.lse = lse;
     a.accumulate = accumulate != 0;
     a.bound = bound;
+    a.parts = 0;
     return launch_fp8_weights(a, static_cast<hipStream_t>(stream)) == hipSuccess ? PK_OK : PK_ERR_DEVICE;
 }
 

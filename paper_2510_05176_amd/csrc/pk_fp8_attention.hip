@@ -279,7 +279,8 @@ __device__ __forceinline__ int first_visible(const Fp8Queries &a, int len, int c
 {
     return a.window > 0 ? (int)min(max((int64_t)len - count + 1 - a.window, (int64_t)0), (int64_t)len) & ~63 : 0;
 }
-// Ends of the sequences' units, lane's sequences 64 i + lane; returns all of them.
+// Ends of the sequences' units (of the visible tokens, or of all), lane's sequences 64 i + lane; returns all of them.
+template <bool VISIBLE>
 __device__ __forceinline__ int ends_of(const Fp8Queries &a, int (&end)[kMostSeqs / 64])
 {
     const int lane = threadIdx.x & 63;
@@ -291,8 +292,13 @@ __device__ __forceinline__ int ends_of(const Fp8Queries &a, int (&end)[kMostSeqs
         const int seq = 64 * i + lane;
         int units = 0;
         if (seq < a.n_seq) {
-            const int len = fp8_state(a.states, seq, a.c.t_capacity).x, count = fp8_count(a.counts, seq, a.n_query);
-            units = count > 0 ? max((len - first_visible(a, len, count) + 63) >> 6, 1) : 1;
+            const int len = fp8_state(a.states, seq, a.c.t_capacity).x;
+            if constexpr (VISIBLE) {
+                const int count = fp8_count(a.counts, seq, a.n_query);
+                units = count > 0 ? max((len - first_visible(a, len, count) + 63) >> 6, 1) : 1;
+            } else {
+                units = max((len + 63) >> 6, 1);
+            }
         }
         for (int o = 1; o < min(a.n_seq, 64); o <<= 1) {
             const int v = __shfl_up(units, o);
@@ -304,6 +310,33 @@ __device__ __forceinline__ int ends_of(const Fp8Queries &a, int (&end)[kMostSeqs
     return before;
 }
 __device__ __forceinline__ int run_length(int all, int parts) { return max((all + parts - 1) / parts, kLeastUnits); }
+
+struct Run {
+    int seq, seq_from;   // the sequence that the run begins in, and where its units begin
+    int at, stop;        // the run's units
+    int per;
+};
+// All waves of the workgroup; false: the run has nothing.  sm_end: kMostSeqs ends for the workgroup.
+template <bool VISIBLE>
+__device__ __forceinline__ bool find_run(const Fp8Queries &a, int parts, int run, int *sm_end, Run &r)
+{
+    const int lane = threadIdx.x & 63;
+    int end[kMostSeqs / 64];
+    const int all = __builtin_amdgcn_readfirstlane(ends_of<VISIBLE>(a, end));
+    r.per = run_length(all, parts);
+    r.at = run * r.per;
+    r.stop = min(r.at + r.per, all);
+    if (r.at >= r.stop) return false;
+#pragma unroll
+    for (int i = kMostSeqs / 64 - 1; i >= 0; --i) {
+        if (64 * i + lane < a.n_seq && threadIdx.x < 64) sm_end[64 * i + lane] = end[i];
+        const uint64_t behind = __ballot(64 * i + lane < a.n_seq && end[i] > r.at);
+        if (behind) r.seq = 64 * i + __ffsll((unsigned long long)behind) - 1;
+    }
+    __syncthreads();
+    r.seq_from = r.seq > 0 ? __builtin_amdgcn_readfirstlane(sm_end[r.seq - 1]) : 0;
+    return true;
+}
 
 template <int D>
 __device__ __forceinline__ void store_row(const Fp8AttentionArgs &a, const Place &p, int row, int c, const float *x, int n)
@@ -332,23 +365,10 @@ __global__ __launch_bounds__(64 * NW, 2) void fp8_attention_kernel(Fp8AttentionA
     const int kvh = blockIdx.x % hkv, rest = blockIdx.x / hkv;
     const int group = rest % a.groups, run = rest / a.groups;
     __shared__ int sm_end[kMostSeqs];
-    int seq = run, seq_from = 0, seq_to = 0, at_unit = 0, stop = 0, per = 0;
-    if (a.parts > 0) {
-        int end[kMostSeqs / 64];
-        const int all = __builtin_amdgcn_readfirstlane(ends_of(a.in, end));
-        per = run_length(all, a.parts);
-        at_unit = run * per;
-        stop = min(at_unit + per, all);
-        if (at_unit >= stop) return;
-#pragma unroll
-        for (int i = kMostSeqs / 64 - 1; i >= 0; --i) {
-            if (64 * i + lane < a.in.n_seq && wave == 0) sm_end[64 * i + lane] = end[i];
-            const uint64_t behind = __ballot(64 * i + lane < a.in.n_seq && end[i] > at_unit);
-            if (behind) seq = 64 * i + __ffsll((unsigned long long)behind) - 1;
-        }
-        __syncthreads();
-        seq_from = seq > 0 ? __builtin_amdgcn_readfirstlane(sm_end[seq - 1]) : 0;
-    }
+    Run deal = {run, 0, 0, 0, 0};
+    if (a.parts > 0 && !find_run<true>(a.in, a.parts, run, sm_end, deal)) return;
+    int seq = deal.seq, seq_from = deal.seq_from, seq_to = 0;
+    const int at_unit = deal.at, stop = deal.stop;
     for (;; seq_from = seq_to, ++seq) {   // the pieces of the run
     if (a.parts > 0) seq_to = __builtin_amdgcn_readfirstlane(sm_end[seq]);
     const bool whole = a.parts == 0 || (at_unit <= seq_from && seq_to <= stop);   // the sequence is this piece
@@ -682,7 +702,7 @@ __global__ __launch_bounds__(64 * kMergeRows) void fp8_merge_kernel(Fp8Attention
     const int kvh = blockIdx.x % hkv, rest = blockIdx.x / hkv, row = rest % groups * kMergeRows + wave, seq = rest / groups;
     const Place p = place_of<false>(a.in, seq * hkv + kvh);   // (requested before the rest)
     int end[kMostSeqs / 64], from = 0, to = 0;
-    const int all = __builtin_amdgcn_readfirstlane(ends_of(a.in, end)), per = run_length(all, a.parts);
+    const int all = __builtin_amdgcn_readfirstlane(ends_of<true>(a.in, end)), per = run_length(all, a.parts);
 #pragma unroll
     for (int i = 0; i < kMostSeqs / 64; ++i) {
         const int before = __shfl(end[i], (seq - 1) & 63), here = __shfl(end[i], seq & 63);
@@ -744,111 +764,162 @@ __global__ __launch_bounds__(64 * kMergeRows) void fp8_merge_kernel(Fp8Attention
 // Query operands of up to this many tiles of 16 rows in LDS at a time: 32 KB at 128 channels, 64 at 256
 constexpr int kWeightTiles = 8;
 
+// exp(s - lse) as 2^(x f - l) where no option changes the score x f: f takes |scale| * log2 e in, rounded once, and l is lse times the very
+// factor that this makes of log2 e, so that the rounding costs only where s and lse differ.
+__device__ __forceinline__ float scale2_of(float scale) { return fabsf(scale) * kLog2e; }
+__device__ __forceinline__ double log2e_of(float scale)
+{
+    const double s = fabs((double)scale), s2 = (double)scale2_of(scale);
+    return s > 0.0 && s2 > 0.0 && s2 < 3e38 ? s2 / s : 1.4426950408889634;
+}
+
 // A wave takes 64 tokens at a time, their K operands in registers, against the rows in LDS; the sums over rows stay in registers
 // until all tiles are done.  More rows than fit go in rounds that add to what the first wrote, each token in the same lane.
 template <int D, bool OPT>
-__global__ __launch_bounds__(kThreads, 2) void fp8_weights_kernel(Fp8WeightsArgs a, int ranges)
+__global__ __launch_bounds__(kThreads, 2) void fp8_weights_kernel(Fp8WeightsArgs a)
 {
     using S = Shape<D>;
     __shared__ half8v sm_q[kWeightTiles][S::kSteps][64];
     __shared__ Row sm_row[kWeightTiles * 16];
     __shared__ float sm_lse[kWeightTiles * 16];
+    __shared__ int sm_last[kWeightTiles];   // the first row of a tile that sees least
+    __shared__ int sm_end[kMostSeqs];
     const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int N = a.in.n_seq * a.in.c.n_kv_heads;
-    const int range = blockIdx.x / N;
-    const Place p = place_of<true>(a.in, blockIdx.x - range * N);
-    const int rows = p.count * a.in.r;
-    const int per = ((p.len + ranges - 1) / ranges + 63) & ~63;
-    const int from = (int)min((int64_t)range * per, (int64_t)p.len), to = min(from + per, p.len);
-    if (from >= to) return;
-    const int32_t *pos = OPT && (a.in.slopes || a.in.window > 0) ? a.in.c.pos + (int64_t)p.stream * a.in.c.t_capacity : nullptr;
-    float *weight = a.in.c.weight + (int64_t)p.stream * a.in.c.t_capacity;
+    const int hkv = a.in.c.n_kv_heads, run = blockIdx.x / hkv, kvh = blockIdx.x - run * hkv;
     const uint32_t k_off = n * D + g * (D / 4);
-    const StreamMap map = a.in.c.map.of(p.stream);
-    for (int first = 0; first < max(rows, 1); first += 16 * kWeightTiles) {
-        const int tiles = (min(rows - first, 16 * kWeightTiles) + 15) / 16;
-        if (first > 0) __syncthreads();
-        for (int tile = wave; tile < tiles; tile += kWaves) {
-            const int at = first + 16 * tile + n;
-            half8v qf[S::kSteps];
-            Row row = row_of(a.in, p, at);
-            load_query<D>(qf, row.factor, a.in, p.seq, p.kvh, at, at < rows, g);
+    const float scale2 = scale2_of(a.in.scale);
+    const double to_log2 = log2e_of(a.in.scale);
+    Run deal = {run, 0, 0, 0, 0};
+    if (a.parts > 0 && !find_run<false>(a.in, a.parts, run, sm_end, deal)) return;
+    int seq = deal.seq, seq_from = deal.seq_from, seq_to = 0;
+    for (;; seq_from = seq_to, ++seq) {   // the pieces of the run
+        const Place p = place_of<true>(a.in, seq * hkv + kvh);
+        const int rows = p.count * a.in.r;
+        int from = 0, to = p.len;
+        if (a.parts > 0) {
+            seq_to = __builtin_amdgcn_readfirstlane(sm_end[seq]);
+            from = (max(deal.at, seq_from) - seq_from) * 64;
+            to = (int)min((int64_t)(min(deal.stop, seq_to) - seq_from) * 64, (int64_t)to);
+        }
+        const int32_t *pos = OPT && (a.in.slopes || a.in.window > 0) ? a.in.c.pos + (int64_t)p.stream * a.in.c.t_capacity : nullptr;
+        float *weight = a.in.c.weight + (int64_t)p.stream * a.in.c.t_capacity;
+        const StreamMap map = a.in.c.map.of(p.stream);
+        for (int first = 0; first < max(rows, 1); first += 16 * kWeightTiles) {
+            const int tiles = (min(rows - first, 16 * kWeightTiles) + 15) / 16;
+            __syncthreads();   // the last round's rows are not needed any more
+            for (int tile = wave; tile < tiles; tile += kWaves) {
+                const int at = first + 16 * tile + n;
+                half8v qf[S::kSteps];
+                Row row = row_of(a.in, p, at);
+                load_query<D>(qf, row.factor, a.in, p.seq, p.kvh, at, at < rows, g);
 #pragma unroll
-            for (int s = 0; s < S::kSteps; ++s) sm_q[tile][s][lane] = qf[s];
-            if (g == 0) {
+                for (int s = 0; s < S::kSteps; ++s) sm_q[tile][s][lane] = qf[s];
                 const int i = at / a.in.r, h = at - i * a.in.r;
-                float lse = at < rows ? a.lse[((int64_t)p.seq * a.in.c.n_kv_heads * a.in.r + p.kvh * a.in.r + h) * a.in.n_query + i] : INFINITY;
+                float lse = INFINITY;
+                if (at < rows) lse = a.lse[((int64_t)p.seq * hkv * a.in.r + p.kvh * a.in.r + h) * a.in.n_query + i];
                 if (lse == -INFINITY) {   // a row that saw nothing adds nothing
                     lse = INFINITY;
                     row.last = -1;
                 }
-                sm_lse[16 * tile + n] = lse;
-                sm_row[16 * tile + n] = row;
+                if constexpr (!OPT) {
+                    row.factor *= scale2;
+                    lse = (float)((double)lse * to_log2);
+                }
+                int least = row.last;
+                for (int o = 1; o < 16; o <<= 1) least = min(least, __shfl_xor(least, o));
+                if (g == 0) {
+                    sm_lse[16 * tile + n] = lse;
+                    sm_row[16 * tile + n] = row;
+                }
+                if (lane == 0) sm_last[tile] = least;
             }
-        }
-        __syncthreads();
-        int lo, hi;
-        key_range(a.in, p, first, min(first + 16 * kWeightTiles, rows) - 1, lo, hi);
-        for (int t0 = from + 64 * wave; t0 < to; t0 += 64 * kWaves) {
-            float sum[16];
+            __syncthreads();
+            int lo, hi;
+            key_range(a.in, p, first, min(first + 16 * kWeightTiles, rows) - 1, lo, hi);
+            for (int t0 = from + 64 * wave; t0 < to; t0 += 64 * kWaves) {
+                float sum[16];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) sum[i] = 0.f;
-            if (rows > 0 && t0 < hi && t0 + 64 > lo) {
-                const int64_t at = map.pos(t0);
-                uint32_t kw[4][S::kKWords];
+                for (int i = 0; i < 16; ++i) sum[i] = 0.f;
+                if (rows > 0 && t0 < hi && t0 + 64 > lo) {
+                    const int64_t at = map.pos(t0);
+                    uint32_t kw[4][S::kKWords];
 #pragma unroll
-                for (int j = 0; j < 4; ++j) load_k<D>(kw[j], a.in.c.k_codes + at * D + 16 * j * D, k_off);
-                const float ks[2] = {fabsf(scalar_load(a.in.c.k_scale + (at >> a.in.c.log_block))), fabsf(scalar_load(a.in.c.k_scale + ((at + 32) >> a.in.c.log_block)))};
-                half8v kf[4][S::kSteps];
+                    for (int j = 0; j < 4; ++j) load_k<D>(kw[j], a.in.c.k_codes + at * D + 16 * j * D, k_off);
+                    const float ks[2] = {fabsf(scalar_load(a.in.c.k_scale + (at >> a.in.c.log_block))), fabsf(scalar_load(a.in.c.k_scale + ((at + 32) >> a.in.c.log_block)))};
+                    half8v kf[4][S::kSteps];
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
+                    for (int j = 0; j < 4; ++j)
 #pragma unroll
-                    for (int s = 0; s < S::kSteps; ++s) kf[j][s] = k_operand<D>(kw[j], s);
-                for (int tile = 0; tile < tiles; ++tile) {
-                    const Row row = sm_row[16 * tile + n];
-                    const float lse = sm_lse[16 * tile + n];
-                    float4v x[4];
+                        for (int s = 0; s < S::kSteps; ++s) kf[j][s] = k_operand<D>(kw[j], s);
+                    // a tile's operands and factors are read from LDS while the last one's exponentials run
+                    half8v q[S::kSteps];
+                    float next_lse, next_c;
+                    int next_last;
+                    const auto read_tile = [&](int tile) {
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) x[j] = float4v{0.f, 0.f, 0.f, 0.f};
+                        for (int s = 0; s < S::kSteps; ++s) q[s] = sm_q[tile][s][lane];
+                        next_lse = sm_lse[16 * tile + n];
+                        next_c = sm_row[16 * tile + n].factor;
+                        next_last = sm_last[tile];
+                    };
+                    read_tile(0);
+                    for (int tile = 0; tile < tiles; ++tile) {
+                        float4v x[4];
 #pragma unroll
-                    for (int s = 0; s < S::kSteps; ++s) {
-                        const half8v q = sm_q[tile][s][lane];
+                        for (int j = 0; j < 4; ++j) x[j] = float4v{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                        for (int j = 0; j < 4; ++j) x[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[j][s], q, x[j], 0, 0, 0);
+                        for (int s = 0; s < S::kSteps; ++s)
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) x[j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kf[j][s], q[s], x[j], 0, 0, 0);
+                        const float lse = next_lse, c = next_c;
+                        const bool edge = t0 + 63 > __builtin_amdgcn_readfirstlane(next_last);
+                        read_tile(min(tile + 1, tiles - 1));
+                        float y[16], f[2];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) y[i] = x[i >> 2][i & 3];
+                        if constexpr (OPT) {
+                            const Row row = sm_row[16 * tile + n];
+                            to_scores<true>(y, f, ks, a.in, 1.f, row, t0 + 4 * g, pos, edge, a.in.window > 0);
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) sum[i] += exp2_((y[i] - lse) * kLog2e);
+                        } else {
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) f[h] = fmaxf(ks[h] * c, 0x1p-126f);
+                            if (edge) {
+                                const int last = sm_row[16 * tile + n].last;
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) y[i] = t0 + 4 * g + 16 * (i >> 2) + (i & 3) <= last ? y[i] : -INFINITY;
+                            }
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) sum[i] += exp2_(fmaf(y[i], f[i >> 3], -lse));
+                        }
                     }
-                    const bool edge = __any(t0 + 63 > row.last);
-                    const bool windowed = OPT && a.in.window > 0;
-                    float y[16], f[2];
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) y[i] = x[i >> 2][i & 3];
-                    to_scores<OPT>(y, f, ks, a.in, 1.f, row, t0 + 4 * g, pos, edge, windowed);
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) sum[i] += exp2_(fmaf(y[i], f[i >> 3], -lse) * kLog2e);
                 }
-            }
 #pragma unroll
-            for (int i = 0; i < 16; ++i) sum[i] = row_sum(sum[i]);
-            if (n < 4) {   // lane 16 g + n writes tokens 16 n + 4 g .. + 3
-                float4 v;
-                v.x = n == 0 ? sum[0] : n == 1 ? sum[4] : n == 2 ? sum[8] : sum[12];
-                v.y = n == 0 ? sum[1] : n == 1 ? sum[5] : n == 2 ? sum[9] : sum[13];
-                v.z = n == 0 ? sum[2] : n == 1 ? sum[6] : n == 2 ? sum[10] : sum[14];
-                v.w = n == 0 ? sum[3] : n == 1 ? sum[7] : n == 2 ? sum[11] : sum[15];
-                const int t = t0 + 16 * n + 4 * g;
-                float *w = weight + t;
-                const bool add = a.accumulate || first > 0;
-                if (t + 3 < to) {
-                    float4 old = make_float4(0.f, 0.f, 0.f, 0.f);
-                    if (add) old = *reinterpret_cast<const float4 *>(w);
-                    *reinterpret_cast<float4 *>(w) = make_float4(old.x + v.x, old.y + v.y, old.z + v.z, old.w + v.w);
-                } else {
-                    const float y[4] = {v.x, v.y, v.z, v.w};
-                    for (int i = 0; i < 4; ++i)
-                        if (t + i < to) w[i] = (add ? w[i] : 0.f) + y[i];
+                for (int i = 0; i < 16; ++i) sum[i] = row_sum(sum[i]);
+                if (n < 4) {   // lane 16 g + n writes tokens 16 n + 4 g .. + 3
+                    float4 v;
+                    v.x = n == 0 ? sum[0] : n == 1 ? sum[4] : n == 2 ? sum[8] : sum[12];
+                    v.y = n == 0 ? sum[1] : n == 1 ? sum[5] : n == 2 ? sum[9] : sum[13];
+                    v.z = n == 0 ? sum[2] : n == 1 ? sum[6] : n == 2 ? sum[10] : sum[14];
+                    v.w = n == 0 ? sum[3] : n == 1 ? sum[7] : n == 2 ? sum[11] : sum[15];
+                    const int t = t0 + 16 * n + 4 * g;
+                    float *w = weight + t;
+                    const bool add = a.accumulate || first > 0;
+                    if (t + 3 < to) {
+                        float4 old = make_float4(0.f, 0.f, 0.f, 0.f);
+                        if (add) old = *reinterpret_cast<const float4 *>(w);
+                        *reinterpret_cast<float4 *>(w) = make_float4(old.x + v.x, old.y + v.y, old.z + v.z, old.w + v.w);
+                    } else {
+                        const float y[4] = {v.x, v.y, v.z, v.w};
+                        for (int i = 0; i < 4; ++i)
+                            if (t + i < to) w[i] = (add ? w[i] : 0.f) + y[i];
+                    }
                 }
             }
         }
+        if (a.parts == 0 || seq_to >= deal.stop) break;
     }
 }
 
@@ -907,14 +978,19 @@ hipError_t launch_d(Fp8AttentionArgs &a, hipStream_t s)
     return hipGetLastError();
 }
 
+#ifndef WT
+#define WT 512
+#endif
 template <int D>
-hipError_t launch_weights_d(const Fp8WeightsArgs &a, hipStream_t s)
+hipError_t launch_weights_d(Fp8WeightsArgs &a, hipStream_t s)
 {
-    const int64_t N = (int64_t)a.in.n_seq * a.in.c.n_kv_heads;
-    const int64_t most = ((int64_t)a.bound + 64 * kWaves - 1) / (64 * kWaves), want = (1024 + N - 1) / N;
-    const int ranges = (int)(most < want ? (most < 1 ? 1 : most) : want);
-    if (a.in.cap > 0.f || a.in.slopes || a.in.window > 0) fp8_weights_kernel<D, true><<<(uint32_t)(N * ranges), kThreads, 0, s>>>(a, ranges);
-    else fp8_weights_kernel<D, false><<<(uint32_t)(N * ranges), kThreads, 0, s>>>(a, ranges);
+    const int64_t units = (int64_t)a.in.n_seq * ((a.bound + 63) / 64), hkv = a.in.c.n_kv_heads;
+    int64_t parts = WT / hkv < 1 ? 1 : WT / hkv;
+    if (parts * kLeastUnits > units) parts = (units + kLeastUnits - 1) / kLeastUnits;
+    a.parts = a.in.n_seq > kMostSeqs || a.in.n_seq >= 4 * parts || parts <= 1 ? 0 : (int)parts;
+    const uint32_t grid = (uint32_t)((a.parts > 0 ? a.parts : a.in.n_seq) * hkv);
+    if (a.in.cap > 0.f || a.in.slopes || a.in.window > 0) fp8_weights_kernel<D, true><<<grid, kThreads, 0, s>>>(a);
+    else fp8_weights_kernel<D, false><<<grid, kThreads, 0, s>>>(a);
     return hipGetLastError();
 }
 
@@ -937,7 +1013,7 @@ hipError_t launch_fp8_attention(Fp8AttentionArgs &a, hipStream_t s)
     return a.in.d == 64 ? launch_d<64>(a, s) : a.in.d == 96 ? launch_d<96>(a, s) : a.in.d == 128 ? launch_d<128>(a, s) : launch_d<256>(a, s);
 }
 
-hipError_t launch_fp8_weights(const Fp8WeightsArgs &a, hipStream_t s)
+hipError_t launch_fp8_weights(Fp8WeightsArgs &a, hipStream_t s)
 {
     return a.in.d == 64    ? launch_weights_d<64>(a, s)
            : a.in.d == 96  ? launch_weights_d<96>(a, s)
