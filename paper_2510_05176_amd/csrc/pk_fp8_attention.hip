@@ -18,33 +18,44 @@ constexpr int kWaves = 4, kThreads = 64 * kWaves;
 
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// tanh in binary32, of N values.  Below 0.55 the odd Taylor series (the first term left out is 4e-8 of the result at 0.55), above it
-// 1 - 2 / (e^{2x} + 1), whose rounding is no longer magnified there; a wave without such a value does not compute it.
-template <int N>
-__device__ __forceinline__ void tanh_all(float (&x)[N])
+// x[i] = m * tanh(x[i] * c[i / 8]) in binary32.  Below 0.55 the odd Taylor series, above it 1 - 2 / (e^{2y} + 1), whose rounding is no longer
+// magnified there; how far the series goes, and whether the other form is computed at all, is the wave's largest argument's to say (the first term
+// left out is 2e-9 of the result at 0.25 and 4e-8 at 0.55).  tanh y = y + y^3 s(y^2), s from 2^(2k) (2^(2k) - 1) B_2k / (2k)!.
+__device__ __forceinline__ void capped(float (&x)[16], const float (&c)[2], float m)
 {
     float most = 0.f;
 #pragma unroll
-    for (int i = 0; i < N; ++i) most = fmaxf(most, fabsf(x[i]));   // (a NaN does not count and comes out of the series as one)
+    for (int i = 0; i < 16; ++i) most = fmaxf(most, fabsf(x[i]) * c[i >> 3]);   // (a NaN does not count and comes out of the series as one)
+    if (!__any(most >= 0.25f)) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const float y = x[i] * c[i >> 3], y2 = y * y;
+            float s = fmaf(-1382.f / 155925.f, y2, 62.f / 2835.f);
+            s = fmaf(s, y2, -17.f / 315.f);
+            s = fmaf(s, y2, 2.f / 15.f);
+            s = fmaf(s, y2, -1.f / 3.f);
+            const float ym = y * m;
+            x[i] = fmaf(s * y2, ym, ym);
+        }
+        return;
+    }
     const bool far = __any(most >= 0.55f);
 #pragma unroll
-    for (int i = 0; i < N; ++i) {
-        const float y = x[i] * x[i];
-        // coefficients of x^3, x^5, ...: 2^(2k) (2^(2k) - 1) B_2k / (2k)!
-        float s = -929569.f / 638512875.f;
-        s = fmaf(s, y, 21844.f / 6081075.f);
-        s = fmaf(s, y, -1382.f / 155925.f);
-        s = fmaf(s, y, 62.f / 2835.f);
-        s = fmaf(s, y, -17.f / 315.f);
-        s = fmaf(s, y, 2.f / 15.f);
-        s = fmaf(s, y, -1.f / 3.f);
-        float t = fmaf(s * y, x[i], x[i]);
+    for (int i = 0; i < 16; ++i) {
+        const float y = x[i] * c[i >> 3], y2 = y * y;
+        float s = fmaf(-929569.f / 638512875.f, y2, 21844.f / 6081075.f);
+        s = fmaf(s, y2, -1382.f / 155925.f);
+        s = fmaf(s, y2, 62.f / 2835.f);
+        s = fmaf(s, y2, -17.f / 315.f);
+        s = fmaf(s, y2, 2.f / 15.f);
+        s = fmaf(s, y2, -1.f / 3.f);
+        float t = fmaf(s * y2, y, y);
         if (far) {
-            const float a = fabsf(x[i]), e = exp2_(fminf(a, 16.f) * (2.f * kLog2e));
-            const float big = copysignf(1.f - 2.f * __builtin_amdgcn_rcpf(e + 1.f), x[i]);
+            const float a = fabsf(y), e = exp2_(fminf(a, 16.f) * (2.f * kLog2e));
+            const float big = copysignf(1.f - 2.f * __builtin_amdgcn_rcpf(e + 1.f), y);
             t = a >= 0.55f ? big : t;
         }
-        x[i] = t;
+        x[i] = t * m;
     }
 }
 
@@ -198,11 +209,9 @@ __device__ __forceinline__ void to_scores(float (&x)[16], float (&f)[2], const f
     if constexpr (OPT) {
         if (a.cap > 0.f) {
             const float inv = 1.f / a.cap;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) x[i] *= f[i >> 3] * inv;
-            tanh_all(x);
-#pragma unroll
-            for (int i = 0; i < 16; ++i) x[i] *= a.cap * post;
+            f[0] *= inv;
+            f[1] *= inv;
+            capped(x, f, a.cap * post);
         } else {
 #pragma unroll
             for (int i = 0; i < 16; ++i) x[i] *= f[i >> 3] * post;
@@ -696,7 +705,7 @@ constexpr int kMergeRows = 4;
 template <int D>
 __global__ __launch_bounds__(64 * kMergeRows) void fp8_merge_kernel(Fp8AttentionArgs a)
 {
-    constexpr int kPer = D <= 128 ? 2 : 4;   // channels per lane
+    constexpr int kPer = D <= 128 ? 2 : 4, kTogether = 4;   // channels per lane, pieces whose loads are on their way together
     const int rows = a.in.r * a.in.n_query, hkv = a.in.c.n_kv_heads, groups = (rows + kMergeRows - 1) / kMergeRows;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int kvh = blockIdx.x % hkv, rest = blockIdx.x / hkv, row = rest % groups * kMergeRows + wave, seq = rest / groups;
@@ -735,20 +744,29 @@ __global__ __launch_bounds__(64 * kMergeRows) void fp8_merge_kernel(Fp8Attention
         const float sum_of_row[1] = {row_sum(share)};
         sum += fold_rows(sum_of_row, AddF());
         const int here = min(pieces - s0, 64);
-#pragma unroll 8
-        for (int s = 0; s < here; ++s) {
-            const float w = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, share), s));
-            const float *o = a.part_o + (first + (s0 + s) * step) * D + c;
-            if constexpr (kPer == 2) {
-                const float2 v = *reinterpret_cast<const float2 *>(o);
-                y[0] = fmaf(w, v.x, y[0]);
-                y[1] = fmaf(w, v.y, y[1]);
-            } else {
-                const float4 v = *reinterpret_cast<const float4 *>(o);
-                y[0] = fmaf(w, v.x, y[0]);
-                y[1] = fmaf(w, v.y, y[1]);
-                y[2] = fmaf(w, v.z, y[2]);
-                y[3] = fmaf(w, v.w, y[3]);
+        for (int s = 0; s < here; s += kTogether) {
+            float v[kTogether][kPer];
+#pragma unroll
+            for (int k = 0; k < kTogether; ++k) {   // (past the last piece: it again, with no weight)
+                const float *o = a.part_o + (first + (s0 + min(s + k, here - 1)) * step) * D + c;
+                if constexpr (kPer == 2) {
+                    const float2 x = *reinterpret_cast<const float2 *>(o);
+                    v[k][0] = x.x;
+                    v[k][1] = x.y;
+                } else {
+                    const float4 x = *reinterpret_cast<const float4 *>(o);
+                    v[k][0] = x.x;
+                    v[k][1] = x.y;
+                    v[k][2] = x.z;
+                    v[k][3] = x.w;
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < kTogether; ++k) {
+                const float w = s + k < here ? __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, share), min(s + k, 63))) : 0.f;
+                if (s + k < here)
+#pragma unroll
+                    for (int i = 0; i < kPer; ++i) y[i] = fmaf(w, v[k][i], y[i]);
             }
         }
     }
@@ -978,14 +996,11 @@ hipError_t launch_d(Fp8AttentionArgs &a, hipStream_t s)
     return hipGetLastError();
 }
 
-#ifndef WT
-#define WT 512
-#endif
 template <int D>
 hipError_t launch_weights_d(Fp8WeightsArgs &a, hipStream_t s)
 {
     const int64_t units = (int64_t)a.in.n_seq * ((a.bound + 63) / 64), hkv = a.in.c.n_kv_heads;
-    int64_t parts = WT / hkv < 1 ? 1 : WT / hkv;
+    int64_t parts = 512 / hkv < 1 ? 1 : 512 / hkv;
     if (parts * kLeastUnits > units) parts = (units + kLeastUnits - 1) / kLeastUnits;
     a.parts = a.in.n_seq > kMostSeqs || a.in.n_seq >= 4 * parts || parts <= 1 ? 0 : (int)parts;
     const uint32_t grid = (uint32_t)((a.parts > 0 ? a.parts : a.in.n_seq) * hkv);

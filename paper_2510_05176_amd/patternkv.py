@@ -626,7 +626,7 @@ def pk_fp8_attention(cfg: Fp8Config, cache: Fp8Cache, q: torch.Tensor, softmax_s
                      slopes: torch.Tensor | None = None, counts: torch.Tensor | None = None, bound: int | None = None,
                      out: torch.Tensor | None = None, lse: torch.Tensor | None = None, workspace: torch.Tensor | None = None):
     """Attention of the last n tokens of every sequence, q [n_seq, n_q_heads, n, d] (or [n_seq, n_q_heads, d] for one), over the
-    tokens that the cache holds -> out, the same shape and type.  Strides as in pk_fp8_append.  cap, window, slopes [n_q_heads]: see
+    tokens that the cache holds -> out, the same shape and type, laid out like q.  Strides as in pk_fp8_append.  cap, window, slopes [n_q_heads]: see
     include/patternkv.h.  counts int32 [n_seq]: the sequence's queries are the first counts[i] (rows behind them are left as they
     were).  bound: no sequence holds more tokens than this (default: the capacity); sizes the launch.
     lse float32 [n_seq, n_q_heads, n] receives the log-sum-exp."""
@@ -636,14 +636,13 @@ def pk_fp8_attention(cfg: Fp8Config, cache: Fp8Cache, q: torch.Tensor, softmax_s
     qs = _fp8_vectors(cfg, cache, q, cfg.n_q_heads, "q")
     n = q.shape[2]
     if out is None:
-        # a token's heads next to each other, as the projection that follows takes them; rows that are not written are zero
-        new = torch.empty if counts is None else torch.zeros
-        o = new((cfg.n_seq, n, cfg.n_q_heads, cfg.head_dim), dtype=q.dtype, device=q.device).transpose(1, 2)
+        # laid out like q where q is dense (then its strides serve for both); rows that are not written are zero
+        o = torch.empty_like(q) if counts is None else torch.zeros_like(q)
     else:
         o = out.unsqueeze(2) if one and out.dim() == 3 else out
         if o.shape != q.shape:
             raise ValueError(f"out: expected {list(q.shape)}, got {list(o.shape)}")
-    os_ = _fp8_vectors(cfg, cache, o, cfg.n_q_heads, "out")
+    os_ = qs if out is None and o.stride() == q.stride() else _fp8_vectors(cfg, cache, o, cfg.n_q_heads, "out")
     bound = cfg.t_capacity if bound is None else bound
     workspace = _fp8_workspace(cfg, cache, workspace, FP8_OP_ATTENTION, n, bound)
     _check(_lib.pk_fp8_attention(cfg.packed, cache.packed, cache.states.data_ptr(), bound, q.data_ptr(), qs, n, _fp8_counts(cfg, cache, counts),

@@ -106,13 +106,14 @@ def test_append_refuses(pk):
 
 def test_attention_and_weights_refuse(pk):
     bad = pk._pack_fp8_scores
+    long = pk.Fp8Config(**{**BASE, "t_capacity": 8192}).packed   # split over workgroups, so that there is something to merge
     assert attention(pk, n=0) == OK
     for want, kw in [(INVALID, dict(states=0)), (INVALID, dict(q=0)), (INVALID, dict(out=0)), (INVALID, dict(n=-1)), (INVALID, dict(bound=-1)),
                      (INVALID, dict(scores=bad(1.0, -1.0, 0, 0))), (INVALID, dict(scores=bad(1.0, float("nan"), 0, 0))),
                      (INVALID, dict(scores=bad(1.0, 0.0, -1, 0))), (ALIGNMENT, dict(scores=bad(1.0, 0.0, 0, P + 4))), (ALIGNMENT, dict(q=P + 8)),
                      (ALIGNMENT, dict(out=P + 8)), (ALIGNMENT, dict(lse=P + 4)), (ALIGNMENT, dict(ws=P + 4)), (ALIGNMENT, dict(qs=strides(pk, 8, 9, 8))),
                      (ALIGNMENT, dict(os_=strides(pk, 8, 8, 12))), (CAPACITY, dict(bound=1025)), (CAPACITY, dict(n=1025)),
-                     (WORKSPACE, dict(ws=0)), (WORKSPACE, dict(size=255))]:
+                     (WORKSPACE, dict(cfg=long, bound=8192, ws=0)), (WORKSPACE, dict(cfg=long, bound=8192, size=255))]:
         assert attention(pk, **kw) == want, kw
     assert weights(pk, n=0) == OK
     for want, kw in [(INVALID, dict(lse=0)), (INVALID, dict(cache=cache_of(pk, weight=0))), (INVALID, dict(q=0)), (ALIGNMENT, dict(lse=P + 8)),
