@@ -112,10 +112,10 @@ pk_status take_queries(const pk_fp8_config *cfg, const pk_fp8_cache *cache, cons
     pk_status st = check_config(cfg);
     if (st != PK_OK) return st;
     if ((st = check_cache(cfg, cache)) != PK_OK) return st;
-    if (!states || !q || !scores || n_query < 0 || bound < 0) return PK_ERR_INVALID_ARG;
+    if (!states || (!q && n_query > 0) || !scores || n_query < 0 || bound < 0) return PK_ERR_INVALID_ARG;
     if ((st = check_strides(qs)) != PK_OK) return st;
     if (!aligned16(states) || !aligned16(q) || !aligned16(counts) || !aligned16(scores->slopes)) return PK_ERR_ALIGNMENT;
-    if (!(scores->cap >= 0.f) || scores->window < 0) return PK_ERR_INVALID_ARG;   // also a NaN
+    if (!(scores->cap == 0.f || (scores->cap >= 1e-30f && scores->cap <= 1e30f)) || scores->window < 0) return PK_ERR_INVALID_ARG;   // also a NaN
     if (n_query > cfg->t_capacity || bound > cfg->t_capacity) return PK_ERR_CAPACITY;
     a.c = make_view(cfg, cache);
     a.states = states;
@@ -210,8 +210,10 @@ pk_status pk_fp8_attention(const pk_fp8_config *cfg, const pk_fp8_cache *cache, 
     Fp8AttentionArgs a;
     pk_status st = take_queries(cfg, cache, states, bound, q, qs, n_query, counts, scores, a.in);
     if (st != PK_OK) return st;
-    if (!out) return PK_ERR_INVALID_ARG;
+    if (!out && n_query > 0) return PK_ERR_INVALID_ARG;
     if ((st = check_strides(os)) != PK_OK) return st;
+    // a row of the output has one place
+    if ((cfg->n_seq > 1 && os->seq == 0) || (n_query > 1 && os->token == 0) || (cfg->n_q_heads > 1 && os->head == 0)) return PK_ERR_SHAPE;
     if (!aligned16(out) || !aligned16(lse) || !aligned16(workspace)) return PK_ERR_ALIGNMENT;
     if (n_query == 0) return PK_OK;
     const AttentionPlan p = plan_attention(cfg, n_query, bound);
@@ -238,7 +240,7 @@ pk_status pk_fp8_weights(const pk_fp8_config *cfg, const pk_fp8_cache *cache, co
     Fp8WeightsArgs a;
     const pk_status st = take_queries(cfg, cache, states, bound, q, qs, n_query, counts, scores, a.in);
     if (st != PK_OK) return st;
-    if (!lse || !cache->weight) return PK_ERR_INVALID_ARG;
+    if ((!lse && n_query > 0) || !cache->weight) return PK_ERR_INVALID_ARG;
     if (!aligned16(lse)) return PK_ERR_ALIGNMENT;
     if (n_query == 0 && accumulate) return PK_OK;
     a.lse = lse;

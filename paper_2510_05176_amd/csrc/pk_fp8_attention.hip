@@ -963,7 +963,7 @@ bool eight_waves(int64_t workgroups, int64_t bound) { return workgroups <= 256 &
 // long runs, which make half as many pieces then (16 sequences x 32k tokens 185.6 -> 181.4 us, 8 of them with 256 channels 201 -> 186); shorter
 // ones change from sequence to sequence more often, where eight waves wait for each other (32 sequences of 700 to 6000 tokens, five
 // queries: 72.5 -> 77.5).
-bool long_runs(int64_t n_seq, int64_t across, int64_t bound) { return n_seq * ((bound + 63) / 64) * across >= 128 * 256; }
+bool long_runs(int64_t n_seq, int64_t across, int64_t bound) { return across <= 256 && n_seq * ((bound + 63) / 64) * across >= 128 * 256; }
 
 template <int D, int RT, int NW, bool BY_ROWS>
 void launch_rt(const Fp8AttentionArgs &a, uint32_t grid, bool opt, hipStream_t s)

@@ -1,7 +1,8 @@
 """The 8-bit cache's entry points without a GPU: sizes, refusals (every one before a launch, so that fake pointers do), and the
 64-bit reference that the GPU tests compare with against torch's own e4m3 type."""
-import ctypes as C
 import os
+import shutil
+import subprocess
 
 import numpy as np
 import pytest
@@ -107,15 +108,17 @@ def test_append_refuses(pk):
 def test_attention_and_weights_refuse(pk):
     bad = pk._pack_fp8_scores
     long = pk.Fp8Config(**{**BASE, "t_capacity": 8192}).packed   # split over workgroups, so that there is something to merge
-    assert attention(pk, n=0) == OK
+    assert attention(pk, n=0) == OK and attention(pk, n=0, q=0, out=0) == OK
     for want, kw in [(INVALID, dict(states=0)), (INVALID, dict(q=0)), (INVALID, dict(out=0)), (INVALID, dict(n=-1)), (INVALID, dict(bound=-1)),
                      (INVALID, dict(scores=bad(1.0, -1.0, 0, 0))), (INVALID, dict(scores=bad(1.0, float("nan"), 0, 0))),
-                     (INVALID, dict(scores=bad(1.0, 0.0, -1, 0))), (ALIGNMENT, dict(scores=bad(1.0, 0.0, 0, P + 4))), (ALIGNMENT, dict(q=P + 8)),
+                     (INVALID, dict(scores=bad(1.0, 0.0, -1, 0))), (INVALID, dict(scores=bad(1.0, float("inf"), 0, 0))), (INVALID, dict(scores=bad(1.0, 1e-38, 0, 0))),
+                     (SHAPE, dict(os_=strides(pk, 0, 256, 128))), (SHAPE, dict(os_=strides(pk, 8192, 256, 0))), (SHAPE, dict(n=2, os_=strides(pk, 8192, 0, 128))),
+                     (ALIGNMENT, dict(scores=bad(1.0, 0.0, 0, P + 4))), (ALIGNMENT, dict(q=P + 8)),
                      (ALIGNMENT, dict(out=P + 8)), (ALIGNMENT, dict(lse=P + 4)), (ALIGNMENT, dict(ws=P + 4)), (ALIGNMENT, dict(qs=strides(pk, 8, 9, 8))),
                      (ALIGNMENT, dict(os_=strides(pk, 8, 8, 12))), (CAPACITY, dict(bound=1025)), (CAPACITY, dict(n=1025)),
                      (WORKSPACE, dict(cfg=long, bound=8192, ws=0)), (WORKSPACE, dict(cfg=long, bound=8192, size=255))]:
         assert attention(pk, **kw) == want, kw
-    assert weights(pk, n=0) == OK
+    assert weights(pk, n=0) == OK and weights(pk, n=0, q=0, lse=0) == OK
     for want, kw in [(INVALID, dict(lse=0)), (INVALID, dict(cache=cache_of(pk, weight=0))), (INVALID, dict(q=0)), (ALIGNMENT, dict(lse=P + 8)),
                      (CAPACITY, dict(bound=2000)), (INVALID, dict(scores=bad(1.0, 0.0, -5, 0)))]:
         assert weights(pk, **kw) == want, kw
@@ -174,3 +177,19 @@ def test_reference_codes_are_e4m3():
 def test_reference_exponents():
     for top, e in [(448.0, 0), (448.25, 1), (447.0, 0), (224.0, -1), (224.5, 0), (0.0, -126), (1.0, -8), (65504.0, 8), (2.0 ** -140, -126)]:
         assert ref.block_exponent(np.array([0.0, -top, np.inf, np.nan])) == e, top
+
+
+@pytest.mark.skipif(shutil.which("hipcc") is None and not os.path.exists("/opt/rocm/bin/hipcc"), reason="no hipcc")
+def test_host_checks_under_asan_ubsan(tmp_path):
+    """The host side with its launches replaced by stubs; the sanitizer flags go to the host pass only."""
+    csrc, driver, exe = os.path.join(ROOT, "paper_2510_05176_amd", "csrc"), os.path.join(ROOT, "tests", "sanitize", "fp8_api_driver.cpp"), str(tmp_path / "fp8_san")
+    san = [x for f in ("-fsanitize=address,undefined", "-fno-sanitize-recover=undefined") for x in ("-Xarch_host", f)]
+    cmd = [shutil.which("hipcc") or "/opt/rocm/bin/hipcc", "-x", "hip", "-std=c++17", "--offload-arch=gfx950", "-O1", "-g", "-fno-omit-frame-pointer"] + san + [
+        "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-I", os.path.join(ROOT, "include"), "-I", csrc, os.path.join(csrc, "pk_fp8_api.hip"), driver, "-o", exe]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr[-4000:]
+    env = dict(os.environ, ASAN_OPTIONS="detect_leaks=1:abort_on_error=0", UBSAN_OPTIONS="print_stacktrace=1")
+    env.pop("LD_PRELOAD", None)
+    r = subprocess.run([exe], capture_output=True, text=True, env=env, timeout=120)
+    assert r.returncode == 0 and r.stdout.strip().endswith("ok"), (r.returncode, r.stdout[-2000:], r.stderr[-4000:])
+    assert "runtime error" not in r.stderr and "AddressSanitizer" not in r.stderr, r.stderr[-4000:]

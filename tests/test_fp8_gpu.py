@@ -43,7 +43,8 @@ class Pair:
     def new_cache(self, cfg):
         cache = self.pk.Fp8Cache(cfg)
         for n in ("k_codes", "v_codes"):   # what lies behind the tokens held is anything, NaN codes included
-            cache.buf[n].copy_(torch.from_numpy(self.rng.integers(0, 256, cache.buf[n].numel()).astype(np.uint8)))
+            noise = torch.from_numpy(self.rng.integers(0, 256, 65521).astype(np.uint8)).cuda()
+            cache.buf[n].copy_(noise.repeat(-(-cache.buf[n].numel() // 65521))[:cache.buf[n].numel()])
         for n in ("k_scale", "v_scale", "weight"):
             cache.buf[n].fill_(math.nan)
         if cfg.page_tokens:
@@ -134,7 +135,7 @@ class Pair:
                 assert np.array_equal(got_lse[b, :, :m] == -np.inf, empty) and (got[b, :, :m][empty] == 0).all()
                 ok = ~empty & ~np.isnan(want_lse)
                 assert np.array_equal(np.isnan(got_lse[b, :, :m]), np.isnan(want_lse))
-                far = np.abs(got_lse[b, :, :m] - want_lse)[ok]
+                far = np.abs(got_lse[b, :, :m][ok] - want_lse[ok])
                 assert (far <= (off + s.length * 2.0 ** -24 + 2.0 ** -22 * (np.abs(want_lse) + 2))[ok]).all()
             if weights is not None:
                 soft = soft if m else np.zeros((cfg.n_q_heads, 0, s.length))
@@ -247,18 +248,28 @@ ATTENDS = [
 ]
 
 
+# What the capacity decides: short caches are taken whole, longer ones in runs whose pieces are merged, and very long ones in long runs.
+CAPS = [1024, 4096, 1 << 19]
+
+
+@pytest.mark.parametrize("cap", CAPS)
 @pytest.mark.parametrize("lengths,n,r,d,block,bf16,page,how", ATTENDS)
-def test_attention_and_weights(pk, lengths, n, r, d, block, bf16, page, how):
-    p = Pair(pk, 5, n_seq=4, hkv=2, r=r, d=d, block=block, cap=1024, bf16=bf16, page=page, spread=0.5)
+def test_attention_and_weights(pk, lengths, n, r, d, block, bf16, page, how, cap):
+    p = Pair(pk, 5, n_seq=4, hkv=2, r=r, d=d, block=block, cap=cap, bf16=bf16, page=page, spread=0.5)
     p.append(max(lengths), counts=lengths)
     p.attend(n, weights=False, **how)
     p.attend(n, weights=True, **how)
     p.attend(n, counts=[n, n // 2, 0, max(n - 1, 0)], weights=True, bound=64, **how)   # a bound below the lengths costs time only
 
 
-def test_empty_sequences(pk):
-    """Nothing held, and more queries than tokens: no row sees anything, or only the last do."""
-    p = Pair(pk, 6, n_seq=3, cap=256)
+@pytest.mark.parametrize("cap", [256, 4096])
+def test_empty_sequences(pk, cap):
+    """Nothing held, and more queries than tokens: no row sees anything, or only the last do.  No queries, no new vectors."""
+    p = Pair(pk, 6, n_seq=3, cap=cap)
+    p.attend(0)
+    p.append(0)
+    p.check()
+    assert p.append(0, states_out=torch.full_like(p.cache.states, 5)).tolist() == [[0, 0, 0, 0]] * 3
     p.attend(1, weights=True)
     p.attend(4, weights=False)
     p.append(3, counts=[0, 3, 1])
@@ -267,20 +278,36 @@ def test_empty_sequences(pk):
         p.attend(n, weights=False, counts=[n, 0, min(n, 2)], window=2)
 
 
-def test_few_heads_and_queries_share_tiles(pk):
+@pytest.mark.parametrize("cap", [320, 2240, 1 << 21])
+def test_few_heads_and_queries_share_tiles(pk, cap):
     """Every number of rows around the tile sizes."""
-    p = Pair(pk, 7, n_seq=1, hkv=1, r=1, d=64, cap=320)
+    p = Pair(pk, 7, n_seq=1, hkv=1, r=1, d=64, cap=cap)
     p.append(300)
     for n in (15, 16, 17, 31, 32, 33, 63, 64, 65, 127, 128, 129, 300):
         p.attend(n, weights=False)
 
 
+@pytest.mark.parametrize("n_seq,hkv,r,n,window", [(70, 1, 1, 1, 0), (200, 1, 3, 2, 0), (256, 1, 1, 1, 50), (257, 1, 1, 1, 0), (65, 2, 2, 1, 100), (33, 4, 40, 1, 0)])
+def test_many_sequences_of_unequal_lengths(pk, n_seq, hkv, r, n, window):
+    """Runs that begin and end anywhere in the batch, several sequences in one run and several runs in one sequence, empty ones among
+    them; more sequences than one wave has lanes, and more than are dealt out."""
+    rng = np.random.default_rng(n_seq)
+    p = Pair(pk, 19, n_seq=n_seq, hkv=hkv, r=r, d=64, cap=2176, spread=0.3)
+    lengths = [0, 2100, 1] + [int(x) for x in rng.integers(0, 150, n_seq - 4)] + [1300]
+    p.append(150, counts=[min(x, 150) for x in lengths])
+    rest = [x - min(x, 150) for x in lengths]
+    p.append(max(rest), counts=rest)
+    p.attend(n, weights=False, window=window)
+    p.attend(n, weights=True, counts=[int(x) for x in rng.integers(0, n + 1, n_seq)], window=window)
+
+
+@pytest.mark.parametrize("cap", [512, 4096])
 @pytest.mark.parametrize("n,how", [(1, {}), (1, dict(window=40)), (6, {}), (6, dict(window=40)), (150, {}), (150, dict(window=100))])
 @pytest.mark.parametrize("d,block", [(128, 64), (96, 32), (256, 128)])
-def test_masked_values_do_not_reach_a_row(pk, n, how, d, block):
+def test_masked_values_do_not_reach_a_row(pk, n, how, d, block, cap):
     """NaN in K and V at tokens that some rows see and others do not, and in whole blocks; and behind the tokens held (every
     cache of these tests starts with NaN codes and scales there)."""
-    p = Pair(pk, 8, n_seq=2, hkv=1, r=2, d=d, block=block, cap=512)
+    p = Pair(pk, 8, n_seq=2, hkv=1, r=2, d=d, block=block, cap=cap)
     k, v = p.vectors(300, 1), p.vectors(300, 1)
     for t, c in ((298, 5), (297, 70 % d), (220, d - 1), (150, 0)):
         v[0][0, 0, t, c] = math.nan
@@ -306,11 +333,12 @@ def test_scores_of_any_size(pk):
     p.attend(2, q=(q[0], q[1] * 0.0), weights=False)
 
 
+@pytest.mark.parametrize("cap", [512, 4096])
 @pytest.mark.parametrize("bf16", [False, True])
-def test_value_scales_of_every_size(pk, bf16):
+def test_value_scales_of_every_size(pk, bf16, cap):
     """Blocks whose V scales differ by up to 2^24 (bfloat16: 2^70) in both orders, the large ones with little softmax weight: the rest of
     the result keeps its precision."""
-    p = Pair(pk, 10, n_seq=1, hkv=1, r=2, d=64, block=32, cap=512, bf16=bf16, spread=0.0)
+    p = Pair(pk, 10, n_seq=1, hkv=1, r=2, d=64, block=32, cap=cap, bf16=bf16, spread=0.0)
     k, v = p.vectors(512, 1), p.vectors(512, 1)
     sizes = [0, 3, -4, 10, 2, -9, 12, 1, 0, 5, -3, 8, 4, 0, 11, 2] if not bf16 else [0, 3, -40, 30, 2, -9, 12, 1, 0, 25, -35, 8, 4, 0, 11, 2]
     for i, e in enumerate(sizes):
@@ -432,10 +460,11 @@ def test_a_serving_loop(pk, bf16, page):
     p.check()
 
 
-def test_replayed_graph_grows_the_sequences(pk):
+@pytest.mark.parametrize("cap", [1024, 4096])
+def test_replayed_graph_grows_the_sequences(pk, cap):
     """A generation step (append in place, attention, weights) captured once and replayed with new tokens, eager work and waits in
     between, against the same steps without a graph."""
-    a, b = (Pair(pk, 15, n_seq=3, hkv=2, r=4, cap=1024) for _ in range(2))
+    a, b = (Pair(pk, 15, n_seq=3, hkv=2, r=4, cap=cap) for _ in range(2))
     a.append(200, counts=[200, 63, 0])
     b.append(200, counts=[200, 63, 0])
     new = [(a.vectors(1, 2)[0], a.vectors(1, 2)[0], a.vectors(1, 8)[0]) for _ in range(6)]
