@@ -235,8 +235,9 @@ __device__ __forceinline__ void to_scores(float (&x)[16], float (&f)[2], const f
         for (int h = 0; h < 2; ++h) f[h] = fmaxf(f[h] * post, 0x1p-126f);
     }
     if (edge) {
+        const int more = row.last - t;   // tokens after t that the row sees
 #pragma unroll
-        for (int i = 0; i < 16; ++i) x[i] = t + 16 * (i >> 2) + (i & 3) <= row.last ? x[i] : -INFINITY;
+        for (int i = 0; i < 16; ++i) x[i] = 16 * (i >> 2) + (i & 3) <= more ? x[i] : -INFINITY;
     }
 }
 
@@ -502,12 +503,14 @@ __global__ __launch_bounds__(64 * NW, 2) void fp8_attention_kernel(Fp8AttentionA
             }
             const int fold = min(unit - field, 60);   // from 29 on fp16 leaves nothing of the numerators
             if (half == 0 ? shift != 0 || __any(moved) : shift != 0) {
-                asm volatile("");   // a branch: most blocks leave o as it is
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) {
                     const float f = ldexpf(half == 0 ? by[rt] : 1.f, shift);
 #pragma unroll
-                    for (int ct = 0; ct < S::kTiles; ++ct) o[rt][ct] *= f;
+                    for (int ct = 0; ct < S::kTiles; ++ct) {
+                        asm volatile("" : "+v"(o[rt][ct]));   // a branch, not a multiplication by 1 for the many blocks that leave o as it is
+                        o[rt][ct] *= f;
+                    }
                 }
             }
             half8v pf[RT];
@@ -905,9 +908,9 @@ __global__ __launch_bounds__(kThreads, 2) void fp8_weights_kernel(Fp8WeightsArgs
 #pragma unroll
                             for (int h = 0; h < 2; ++h) f[h] = fmaxf(ks[h] * c, 0x1p-126f);
                             if (edge) {
-                                const int last = sm_row[16 * tile + n].last;
+                                const int more = sm_row[16 * tile + n].last - (t0 + 4 * g);   // tokens after the lane's first that the row sees
 #pragma unroll
-                                for (int i = 0; i < 16; ++i) y[i] = t0 + 4 * g + 16 * (i >> 2) + (i & 3) <= last ? y[i] : -INFINITY;
+                                for (int i = 0; i < 16; ++i) y[i] = 16 * (i >> 2) + (i & 3) <= more ? y[i] : -INFINITY;
                             }
 #pragma unroll
                             for (int i = 0; i < 16; ++i) sum[i] += exp2_(fmaf(y[i], f[i >> 3], -lse));
