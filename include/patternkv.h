@@ -444,7 +444,7 @@ typedef struct {
     int64_t seq, token, head;
 } pk_strides;
 
-/* What is done to the scores.  s = softmax_scale * q.k; cap (0, or 1e-30 to 1e30) > 0: s = cap * tanh(s / cap); slopes: s -= slopes[query head] *
+/* What is done to the scores.  s = softmax_scale * q.k (finite); cap (0, or 1e-30 to 1e30) > 0: s = cap * tanh(s / cap); slopes: s -= slopes[query head] *
  * (pos of the query - pos of the key); window > 0: keys `window` or more positions back are masked. */
 typedef struct {
     float softmax_scale;

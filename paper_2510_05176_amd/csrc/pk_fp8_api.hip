@@ -1,4 +1,6 @@
 // Host side of the 8-bit cache's entry points (pk_fp8_* of include/patternkv.h): checks, sizes, launches.
+#include <cfloat>
+#include <cmath>
 #include <cstring>
 
 #include "pk_fp8.h"
@@ -115,8 +117,10 @@ pk_status take_queries(const pk_fp8_config *cfg, const pk_fp8_cache *cache, cons
     if (!states || (!q && n_query > 0) || !scores || n_query < 0 || bound < 0) return PK_ERR_INVALID_ARG;
     if ((st = check_strides(qs)) != PK_OK) return st;
     if (!aligned16(states) || !aligned16(q) || !aligned16(counts) || !aligned16(scores->slopes)) return PK_ERR_ALIGNMENT;
+    if (!(std::fabs(scores->softmax_scale) <= FLT_MAX)) return PK_ERR_INVALID_ARG;
     if (!(scores->cap == 0.f || (scores->cap >= 1e-30f && scores->cap <= 1e30f)) || scores->window < 0) return PK_ERR_INVALID_ARG;   // also a NaN
     if (n_query > cfg->t_capacity || bound > cfg->t_capacity) return PK_ERR_CAPACITY;
+    if ((int64_t)n_query * (cfg->n_q_heads / cfg->n_kv_heads) > (1 << 28)) return PK_ERR_UNSUPPORTED;   // rows of a KV head, counted in 32 bits
     a.c = make_view(cfg, cache);
     a.states = states;
     a.q = q;

@@ -336,8 +336,8 @@ __global__ __launch_bounds__(kMoveThreads) void fp8_move_kernel(Fp8EvictArgs a)
     if (n <= 0) return;
     const StreamMap from = a.from.map.of(stream);
     if (tid < n) {
-        // an index from the workspace is one that the selection wrote, below the sequence's length
-        const int t = st.x <= a.budget ? t0 + tid : a.kept[(int64_t)stream * a.budget + t0 + tid];
+        // an index is one that the selection wrote, below the sequence's length; whatever the workspace holds, it leads nowhere else
+        const int t = st.x <= a.budget ? t0 + tid : min(max(a.kept[(int64_t)stream * a.budget + t0 + tid], 0), a.from.t_capacity - 1);
         const int page = from.pages ? min(max(from.pages[t >> from.shift], 0), from.n_pages - 1) : 0;
         const int64_t row = from.pos_in(page, t);
         sm_row[tid] = row;

@@ -553,7 +553,9 @@ class Fp8Cache:
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda device: torch.cuda.current_stream(device).cuda_stream)
 
 
-def _fp8_stream(cache: Fp8Cache):
+def _fp8_stream(cfg: Fp8Config, cache: Fp8Cache):
+    if cfg is not cache.cfg and cfg != cache.cfg:
+        raise ValueError("the cache was made for another configuration")
     # the launches go to the current device's stream, so the memory has to be that device's
     index = cache.device.index
     if index is None or index != torch.cuda.current_device():
@@ -618,7 +620,7 @@ def pk_fp8_append(cfg: Fp8Config, cache: Fp8Cache, k_new: torch.Tensor, v_new: t
     if out is not cache.states and (out.dtype != torch.int32 or tuple(out.shape) != (cfg.n_seq, 4) or not out.is_contiguous() or out.device != cache.device):
         raise ValueError(f"states_out: expected contiguous int32 [{cfg.n_seq}, 4] on {cache.device}")
     _check(_lib.pk_fp8_append(cfg.packed, cache.packed, cache.states.data_ptr(), out.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), ks, vs,
-                              k_new.shape[2], _fp8_counts(cfg, cache, counts), _fp8_stream(cache)), "pk_fp8_append")
+                              k_new.shape[2], _fp8_counts(cfg, cache, counts), _fp8_stream(cfg, cache)), "pk_fp8_append")
     return out
 
 
@@ -648,7 +650,7 @@ def pk_fp8_attention(cfg: Fp8Config, cache: Fp8Cache, q: torch.Tensor, softmax_s
     _check(_lib.pk_fp8_attention(cfg.packed, cache.packed, cache.states.data_ptr(), bound, q.data_ptr(), qs, n, _fp8_counts(cfg, cache, counts),
                                  _fp8_scores(cfg, cache, softmax_scale, cap, window, slopes), o.data_ptr(), os_,
                                  None if lse is None else _fp8_lse(cfg, cache, lse, n), None if workspace is None else workspace.data_ptr(),
-                                 0 if workspace is None else workspace.numel(), _fp8_stream(cache)), "pk_fp8_attention")
+                                 0 if workspace is None else workspace.numel(), _fp8_stream(cfg, cache)), "pk_fp8_attention")
     return out if out is not None else o.squeeze(2) if one else o
 
 
@@ -663,16 +665,16 @@ def pk_fp8_weights(cfg: Fp8Config, cache: Fp8Cache, q: torch.Tensor, lse: torch.
     bound = cfg.t_capacity if bound is None else bound
     _check(_lib.pk_fp8_weights(cfg.packed, cache.packed, cache.states.data_ptr(), bound, q.data_ptr(), qs, n, _fp8_counts(cfg, cache, counts),
                                _fp8_scores(cfg, cache, softmax_scale, cap, window, slopes), _fp8_lse(cfg, cache, lse, n), 1 if accumulate else 0,
-                               _fp8_stream(cache)), "pk_fp8_weights")
+                               _fp8_stream(cfg, cache)), "pk_fp8_weights")
 
 
 def pk_fp8_evict(cfg: Fp8Config, cache: Fp8Cache, to_cfg: Fp8Config, to: Fp8Cache, budget: int, keep_first: int = 0, keep_last: int = 0,
                  workspace: torch.Tensor | None = None):
     """Bring every sequence down to `budget` tokens in another cache: the first keep_first, the last keep_last, and of the others those
     with the largest weight."""
-    if to.device != cache.device:
-        raise ValueError(f"the caches are on {cache.device} and {to.device}")
+    if to.device != cache.device or (to_cfg is not to.cfg and to_cfg != to.cfg):
+        raise ValueError(f"the caches are on {cache.device} and {to.device}; each goes with its own configuration")
     workspace = _fp8_workspace(cfg, cache, workspace, FP8_OP_EVICT, budget, 0)
     _check(_lib.pk_fp8_evict(cfg.packed, cache.packed, cache.states.data_ptr(), to_cfg.packed, to.packed, to.states.data_ptr(), budget, keep_first,
                              keep_last, None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.numel(),
-                             _fp8_stream(cache)), "pk_fp8_evict")
+                             _fp8_stream(cfg, cache)), "pk_fp8_evict")

@@ -108,10 +108,12 @@ def test_append_refuses(pk):
 def test_attention_and_weights_refuse(pk):
     bad = pk._pack_fp8_scores
     long = pk.Fp8Config(**{**BASE, "t_capacity": 8192}).packed   # split over workgroups, so that there is something to merge
+    wide = pk.Fp8Config(n_seq=1, n_kv_heads=1, n_q_heads=64, t_capacity=1 << 25).packed
     assert attention(pk, n=0) == OK and attention(pk, n=0, q=0, out=0) == OK
     for want, kw in [(INVALID, dict(states=0)), (INVALID, dict(q=0)), (INVALID, dict(out=0)), (INVALID, dict(n=-1)), (INVALID, dict(bound=-1)),
                      (INVALID, dict(scores=bad(1.0, -1.0, 0, 0))), (INVALID, dict(scores=bad(1.0, float("nan"), 0, 0))),
-                     (INVALID, dict(scores=bad(1.0, 0.0, -1, 0))), (INVALID, dict(scores=bad(1.0, float("inf"), 0, 0))), (INVALID, dict(scores=bad(1.0, 1e-38, 0, 0))),
+                     (INVALID, dict(scores=bad(1.0, 0.0, -1, 0))), (INVALID, dict(scores=bad(float("nan"), 0.0, 0, 0))), (INVALID, dict(scores=bad(float("-inf"), 0.0, 0, 0))),
+                     (UNSUPPORTED, dict(cfg=wide, bound=64, n=(1 << 22) + 1)), (INVALID, dict(scores=bad(1.0, float("inf"), 0, 0))), (INVALID, dict(scores=bad(1.0, 1e-38, 0, 0))),
                      (SHAPE, dict(os_=strides(pk, 0, 256, 128))), (SHAPE, dict(os_=strides(pk, 8192, 256, 0))), (SHAPE, dict(n=2, os_=strides(pk, 8192, 0, 128))),
                      (ALIGNMENT, dict(scores=bad(1.0, 0.0, 0, P + 4))), (ALIGNMENT, dict(q=P + 8)),
                      (ALIGNMENT, dict(out=P + 8)), (ALIGNMENT, dict(lse=P + 4)), (ALIGNMENT, dict(ws=P + 4)), (ALIGNMENT, dict(qs=strides(pk, 8, 9, 8))),
@@ -156,6 +158,10 @@ def test_binding_refuses(pk):
         pk.pk_fp8_attention(cfg, cache, q, 1.0, slopes=torch.zeros(2))
     with pytest.raises(ValueError):
         pk.pk_fp8_weights(cfg, cache, q, torch.zeros(2, 8), 1.0)
+    with pytest.raises(ValueError):
+        pk._fp8_stream(pk.Fp8Config(**{**BASE, "t_capacity": 2048}), cache)     # another configuration's cache
+    with pytest.raises(ValueError):
+        pk._fp8_stream(cfg, cache)                                              # not on the current device
     with pytest.raises(AssertionError):
         pk.Fp8Cache(cfg, device="cpu", arrays={**cache.buf, "pos": cache.buf["pos"][:-1]})
     with pytest.raises(AssertionError):
