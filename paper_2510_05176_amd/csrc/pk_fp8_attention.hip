@@ -367,8 +367,108 @@ __device__ __forceinline__ void store_lse(const Fp8AttentionArgs &a, const Place
     a.lse[((int64_t)p.seq * a.in.c.n_kv_heads * a.in.r + p.kvh * a.in.r + h) * a.in.n_query + i] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
-// Rows of a workgroup: BY_ROWS, every wave has RT tiles of its own and walks all keys; else the waves share RT tiles and deal the keys
-// out among them, 64 at a time.
+// 64 tokens as operands of both products, for the four waves of a workgroup that walk the same keys: each reads and converts a quarter.
+template <int D>
+struct Tile {
+    half8v k[Shape<D>::kSteps][4][64];   // of 16 tokens each
+    half8v v[2][Shape<D>::kTiles][64];   // of 32 tokens each
+};
+// What a wave contributes: K of 16 tokens; V of 32, half of the channels that a lane has (64 channels: all, of which half are used)
+template <int D>
+struct Quarter {
+    static constexpr int kWords = D == 256 ? 2 : 1;
+    uint32_t k[D / 16], v[8][kWords];
+    float ks[2], vs[2];   // scales of the 64 tokens' halves
+};
+template <int D>
+__device__ __forceinline__ void fetch(Quarter<D> &x, const Fp8View &c, int64_t at, int wave, int n, int g)
+{
+    load_k<D>(x.k, c.k_codes + (at + 16 * wave) * D, n * D + g * (D / 4));
+    const uint8_t *v = c.v_codes + (at + 32 * (wave >> 1)) * D;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        const uint8_t *row = v + (16 * (j >> 2) + (j & 3)) * D;
+        if constexpr (D == 96) {
+            if (wave & 1) x.v[j][0] = *reinterpret_cast<const uint16_t *>(row + (4 * g * D + 64 + 2 * n));
+            else x.v[j][0] = *reinterpret_cast<const uint32_t *>(row + (4 * g * D + 4 * n));
+        } else if constexpr (D == 256) {
+            const uint2 w = *reinterpret_cast<const uint2 *>(row + 8 * (wave & 1) + (4 * g * D + 16 * n));
+            x.v[j][0] = w.x;
+            x.v[j][1] = w.y;
+        } else {
+            x.v[j][0] = *reinterpret_cast<const uint32_t *>(row + (D == 64 ? 0 : 4 * (wave & 1)) + (4 * g * D + D / 16 * n));
+        }
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const int64_t block = (at + 32 * h) >> c.log_block;
+        x.ks[h] = scalar_load(c.k_scale + block);
+        x.vs[h] = scalar_load(c.v_scale + block);
+    }
+}
+// left: tokens from the tile's first that exist; codes behind them may be anything, and are not to reach the product
+template <int D>
+__device__ __forceinline__ void lay_down(Tile<D> &to, Quarter<D> &x, int wave, int lane, int g, int left)
+{
+#pragma unroll
+    for (int s = 0; s < Shape<D>::kSteps; ++s) to.k[s][wave][lane] = k_operand<D>(x.k, s);
+    const int half = wave >> 1, part = wave & 1;
+    if (left < 64 || (half ? x.vs[1] : x.vs[0]) < 0.f) {
+        asm volatile("" : "+v"(g));   // what follows from it is computed here, not kept for the whole loop
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const bool none = 32 * half + 16 * (j >> 2) + 4 * g + (j & 3) >= left;
+#pragma unroll
+            for (int w = 0; w < Quarter<D>::kWords; ++w) x.v[j][w] = none ? 0u : x.v[j][w] & ~((nan_codes(x.v[j][w]) >> 7) * 0xffu);   // NaN codes have a product of their own
+        }
+    }
+#pragma unroll
+    for (int w = 0; w < Quarter<D>::kWords; ++w)
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {   // channels 0, 1 and 2, 3 of the word
+            if (D == 64 && b != part) continue;
+            if (D == 96 && b > 0 && part) continue;
+            uint32_t pair[4];   // of tokens
+#pragma unroll
+            for (int q = 0; q < 4; ++q) pair[q] = __builtin_amdgcn_perm(x.v[2 * q + 1][w], x.v[2 * q][w], b ? 0x07030602u : 0x05010400u);
+#pragma unroll
+            for (int c = 0; c < 2; ++c) {
+                half8v f;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    const half2v h = c ? codes_hi(pair[q]) : codes_lo(pair[q]);
+                    f[2 * q] = h[0];
+                    f[2 * q + 1] = h[1];
+                }
+                to.v[half][(D == 64 ? 0 : 4 * (part * Quarter<D>::kWords + w)) + 2 * b + c][lane] = f;
+            }
+        }
+}
+
+// Operands of products that follow each other, read from LDS four ahead: left to itself, the compiler reads each one just before its product
+// and waits.
+constexpr int kAhead = 4;
+constexpr int kArithmetic = 0x6;   // what may be moved across a step
+template <int N, int STRIDE, typename PRODUCT>
+__device__ __forceinline__ void products(half8v (&ahead)[kAhead], const half8v *operands, const PRODUCT &product)
+{
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        product(i, ahead[i % kAhead]);
+        if (i + kAhead < N) ahead[i % kAhead] = operands[(i + kAhead) * STRIDE];
+        __builtin_amdgcn_sched_barrier(kArithmetic);
+    }
+}
+template <int STRIDE>
+__device__ __forceinline__ void read_first(half8v (&ahead)[kAhead], const half8v *operands)
+{
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) ahead[i] = operands[i * STRIDE];
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+// Rows of a workgroup: BY_ROWS, every wave has RT tiles of its own and walks all keys, which lie in LDS as operands; else the waves share RT
+// tiles and deal the keys out among them, 64 at a time, each converting what it takes in registers.
 template <int D, int RT, int NW, bool BY_ROWS, bool OPT>
 __global__ __launch_bounds__(64 * NW, 2) void fp8_attention_kernel(Fp8AttentionArgs a)
 {
@@ -382,6 +482,9 @@ __global__ __launch_bounds__(64 * NW, 2) void fp8_attention_kernel(Fp8AttentionA
     __shared__ int sm_end[kMostSeqs];
     Run deal = {run, 0, 0, 0, 0};
     if (a.parts > 0 && !find_run<true>(a.in, a.parts, run, sm_end, deal)) return;
+    constexpr int kTilesInLds = D == 256 ? 1 : 2;   // (of 64 and 32 KB)
+    __shared__ Tile<BY_ROWS ? D : 64> sm_tile[BY_ROWS ? kTilesInLds : 1];
+    int turn = 0;   // of the tiles
     int seq = deal.seq, seq_from = deal.seq_from, seq_to = 0;
     const int at_unit = deal.at, stop = deal.stop;
     for (;; seq_from = seq_to, ++seq) {   // the pieces of the run
@@ -392,35 +495,37 @@ __global__ __launch_bounds__(64 * NW, 2) void fp8_attention_kernel(Fp8AttentionA
     const int row0 = BY_ROWS ? (group * NW + wave) * 16 * RT : group * 16 * RT;
 
     // queries: in registers for one tile of up to 128 channels, else in LDS (the registers then hold two tiles' results or 256 channels' of one)
-    constexpr bool kQueriesInLds = RT > 1 || D == 256;
-    constexpr int kOwn = BY_ROWS ? NW : 1;   // sets of queries
-    __shared__ half8v sm_q[kQueriesInLds ? kOwn : 1][kQueriesInLds ? RT : 1][kQueriesInLds ? S::kSteps : 1][64];
+    constexpr bool kQueriesInLds = !BY_ROWS && (RT > 1 || D == 256);
+    __shared__ half8v sm_q[kQueriesInLds ? RT : 1][kQueriesInLds ? S::kSteps : 1][64];
     Row row[RT];
-    half8v q_reg[S::kSteps];
+    half8v q_reg[kQueriesInLds ? 1 : RT][S::kSteps];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
         const int at = row0 + 16 * rt + n;
         row[rt] = row_of(a.in, p, at);
-        load_query<D>(q_reg, row[rt].factor, a.in, p.seq, p.kvh, at, at < p.count * a.in.r, g);
+        half8v (&qf)[S::kSteps] = q_reg[kQueriesInLds ? 0 : rt];
+        load_query<D>(qf, row[rt].factor, a.in, p.seq, p.kvh, at, at < p.count * a.in.r, g);
         if constexpr (kQueriesInLds) {
-            if (BY_ROWS || wave == 0)
+            if (wave == 0)
 #pragma unroll
-                for (int s = 0; s < S::kSteps; ++s) sm_q[BY_ROWS ? wave : 0][rt][s][lane] = q_reg[s];
+                for (int s = 0; s < S::kSteps; ++s) sm_q[rt][s][lane] = qf[s];
         }
     }
-    if constexpr (kQueriesInLds && !BY_ROWS) __syncthreads();
+    if constexpr (kQueriesInLds) __syncthreads();
     int q_lane = lane;
     const auto query = [&](int rt, int s) -> half8v {
-        if constexpr (kQueriesInLds) return sm_q[BY_ROWS ? wave : 0][rt][s][q_lane];
-        else return q_reg[s];
+        if constexpr (kQueriesInLds) return sm_q[rt][s][q_lane];
+        else return q_reg[rt][s];
     };
-    int lo, hi;
-    key_range(a.in, p, row0, min(row0 + 16 * RT, rows) - 1, lo, hi);
-    if (!whole) {
+    const auto keys_of = [&](int first_row, int end_row, int &lo, int &hi) {   // of the run's
+        key_range(a.in, p, first_row, min(end_row, rows) - 1, lo, hi);
+        if (whole) return;
         const int64_t from = first_visible(a.in, p.len, p.count);
         lo = (int)max(from + (int64_t)(max(at_unit, seq_from) - seq_from) * 64, (int64_t)lo);
         hi = (int)min(from + (int64_t)(min(stop, seq_to) - seq_from) * 64, (int64_t)hi);
-    }
+    };
+    int lo, hi;
+    keys_of(row0, row0 + 16 * RT, lo, hi);
     // the first token that some live row does not see, and the largest position of a live row
     const int sees_all = p.len - p.count + min(row0 / a.in.r, max(p.count - 1, 0)) + 1;
     const int pos_most = p.next - p.count + min((row0 + 16 * RT - 1) / a.in.r, p.count - 1);
@@ -439,32 +544,67 @@ __global__ __launch_bounds__(64 * NW, 2) void fp8_attention_kernel(Fp8AttentionA
 
     const uint32_t k_off = n * D + g * (D / 4), v_off = 4 * g * D + n * (D == 96 ? 4 : D / 16);
     const StreamMap map = a.in.c.map.of(p.stream);
-    const int first = BY_ROWS ? lo : lo + 64 * wave, step = BY_ROWS ? 64 : 64 * NW;
-    for (int t0 = first; t0 < hi; t0 += step) {
-        const int64_t at = map.pos(t0);
+    int first = lo + 64 * wave, last = hi;
+    Quarter<D> quarter;
+    if constexpr (BY_ROWS) {
+        keys_of(group * NW * 16 * RT, (group + 1) * NW * 16 * RT, first, last);
+        if (first < last) fetch<D>(quarter, a.in.c, map.pos(first), wave, n, g);
+    }
+    for (int t0 = first; t0 < last; t0 += BY_ROWS ? 64 : 64 * NW) {
         uint32_t kw[4][S::kKWords], vw[16][S::kVWords];
+        float ks[2], vs[2];
+        if constexpr (BY_ROWS) {
+            // a tile may be overwritten when all waves are past it: with two of them, that is known from the barrier of the one after it
+            if (kTilesInLds == 1) __syncthreads();
+            else turn ^= 1;
+            lay_down<D>(sm_tile[turn], quarter, wave, lane, g, last - t0);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) load_k<D>(kw[j], a.in.c.k_codes + at * D + 16 * j * D, k_off);
+            for (int h = 0; h < 2; ++h) {
+                ks[h] = fabsf(quarter.ks[h]);
+                vs[h] = quarter.vs[h];
+            }
+            __syncthreads();
+            if (t0 + 64 < last) fetch<D>(quarter, a.in.c, map.pos(t0 + 64), wave, n, g);
+            if (t0 < lo || t0 >= hi) continue;   // not this wave's rows'
+        } else {
+            const int64_t at = map.pos(t0);
 #pragma unroll
-        for (int j = 0; j < 16; ++j) load_v<D>(vw[j], a.in.c.v_codes + at * D + (16 * (j >> 2) + (j & 3)) * D, v_off, n);
-        const int64_t b0 = at >> a.in.c.log_block, b1 = (at + 32) >> a.in.c.log_block;
-        const float ks[2] = {fabsf(scalar_load(a.in.c.k_scale + b0)), fabsf(scalar_load(a.in.c.k_scale + b1))};
-        const float vs[2] = {scalar_load(a.in.c.v_scale + b0), scalar_load(a.in.c.v_scale + b1)};
+            for (int j = 0; j < 4; ++j) load_k<D>(kw[j], a.in.c.k_codes + at * D + 16 * j * D, k_off);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) load_v<D>(vw[j], a.in.c.v_codes + at * D + (16 * (j >> 2) + (j & 3)) * D, v_off, n);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int64_t block = (at + 32 * h) >> a.in.c.log_block;
+                ks[h] = fabsf(scalar_load(a.in.c.k_scale + block));
+                vs[h] = scalar_load(a.in.c.v_scale + block);
+            }
+        }
         const bool edge = t0 + 64 > sees_all;
         const bool windowed = OPT && a.in.window > 0 && (int64_t)pos_most - t0 >= a.in.window;
 
+        half8v ahead[BY_ROWS ? kAhead : 1];
         if constexpr (kQueriesInLds) asm volatile("" : "+v"(q_lane));   // read again every time, not kept in registers
         float4v s[RT][4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
 #pragma unroll
             for (int rt = 0; rt < RT; ++rt) s[rt][j] = float4v{0.f, 0.f, 0.f, 0.f};
+        }
+        if constexpr (BY_ROWS) {
+            read_first<64>(ahead, &sm_tile[turn].k[0][0][lane]);
+            products<4 * S::kSteps, 64>(ahead, &sm_tile[turn].k[0][0][lane], [&](int i, const half8v &k) {
 #pragma unroll
-            for (int q = 0; q < S::kSteps; ++q) {
-                const half8v k = k_operand<D>(kw[j], q);
+                for (int rt = 0; rt < RT; ++rt) s[rt][i % 4] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, query(rt, i / 4), s[rt][i % 4], 0, 0, 0);
+            });
+        } else {
 #pragma unroll
-                for (int rt = 0; rt < RT; ++rt) s[rt][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, query(rt, q), s[rt][j], 0, 0, 0);
-            }
+            for (int j = 0; j < 4; ++j)
+#pragma unroll
+                for (int q = 0; q < S::kSteps; ++q) {
+                    const half8v k = k_operand<D>(kw[j], q);
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) s[rt][j] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, query(rt, q), s[rt][j], 0, 0, 0);
+                }
         }
         float x[RT][16], f[RT][2], by[RT];
         bool moved = false;
@@ -495,6 +635,7 @@ __global__ __launch_bounds__(64 * NW, 2) void fp8_attention_kernel(Fp8AttentionA
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
             if (t0 + 32 * half >= hi) break;
+            if constexpr (BY_ROWS) read_first<64>(ahead, &sm_tile[turn].v[half][0][lane]);
             // o is in units of a block's scale.  Blocks of a scale up to 2^6 smaller enter with numerators that are smaller by as much (their
             // fp16 keeps 2^-24 of the reference); others bring o to their unit, up or down, but no further down from the largest scale so far
             // than a binary32 has room for (2^80, beside 2^38 for the sum itself).
@@ -534,7 +675,7 @@ __global__ __launch_bounds__(64 * NW, 2) void fp8_attention_kernel(Fp8AttentionA
             const bool flagged = vs[half] < 0.f;
             if (edge || windowed || flagged) {
                 // what no row of the wave sees must not reach the product, whatever its codes
-                const bool cut = t0 + 32 * half + 32 > hi;
+                const bool cut = !BY_ROWS && t0 + 32 * half + 32 > hi;
                 if (cut) {
 #pragma unroll
                     for (int j = 0; j < 8; ++j)
@@ -554,6 +695,11 @@ __global__ __launch_bounds__(64 * NW, 2) void fp8_attention_kernel(Fp8AttentionA
                             if (OPT && a.in.window > 0) yes = yes && (int64_t)row[rt].pos - pos[t] < a.in.window;
                             see[rt][j] = yes ? (_Float16)1.f : (_Float16)0.f;
                         }
+                    if constexpr (BY_ROWS) {
+                        const uint8_t *v = a.in.c.v_codes + (map.pos(t0) + 32 * half) * D;
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) load_v<D>(vw[8 * half + j], v + (16 * (j >> 2) + (j & 3)) * D, v_off, n);
+                    }
 #pragma unroll
                     for (int w = 0; w < S::kVWords; ++w) {
                         uint32_t mark[8];
@@ -580,6 +726,13 @@ __global__ __launch_bounds__(64 * NW, 2) void fp8_attention_kernel(Fp8AttentionA
                         }
                     }
                 }
+            }
+            if constexpr (BY_ROWS) {
+                products<S::kTiles, 64>(ahead, &sm_tile[turn].v[half][0][lane], [&](int ct, const half8v &f) {
+#pragma unroll
+                    for (int rt = 0; rt < RT; ++rt) o[rt][ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f, pf[rt], o[rt][ct], 0, 0, 0);
+                });
+                continue;
             }
 #pragma unroll
             for (int w = 0; w < S::kVWords; ++w) {
