@@ -367,82 +367,129 @@ __device__ __forceinline__ void store_lse(const Fp8AttentionArgs &a, const Place
     a.lse[((int64_t)p.seq * a.in.c.n_kv_heads * a.in.r + p.kvh * a.in.r + h) * a.in.n_query + i] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
 }
 
-// 64 tokens as operands of both products, for the four waves of a workgroup that walk the same keys: each reads and converts a quarter.
+// 64 tokens as operands of both products, for the four waves of a workgroup that walk the same keys: two read and convert K, two V, half of
+// the tokens each.  (All four with a part of both takes 10 loads each instead of 4 or 8, and the four issue theirs together behind a barrier:
+// 16 cycles of address work per load.)
 template <int D>
 struct Tile {
     half8v k[Shape<D>::kSteps][4][64];   // of 16 tokens each
     half8v v[2][Shape<D>::kTiles][64];   // of 32 tokens each
 };
-// What a wave contributes: K of 16 tokens; V of 32, half of the channels that a lane has (64 channels: all, of which half are used)
+// What a wave reads of them: eight times a piece of a row, at strides that depend on whether it is K or V, so that no branch stands between
+// the loads and a use an iteration later (registers that two branches load into are copied behind them, which waits).
 template <int D>
-struct Quarter {
-    static constexpr int kWords = D == 256 ? 2 : 1;
-    uint32_t k[D / 16], v[8][kWords];
-    float ks[2], vs[2];   // scales of the 64 tokens' halves
-};
-template <int D>
-__device__ __forceinline__ void fetch(Quarter<D> &x, const Fp8View &c, int64_t at, int wave, int n, int g)
-{
-    load_k<D>(x.k, c.k_codes + (at + 16 * wave) * D, n * D + g * (D / 4));
-    const uint8_t *v = c.v_codes + (at + 32 * (wave >> 1)) * D;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        const uint8_t *row = v + (16 * (j >> 2) + (j & 3)) * D;
+struct Share {
+    static constexpr int kV = Shape<D>::kVWords, kK = D / 16;   // words of a row that a lane takes of V, K
+    uint32_t words[8 * kV];   // V [8][kV]; K [2][kK] (96 channels: [2][4] of its words 0 .. 3 and then [2][2] of the rest, V [8] and then [8])
+    float scales;             // of K's and V's halves, in lanes 0 .. 3
+    const uint8_t *from;
+    uint32_t off, step;
+
+    __device__ __forceinline__ Share(const Fp8View &c, int wave, int n, int g)
+    {
+        const bool v = wave >= 2;
+        from = v ? c.v_codes : c.k_codes;
+        off = v ? 4 * g * D + n * (D == 96 ? 4 : D / 16) : n * D + g * (D / 4);
+        step = v ? D : D == 96 ? 4 : 4 * kV;
+    }
+    __device__ __forceinline__ void fetch_scales(const Fp8View &c, int64_t at, int lane)
+    {
+        const int64_t block = (at + 32 * (lane & 1)) >> c.log_block;
+        scales = (lane & 2 ? c.v_scale : c.k_scale)[block];
+    }
+    // piece j of 8; p: place()
+    __device__ __forceinline__ const uint8_t *place(int64_t at, int wave) const { return from + (at + 32 * (wave & 1)) * D; }
+    __device__ __forceinline__ void fetch(const uint8_t *p, int wave, int lane, int j)
+    {
+        const uint8_t *row = p + (16 * (j >> 2) * D + (j & 3) * step);
         if constexpr (D == 96) {
-            if (wave & 1) x.v[j][0] = *reinterpret_cast<const uint16_t *>(row + (4 * g * D + 64 + 2 * n));
-            else x.v[j][0] = *reinterpret_cast<const uint32_t *>(row + (4 * g * D + 4 * n));
-        } else if constexpr (D == 256) {
-            const uint2 w = *reinterpret_cast<const uint2 *>(row + 8 * (wave & 1) + (4 * g * D + 16 * n));
-            x.v[j][0] = w.x;
-            x.v[j][1] = w.y;
+            words[j] = *reinterpret_cast<const uint32_t *>(row + off);
+            // V: the aligned word with channels 64 + 2n and 65 + 2n; K: words 4 and 5 of its tiles, twice
+            const uint8_t *rest = wave >= 2 ? row : p + (16 * ((j >> 1) & 1) * D + 16 + 4 * (j & 1));
+            words[8 + j] = *reinterpret_cast<const uint32_t *>(rest + (wave >= 2 ? off + 64 - 4 * (lane & 15) + 4 * ((lane & 15) >> 1) : off));
+        } else if constexpr (D == 64) {
+            words[j] = *reinterpret_cast<const uint32_t *>(row + off);
+        } else if constexpr (D == 128) {
+            const uint2 w = *reinterpret_cast<const uint2 *>(row + off);
+            words[2 * j] = w.x;
+            words[2 * j + 1] = w.y;
         } else {
-            x.v[j][0] = *reinterpret_cast<const uint32_t *>(row + (D == 64 ? 0 : 4 * (wave & 1)) + (4 * g * D + D / 16 * n));
+            const uint4 w = *reinterpret_cast<const uint4 *>(row + off);
+            words[4 * j] = w.x;
+            words[4 * j + 1] = w.y;
+            words[4 * j + 2] = w.z;
+            words[4 * j + 3] = w.w;
         }
     }
+    __device__ __forceinline__ void fetch_all(const Fp8View &c, int64_t at, int wave, int lane)
+    {
+        fetch_scales(c, at, lane);
+        const uint8_t *p = place(at, wave);
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-        const int64_t block = (at + 32 * h) >> c.log_block;
-        x.ks[h] = scalar_load(c.k_scale + block);
-        x.vs[h] = scalar_load(c.v_scale + block);
+        for (int j = 0; j < 8; ++j) fetch(p, wave, lane, j);
+    }
+    __device__ __forceinline__ void k(int tile, uint32_t (&w)[kK]) const
+    {
+#pragma unroll
+        for (int i = 0; i < kK; ++i) w[i] = D == 96 ? words[i < 4 ? 4 * tile + i : 8 + 2 * tile + i - 4] : words[kK * tile + i];
+    }
+    __device__ __forceinline__ uint32_t v(int j, int w, int lane) const { return D == 96 ? (w ? words[8 + j] >> (16 * (lane & 1)) : words[j]) : words[kV * j + w]; }
+    __device__ __forceinline__ float scale(int i) const { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, scales), i)); }
+};
+// The operands of one word of V of 8 tokens: 4 channels, the first `n` of them
+template <typename STORE>
+__device__ __forceinline__ void v_operands(const uint32_t (&w)[8], int n, const STORE &store)
+{
+#pragma unroll
+    for (int c = 0; c < n; c += 2) {
+        uint32_t pair[4];   // of tokens
+#pragma unroll
+        for (int q = 0; q < 4; ++q) pair[q] = __builtin_amdgcn_perm(w[2 * q + 1], w[2 * q], c ? 0x07030602u : 0x05010400u);
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+            half8v f;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const half2v h = e ? codes_hi(pair[q]) : codes_lo(pair[q]);
+                f[2 * q] = h[0];
+                f[2 * q + 1] = h[1];
+            }
+            store(c + e, f);
+        }
     }
 }
 // left: tokens from the tile's first that exist; codes behind them may be anything, and are not to reach the product
 template <int D>
-__device__ __forceinline__ void lay_down(Tile<D> &to, Quarter<D> &x, int wave, int lane, int g, int left)
+__device__ __forceinline__ void lay_down(Tile<D> &to, const Share<D> &x, int wave, int lane, int left)
 {
+    const int half = wave & 1;
+    if (wave < 2) {
 #pragma unroll
-    for (int s = 0; s < Shape<D>::kSteps; ++s) to.k[s][wave][lane] = k_operand<D>(x.k, s);
-    const int half = wave >> 1, part = wave & 1;
-    if (left < 64 || (half ? x.vs[1] : x.vs[0]) < 0.f) {
-        asm volatile("" : "+v"(g));   // what follows from it is computed here, not kept for the whole loop
+        for (int j = 0; j < 2; ++j) {
+            uint32_t w[D / 16];
+            x.k(j, w);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const bool none = 32 * half + 16 * (j >> 2) + 4 * g + (j & 3) >= left;
-#pragma unroll
-            for (int w = 0; w < Quarter<D>::kWords; ++w) x.v[j][w] = none ? 0u : x.v[j][w] & ~((nan_codes(x.v[j][w]) >> 7) * 0xffu);   // NaN codes have a product of their own
+            for (int s = 0; s < Shape<D>::kSteps; ++s) to.k[s][2 * half + j][lane] = k_operand<D>(w, s);
         }
+        return;
     }
+    const bool clean = left < 64 || x.scale(2 + half) < 0.f;
+    int g = lane >> 4;
+    if (clean) asm volatile("" : "+v"(g));   // what follows from it is computed here, not kept for the whole loop
 #pragma unroll
-    for (int w = 0; w < Quarter<D>::kWords; ++w)
+    for (int w = 0; w < Shape<D>::kVWords; ++w) {
+        uint32_t v[8];
 #pragma unroll
-        for (int b = 0; b < 2; ++b) {   // channels 0, 1 and 2, 3 of the word
-            if (D == 64 && b != part) continue;
-            if (D == 96 && b > 0 && part) continue;
-            uint32_t pair[4];   // of tokens
+        for (int j = 0; j < 8; ++j) v[j] = x.v(j, w, lane);
+        if (clean)
 #pragma unroll
-            for (int q = 0; q < 4; ++q) pair[q] = __builtin_amdgcn_perm(x.v[2 * q + 1][w], x.v[2 * q][w], b ? 0x07030602u : 0x05010400u);
-#pragma unroll
-            for (int c = 0; c < 2; ++c) {
-                half8v f;
-#pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const half2v h = c ? codes_hi(pair[q]) : codes_lo(pair[q]);
-                    f[2 * q] = h[0];
-                    f[2 * q + 1] = h[1];
-                }
-                to.v[half][(D == 64 ? 0 : 4 * (part * Quarter<D>::kWords + w)) + 2 * b + c][lane] = f;
+            for (int j = 0; j < 8; ++j) {
+                // (NaN codes have a product of their own)
+                const bool none = 32 * half + 16 * (j >> 2) + 4 * g + (j & 3) >= left;
+                v[j] = none ? 0u : v[j] & ~((nan_codes(v[j]) >> 7) * 0xffu);
             }
-        }
+        v_operands(v, min(Shape<D>::kTiles - 4 * w, 4), [&](int c, const half8v &f) { to.v[half][4 * w + c][lane] = f; });
+    }
 }
 
 // Operands of products that follow each other, read from LDS four ahead: left to itself, the compiler reads each one just before its product
@@ -545,27 +592,31 @@ __global__ __launch_bounds__(64 * NW, 2) void fp8_attention_kernel(Fp8AttentionA
     const uint32_t k_off = n * D + g * (D / 4), v_off = 4 * g * D + n * (D == 96 ? 4 : D / 16);
     const StreamMap map = a.in.c.map.of(p.stream);
     int first = lo + 64 * wave, last = hi;
-    Quarter<D> quarter;
+    Share<D> share(a.in.c, wave, n, g);
     if constexpr (BY_ROWS) {
         keys_of(group * NW * 16 * RT, (group + 1) * NW * 16 * RT, first, last);
-        if (first < last) fetch<D>(quarter, a.in.c, map.pos(first), wave, n, g);
+        if (first < last) share.fetch_all(a.in.c, map.pos(first), wave, lane);
     }
     for (int t0 = first; t0 < last; t0 += BY_ROWS ? 64 : 64 * NW) {
         uint32_t kw[4][S::kKWords], vw[16][S::kVWords];
         float ks[2], vs[2];
+        int64_t next = 0;
         if constexpr (BY_ROWS) {
             // a tile may be overwritten when all waves are past it: with two of them, that is known from the barrier of the one after it
             if (kTilesInLds == 1) __syncthreads();
             else turn ^= 1;
-            lay_down<D>(sm_tile[turn], quarter, wave, lane, g, last - t0);
+            lay_down<D>(sm_tile[turn], share, wave, lane, last - t0);
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                ks[h] = fabsf(quarter.ks[h]);
-                vs[h] = quarter.vs[h];
+                ks[h] = fabsf(share.scale(h));
+                vs[h] = share.scale(2 + h);
             }
             __syncthreads();
-            if (t0 + 64 < last) fetch<D>(quarter, a.in.c, map.pos(t0 + 64), wave, n, g);
-            if (t0 < lo || t0 >= hi) continue;   // not this wave's rows'
+            next = map.pos(min(t0 + 64, (last - 1) & ~63));   // (behind the last tile: it again)
+            if (t0 < lo || t0 >= hi) {
+                share.fetch_all(a.in.c, next, wave, lane);
+                continue;
+            }   // not this wave's rows'
         } else {
             const int64_t at = map.pos(t0);
 #pragma unroll
@@ -591,10 +642,15 @@ __global__ __launch_bounds__(64 * NW, 2) void fp8_attention_kernel(Fp8AttentionA
             for (int rt = 0; rt < RT; ++rt) s[rt][j] = float4v{0.f, 0.f, 0.f, 0.f};
         }
         if constexpr (BY_ROWS) {
+            // the next tile is requested between the products: 8 loads of four waves at once stand 500 cycles in line for their addresses
+            share.fetch_scales(a.in.c, next, lane);
+            const uint8_t *p_next = share.place(next, wave);
             read_first<64>(ahead, &sm_tile[turn].k[0][0][lane]);
-            products<4 * S::kSteps, 64>(ahead, &sm_tile[turn].k[0][0][lane], [&](int i, const half8v &k) {
+            constexpr int kProducts = 4 * S::kSteps;
+            products<kProducts, 64>(ahead, &sm_tile[turn].k[0][0][lane], [&](int i, const half8v &k) {
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) s[rt][i % 4] = __builtin_amdgcn_mfma_f32_16x16x32_f16(k, query(rt, i / 4), s[rt][i % 4], 0, 0, 0);
+                if ((i + 1) * 8 / kProducts > i * 8 / kProducts) share.fetch(p_next, wave, lane, i * 8 / kProducts);
             });
         } else {
 #pragma unroll
@@ -736,28 +792,13 @@ __global__ __launch_bounds__(64 * NW, 2) void fp8_attention_kernel(Fp8AttentionA
             }
 #pragma unroll
             for (int w = 0; w < S::kVWords; ++w) {
-                uint32_t even[4], odd[4];   // channels 4w, 4w+1 and 4w+2, 4w+3 of token pairs
+                uint32_t v[8];
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    const uint32_t lo2 = vw[8 * half + 2 * q][w], hi2 = vw[8 * half + 2 * q + 1][w];
-                    even[q] = __builtin_amdgcn_perm(hi2, lo2, 0x05010400u);
-                    odd[q] = __builtin_amdgcn_perm(hi2, lo2, 0x07030602u);
-                }
+                for (int j = 0; j < 8; ++j) v[j] = vw[8 * half + j][w];
+                v_operands(v, min(S::kTiles - 4 * w, 4), [&](int c, const half8v &f) {
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    const int ct = 4 * w + c;
-                    if (ct >= S::kTiles) break;
-                    half8v f;
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const uint32_t word = c < 2 ? even[q] : odd[q];
-                        const half2v h = c & 1 ? codes_hi(word) : codes_lo(word);
-                        f[2 * q] = h[0];
-                        f[2 * q + 1] = h[1];
-                    }
-#pragma unroll
-                    for (int rt = 0; rt < RT; ++rt) o[rt][ct] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f, pf[rt], o[rt][ct], 0, 0, 0);
-                }
+                    for (int rt = 0; rt < RT; ++rt) o[rt][4 * w + c] = __builtin_amdgcn_mfma_f32_16x16x32_f16(f, pf[rt], o[rt][4 * w + c], 0, 0, 0);
+                });
             }
         }
     }
