@@ -10,8 +10,9 @@
 // queries in two or three e4m3 terms, would save K's conversion but not V's, which needs the numerators in as many terms.)
 //
 // One token over long caches is bound by HBM (16 sequences x 32k tokens, 8 KV heads of 128 channels: 185 us, 5.8 TB/s, where a plain
-// read reaches 5.5), many rows by instruction issue (1024 queries of 32 heads over 16k tokens: 385 us, 0.70 PFLOP/s: per 64 tokens
-// and 32 rows 64 matrix instructions beside about 390 vector ones, 128 of them conversions of codes and 32 exponentials).
+// read reaches 5.5), many rows by what a wave can issue beside its matrix instructions (1024 queries of 32 heads over 16k tokens: 331 us, 0.81
+// PFLOP/s; 656 with 256 channels, 0.82.  Per 64 tokens and 32 rows 64 matrix instructions beside about 290 vector ones, 32 of them exponentials).
+// There the operands of a tile are converted once for four waves and lie in LDS (each wave converting for itself: 385 us, and 1121 with 256 channels).
 #include "pk_fp8.h"
 
 namespace pk {
@@ -1145,11 +1146,12 @@ __global__ __launch_bounds__(kThreads, 2) void fp8_weights_kernel(Fp8WeightsArgs
     }
 }
 
-// How many rows a workgroup of the attention takes, and how: up to 128 its waves share one or two tiles of rows and deal out the keys (32 rows
-// over one sequence of 16k tokens 27 us and with rows of their own 34, 128 rows 31 and 41; 32 sequences of 700 to 6000 tokens, 128 rows 126 and
-// 138); with more every wave has rows of its own, and keys are read and converted for 32 rows of each of four waves (256 rows, one
-// sequence: 47 us both ways).  Two tiles from 17 rows on, as K and V are converted once for both (32 sequences, 20 rows 67 us, in two groups of
-// one tile 81); at 256 channels the registers hold one.
+// How many rows a workgroup of the attention takes, and how.  Up to 128 channels: two tiles of 16 from 17 rows on, as K and V are converted once
+// for both (32 sequences, 20 rows 67 us, in two groups of one tile 81).  Up to 256 rows the waves share them and deal out the keys, with more
+// every wave has rows of its own and the keys lie in LDS (one sequence of 16k tokens: 128 rows 31 us against 41 with rows of their own, 256 rows 41
+// and 47, 1024 rows 126 and 101; 32 sequences of 700 to 6000 tokens: 128 rows both 128, 256 rows 215 and 209; 64 channels, 256 rows 30 and 35).
+// At 256 channels the registers hold one tile, and sharing the conversions counts from the second on (the same 32 sequences, 32 rows 166 and 122
+// us, 256 rows 636 and 372; one sequence, 32 rows over 16k tokens 33 and 35, 20 rows over 2k 33 and 19).
 struct Rows {
     int tiles;      // per wave (RT)
     bool by_rows;
@@ -1158,7 +1160,7 @@ struct Rows {
 Rows rows_of(int64_t rows, int d)
 {
     Rows x;
-    x.by_rows = rows > 128;
+    x.by_rows = rows > (d == 256 ? 16 : 256);
     x.tiles = d == 256 || rows <= 16 ? 1 : 2;
     x.per_group = 16 * x.tiles * (x.by_rows ? kWaves : 1);
     return x;

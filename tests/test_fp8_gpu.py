@@ -262,6 +262,23 @@ def test_attention_and_weights(pk, lengths, n, r, d, block, bf16, page, how, cap
     p.attend(n, counts=[n, n // 2, 0, max(n - 1, 0)], weights=True, bound=64, **how)   # a bound below the lengths costs time only
 
 
+@pytest.mark.parametrize("cap", [1024, 4096])
+@pytest.mark.parametrize("n,r,d,block,bf16,page,how", [
+    (90, 3, 96, 32, True, 128, dict(cap=5.0)), (100, 3, 96, 64, False, 0, {}), (300, 1, 64, 64, False, 128, {}), (131, 2, 128, 32, True, 128, dict(window=100, slopes=True)),
+    (65, 5, 128, 128, False, 0, {}), (65, 4, 128, 64, True, 0, dict(window=1)), (9, 2, 256, 32, True, 128, {}), (33, 2, 256, 128, False, 0, dict(window=50, cap=10.0))])
+def test_many_rows_share_the_keys(pk, n, r, d, block, bf16, page, how, cap):
+    """Waves with rows of their own over tiles in LDS: some of the waves without rows or keys, more queries than tokens, one tile and
+    several, NaN in a tile that only some rows see, and counts that leave whole workgroups nothing."""
+    lengths = [1, 333, 64, 1000]
+    p = Pair(pk, 23, n_seq=4, hkv=2, r=r, d=d, block=block, cap=cap, bf16=bf16, page=page, spread=0.5)
+    k, v = p.vectors(1000, 2), p.vectors(1000, 2)
+    v[0][1, 1, 330, 7] = v[0][3, 0, 995, d - 1] = v[0][3, 1, 500, 3] = math.nan
+    k, v = (k[0], k[0].double().cpu().numpy()), (v[0], v[0].double().cpu().numpy())
+    p.append(1000, counts=lengths, k=k, v=v)
+    p.attend(n, weights=False, **how)
+    p.attend(n, weights=False, counts=[n, 1, 0, max(n - 1, 0)], **how)
+
+
 @pytest.mark.parametrize("cap", [256, 4096])
 def test_empty_sequences(pk, cap):
     """Nothing held, and more queries than tokens: no row sees anything, or only the last do.  No queries, no new vectors."""
