@@ -657,7 +657,8 @@ def pk_fp8_attention(cfg: Fp8Config, cache: Fp8Cache, q: torch.Tensor, softmax_s
 def pk_fp8_weights(cfg: Fp8Config, cache: Fp8Cache, q: torch.Tensor, lse: torch.Tensor, softmax_scale: float, cap: float = 0.0, window: int = 0,
                    slopes: torch.Tensor | None = None, counts: torch.Tensor | None = None, bound: int | None = None, accumulate: bool = True):
     """Add (accumulate=False: set) the attention weight that every cached token got from the queries of a pk_fp8_attention call, whose
-    arguments and lse these are, in cache.buf["weight"] [n_seq, n_kv_heads, t_capacity]."""
+    arguments and lse these are, in cache.buf["weight"] [n_seq, n_kv_heads, t_capacity].  An lse that is not contiguous is copied."""
+    lse = lse.contiguous()
     if q.dim() == 3:
         q = q.unsqueeze(2)
     qs = _fp8_vectors(cfg, cache, q, cfg.n_q_heads, "q")

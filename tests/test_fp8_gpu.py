@@ -279,6 +279,24 @@ def test_many_rows_share_the_keys(pk, n, r, d, block, bf16, page, how, cap):
     p.attend(n, weights=False, counts=[n, 1, 0, max(n - 1, 0)], **how)
 
 
+def test_lse_in_another_order(pk):
+    """A log-sum-exp that lies query by query, as a softmax over the heads of one KV head leaves it, gives the same weights."""
+    p = Pair(pk, 24, n_seq=2, hkv=1, r=16, cap=512)
+    p.append(300, counts=[300, 77])
+    q, _ = p.vectors(9, 16)
+    lse = torch.empty(2, 16, 9, device="cuda")
+    pk.pk_fp8_attention(p.cfg, p.cache, q, 0.1, lse=lse)
+    pk.pk_fp8_weights(p.cfg, p.cache, q, lse, 0.1, accumulate=False)
+    want = p.cache.buf["weight"].clone()
+    turned = lse.transpose(1, 2).contiguous().transpose(1, 2)
+    assert not turned.is_contiguous()
+    pk.pk_fp8_weights(p.cfg, p.cache, q, turned, 0.1, accumulate=False)
+    held = [want.view(2, -1)[b, :n] for b, n in enumerate((300, 77))]
+    assert all(torch.equal(x, p.cache.buf["weight"].view(2, -1)[b, :len(x)]) for b, x in enumerate(held))
+    with pytest.raises(ValueError):
+        pk.pk_fp8_weights(p.cfg, p.cache, q, lse.transpose(1, 2), 0.1)
+
+
 @pytest.mark.parametrize("cap", [256, 4096])
 def test_empty_sequences(pk, cap):
     """Nothing held, and more queries than tokens: no row sees anything, or only the last do.  No queries, no new vectors."""
