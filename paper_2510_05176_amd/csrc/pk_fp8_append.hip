@@ -59,8 +59,11 @@ __global__ __launch_bounds__((AppendShape<D, B>::kThreads)) void fp8_append_kern
     const int head = blockIdx.x % hkv, rest = blockIdx.x / hkv;
     const int side = NS == 2 ? 0 : rest & 1, blk = NS == 2 ? rest : rest >> 1;   // the first side of the workgroup: 0 K, 1 V
     int2 st = fp8_state(a.states, seq, a.c.t_capacity);
-    // the state may be replaced by this very launch once every workgroup of the sequence has read it: no second load
+    // the state may be replaced by this very launch once every wave of the sequence's workgroups has read it: no second load
     asm volatile("" : "+v"(st.x), "+v"(st.y));
+    // nor a late one: one wave reports for its workgroup below, and a workgroup without a block has no other barrier before that.  (A wave that read
+    // the grown state could take itself for one with a block, and write vectors behind the sequence's last into whatever page is named there.)
+    __syncthreads();
     const int len = __builtin_amdgcn_readfirstlane(st.x), next = __builtin_amdgcn_readfirstlane(st.y);
     const int count = min(fp8_count(a.counts, seq, a.n_new), a.c.t_capacity - len);
     const int t0 = (len / B + blk) * B, end = len + count;
@@ -150,7 +153,7 @@ __global__ __launch_bounds__((AppendShape<D, B>::kThreads)) void fp8_append_kern
     }
     if (tid != 0) return;
     // The state afterwards: from one workgroup where it has a place of its own, else from the sequence's last one to come here, as
-    // the others have read the old one by then (a wave is here only with what it read in hand: its branches above need it).
+    // the others have read the old one by then, every wave of them (the barrier behind the load).
     int32_t *out = a.states_out + 4 * (int64_t)seq;
     if (a.states_out != a.states) {
         if (blockIdx.x == 0) *reinterpret_cast<int4 *>(out) = make_int4(len + count, next + count, 0, 0);

@@ -225,6 +225,26 @@ def test_append_beside_the_old_states(pk):
     p.check()
 
 
+@pytest.mark.parametrize("d,block", [(128, 64), (96, 32), (256, 128), (64, 128)])
+def test_append_leaves_pages_behind_the_tokens_alone(pk, d, block):
+    """Appends in place whose launch has workgroups without a block of vectors; the entries of the page table behind a sequence's last page
+    name pages of its neighbour, as a table does where pages are given out on demand.  The neighbours' codes, scales, positions and
+    weights stay as they are."""
+    page, n_seq, hkv = 128, 16, 2
+    p = Pair(pk, 25, n_seq=n_seq, hkv=hkv, d=d, block=block, cap=1024, page=page)
+    own = torch.arange(n_seq * 2, dtype=torch.int32, device="cuda").view(n_seq, 2)         # two pages of its own each
+    p.cache.page_table.copy_(torch.cat([own, own.roll(-1, 0).repeat(1, 3)], 1))
+    rng = np.random.default_rng(7)
+    start = [int(x) for x in rng.integers(0, 2 * block, n_seq)]
+    p.append(max(start), counts=start)
+    for n in (2, 3, 5, 17, block // 2 + 1, block - 2):
+        room = [2 * page - s.length for s in p.seqs]
+        p.append(n, counts=[min(int(x), r) for x, r in zip(rng.integers(0, n + 1, n_seq), room)])
+        p.check()
+    p.append(150, counts=[min(int(x), 2 * page - s.length) for x, s in zip(rng.integers(0, 30, n_seq), p.seqs)])
+    p.check()
+
+
 ATTENDS = [
     # lengths, n, r, d, block, bf16, page, options
     ([1, 5, 64, 65], 1, 4, 128, 64, False, 0, {}),

@@ -80,3 +80,49 @@ def test_vector_results_are_not_read_too_early(tmp_path):
         total = {k: total.get(k, 0) + n for k, n in seen.items()}
     assert all(total.values()), total
     assert not bad, (len(bad), bad[:4])
+
+
+def _arrives_without_a_barrier(asm):
+    """Of every kernel in the listing (branch targets as labels): whether an atomic on memory can be reached from its start past no barrier."""
+    out = {}
+    for name, body in re.findall(r"^[0-9a-f]* ?<([^>]*)>:\n(.*?)(?=^[0-9a-f]* ?<_Z|\Z)", asm, re.M | re.S):
+        lines = [x.split("//")[0].strip() for x in body.splitlines()]
+        label = {m.group(1): i for i, x in enumerate(lines) if (m := re.match(r"^[0-9a-f]* ?<(L\d+)>:", x))}
+        todo, seen, out[name] = [0], set(), False
+        while todo:
+            i = todo.pop()
+            if i in seen or i >= len(lines):
+                continue
+            seen.add(i)
+            op, _, to = lines[i].partition(" ")
+            assert not op.startswith(("s_setpc", "s_swappc", "s_call")), lines[i]
+            out[name] |= op.startswith(("global_atomic", "flat_atomic", "buffer_atomic"))
+            if op == "s_barrier" or op == "s_endpgm":
+                continue
+            if op.startswith(("s_cbranch", "s_branch")):
+                todo.append(label[to.strip()])
+            if op != "s_branch":
+                todo.append(i + 1)
+    return out
+
+
+def test_the_check_sees_a_missing_barrier():
+    head = "0 <_Zkernel>:\n s_load_dword s2, s[0:1], 0x0\n s_cbranch_scc0 L0\n s_barrier\n s_branch L1\n0 <L0>:\n v_nop\n%s0 <L1>:\n global_atomic_add v0, v1, v2, s[0:1]\n s_endpgm\n"
+    assert _arrives_without_a_barrier(head % "") == {"_Zkernel": True}
+    assert _arrives_without_a_barrier(head % " s_barrier\n") == {"_Zkernel": False}
+
+
+def test_append_counts_a_workgroup_when_all_its_waves_have_the_state(tmp_path):
+    """An append in place replaces the state that its launch reads, once every workgroup of the sequence is counted as arrived.  One wave counts
+    for its workgroup, so on every way there, with a block of vectors or without one, it passes a barrier behind the loads of the
+    others (64 channels in blocks of 32 tokens have workgroups of one wave)."""
+    shutil.copy(LIB, tmp_path / "lib.so")
+    subprocess.run([OBJDUMP, "--offloading", "lib.so"], cwd=tmp_path, check=True, capture_output=True)
+    found = {}
+    for f in sorted(os.listdir(tmp_path)):
+        if f.endswith("gfx950") and b"fp8_append_kernel" in (tmp_path / f).read_bytes():
+            r = subprocess.run([OBJDUMP, "-d", "--mcpu=gfx950", "--no-show-raw-insn", "--symbolize-operands", f], cwd=tmp_path, check=True,
+                               capture_output=True, text=True)
+            found.update({k: v for k, v in _arrives_without_a_barrier(r.stdout).items() if "fp8_append_kernel" in k})
+    assert len(found) == 24
+    assert [k for k, v in found.items() if v and "ILi64ELi32E" not in k] == []
