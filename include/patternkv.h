@@ -495,7 +495,8 @@ pk_status pk_fp8_attention(const pk_fp8_config *cfg, const pk_fp8_cache *cache, 
 /*
  * The attention weight of every cached token: weight[n][t] (+)= sum over the query heads of the KV head and the query tokens of
  * exp(s - lse), the softmax weight that pk_fp8_attention gave it.  Arguments as there; lse as it returned them (a row whose lse
- * is -inf adds nothing).  accumulate == 0: the weights of the tokens held are set instead.  Needs cache->weight.
+ * is -inf adds nothing; where it is NaN, the tokens that the row sees get NaN and the others nothing).  accumulate == 0: the
+ * weights of the tokens held are set instead.  Needs cache->weight.
  * Sums are formed in a fixed order: results are reproducible bit for bit.
  */
 pk_status pk_fp8_weights(const pk_fp8_config *cfg, const pk_fp8_cache *cache, const int32_t *states, int32_t bound, const void *q,

@@ -1036,11 +1036,17 @@ __global__ __launch_bounds__(kThreads, 2) void fp8_weights_kernel(Fp8WeightsArgs
                 half8v qf[S::kSteps];
                 Row row = row_of(a.in, p, at);
                 load_query<D>(qf, row.factor, a.in, p.seq, p.kvh, at, at < rows, g);
-#pragma unroll
-                for (int s = 0; s < S::kSteps; ++s) sm_q[tile][s][lane] = qf[s];
                 const int i = at / a.in.r, h = at - i * a.in.r;
                 float lse = INFINITY;
                 if (at < rows) lse = a.lse[((int64_t)p.seq * hkv * a.in.r + p.kvh * a.in.r + h) * a.in.n_query + i];
+                // a NaN becomes the row's products', so that only tokens that it sees get it: -inf - NaN would be one for all of them
+                const bool none = lse != lse;
+                if (none) lse = 0.f;
+#pragma unroll
+                for (int s = 0; s < S::kSteps; ++s) {
+                    if (none) qf[s][0] = (_Float16)__builtin_nanf("");
+                    sm_q[tile][s][lane] = qf[s];
+                }
                 if (lse == -INFINITY) {   // a row that saw nothing adds nothing
                     lse = INFINITY;
                     row.last = -1;

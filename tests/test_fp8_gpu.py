@@ -317,6 +317,59 @@ def test_lse_in_another_order(pk):
         pk.pk_fp8_weights(p.cfg, p.cache, q, lse.transpose(1, 2), 0.1)
 
 
+def nan_rows(pk, seed, n, d, bf16, cap, n_seq=2):
+    """Sequences of 300 and 290 tokens; of the queries one is NaN, one infinite; a key that only the last queries see is NaN."""
+    p = Pair(pk, seed, n_seq=n_seq, hkv=2, r=2, d=d, cap=cap, bf16=bf16, spread=0.3)
+    k, v = p.vectors(300, 2), p.vectors(300, 2)
+    k[0][1, 1, 288, 5] = math.nan
+    p.append(300, counts=[300, 290], k=(k[0], k[0].double().cpu().numpy()), v=v)
+    q, _ = p.vectors(n, 4)
+    q[0, 1, 1, 3], q[1, 0, 0, d - 1], q[0, 2, n // 2, :] = math.nan, math.nan, math.inf
+    return p, q, q.double().cpu().numpy()
+
+
+@pytest.mark.parametrize("cap", [512, 4096])
+@pytest.mark.parametrize("n,how", [(5, {}), (5, dict(window=40)), (80, {}), (80, dict(window=100, slopes=True)), (80, dict(cap=20.0))])
+@pytest.mark.parametrize("d,bf16", [(128, False), (96, True)])
+def test_weights_of_rows_without_a_result(pk, n, how, d, bf16, cap):
+    """A row whose log-sum-exp is NaN (its query, or a key that it sees, is) gives NaN to the tokens that it sees, and nothing to the others."""
+    p, q, qn = nan_rows(pk, 26, n, d, bf16, cap)
+    how = dict(how)
+    slopes = torch.exp2(-torch.arange(1, 5, device="cuda").float()) if how.pop("slopes", False) else None
+    lse = torch.empty(2, 4, n, device="cuda")
+    pk.pk_fp8_attention(p.cfg, p.cache, q, 0.1, lse=lse, slopes=slopes, **how)
+    for add in (False, True):
+        pk.pk_fp8_weights(p.cfg, p.cache, q, lse, 0.1, slopes=slopes, accumulate=add, **how)
+    got = p.cache.buf["weight"].double().cpu().numpy().reshape(2, 2, -1)
+    partly = 0
+    for b, s in enumerate(p.seqs):
+        with np.errstate(invalid="ignore"):
+            x, size = s.scores(qn[b], 0.1, slopes=None if slopes is None else slopes.double().cpu().numpy(), **how)
+        for h in range(2):
+            want, room = np.zeros(s.length), np.zeros(s.length)
+            for row in range(2 * h, 2 * h + 2):
+                for i in range(n):
+                    seen = x[row, i] != -np.inf
+                    if np.isnan(lse[b, row, i].item()):
+                        assert not np.isfinite(x[row, i][seen]).all()
+                        want[seen] = math.nan
+                        continue
+                    assert np.isfinite(x[row, i][seen]).all()
+                    top = x[row, i][seen].max()
+                    total = top + np.log(np.exp(x[row, i][seen] - top).sum())
+                    w = np.exp(x[row, i] - total)
+                    want += 2 * w
+                    # the scores' roundings in the weight and in the sum, the log-sum-exp's own
+                    room += 2 * w * (2 * (d + 8) * 2.0 ** -24 * size[row, i] + s.length * 2.0 ** -24 + 2.0 ** -21 * (abs(total) + 4) + 2.0 ** -24 * (4 * n + 8))
+            have = got[b, h, :s.length]
+            assert np.isnan(want).any()
+            partly += not np.isnan(want).all()
+            assert np.array_equal(np.isnan(have), np.isnan(want)), (b, h, np.argwhere(np.isnan(have) != np.isnan(want))[:4])
+            ok = ~np.isnan(want)
+            assert (np.abs(have - want)[ok] <= room[ok] + 1e-37).all(), (b, h)
+    assert partly >= 3
+
+
 @pytest.mark.parametrize("cap", [256, 4096])
 def test_empty_sequences(pk, cap):
     """Nothing held, and more queries than tokens: no row sees anything, or only the last do.  No queries, no new vectors."""
