@@ -874,14 +874,15 @@ __global__ __launch_bounds__(64 * NW, 2) void fp8_attention_kernel(Fp8AttentionA
                     float top = -INFINITY;
                     for (int w = 0; w < NW; ++w) top = fmaxf(top, sm_m[w][q]);
                     const float ref = top == -INFINITY ? 0.f : top;
-                    float sum = 0.f, y[4] = {0.f, 0.f, 0.f, 0.f};
+                    float sum = 0.f, share[NW], y[4] = {0.f, 0.f, 0.f, 0.f};
                     for (int w = 0; w < NW; ++w) {
-                        const float share = sm_l[w][q] * exp2_(sm_m[w][q] - ref);
-                        sum += share;
-                        for (int i = 0; i < 4; ++i) y[i] = fmaf(share, sm_o[w][q][c + i], y[i]);
+                        share[w] = sm_l[w][q] * exp2_(sm_m[w][q] - ref);
+                        sum += share[w];
                     }
+                    // parts of 1: a sum of many results near a binary32's largest need not be one, though their mean is
                     const float inv = sum == 0.f ? 0.f : 1.f / sum;
-                    for (int i = 0; i < 4; ++i) y[i] *= inv;
+                    for (int w = 0; w < NW; ++w)
+                        for (int i = 0; i < 4; ++i) y[i] = fmaf(share[w] * inv, sm_o[w][q][c + i], y[i]);
                     if (whole) {
                         store_row<D>(a, p, at, c, y, 4);
                         if (c == 0) store_lse(a, p, at, top, sum);
@@ -931,21 +932,26 @@ __global__ __launch_bounds__(64 * kMergeRows) void fp8_merge_kernel(Fp8Attention
     float top = -INFINITY, sum = 0.f, y[kPer];
 #pragma unroll
     for (int i = 0; i < kPer; ++i) y[i] = 0.f;
-    for (int s0 = 0; s0 < pieces; s0 += 64) {
-        float2 ml = make_float2(-INFINITY, 0.f);
+    float2 ml;   // of the lane's piece
+    const auto load_ml = [&](int s0) {
+        ml = make_float2(-INFINITY, 0.f);
         if (s0 + lane < pieces) ml = *reinterpret_cast<const float2 *>(a.part_ml + 2 * (first + (s0 + lane) * step));
+    };
+    for (int s0 = 0; s0 < pieces; s0 += 64) {
+        load_ml(s0);
         const float most_of_row[1] = {row_max(ml.x)};
         const float most = fold_rows(most_of_row, MaxF());
         if (most > top) {
-            const float by = exp2_(top - most);
+            sum *= exp2_(top - most);
             top = most;
-            sum *= by;
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) y[i] *= by;
         }
-        const float share = ml.y * exp2_(ml.x - (top == -INFINITY ? 0.f : top));
-        const float sum_of_row[1] = {row_sum(share)};
+        const float sum_of_row[1] = {row_sum(ml.y * exp2_(ml.x - (top == -INFINITY ? 0.f : top)))};
         sum += fold_rows(sum_of_row, AddF());
+    }
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    for (int s0 = 0; s0 < pieces; s0 += 64) {
+        if (pieces > 64) load_ml(s0);
+        const float share = ml.y * exp2_(ml.x - (top == -INFINITY ? 0.f : top)) * inv;   // parts of 1, as above
         const int here = min(pieces - s0, 64);
         for (int s = 0; s < here; s += kTogether) {
             float v[kTogether][kPer];
@@ -973,9 +979,6 @@ __global__ __launch_bounds__(64 * kMergeRows) void fp8_merge_kernel(Fp8Attention
             }
         }
     }
-    const float inv = sum == 0.f ? 0.f : 1.f / sum;
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) y[i] *= inv;
     if (lane * kPer < D) store_row<D>(a, p, row, c, y, kPer);
     if (lane == 0) store_lse(a, p, row, top, sum);
 }

@@ -458,6 +458,38 @@ def test_value_scales_of_every_size(pk, bf16, cap):
     p.attend(1, q=q)
 
 
+def attend_closely(p, n, q, scale=None, **how):
+    """The attention against the definition where a bound by the largest value would say nothing: a numerator is off by 2^-11 of itself or by
+    2^-36 of the row's largest (2^6 more where its block's scale of V is up to 2^6 smaller), sums by the roundings of 1024 additions."""
+    scale = p.cfg.head_dim ** -0.5 if scale is None else scale
+    sl = torch.exp2(-torch.arange(1, p.cfg.n_q_heads + 1, device="cuda").float()) if how.pop("slopes", False) else None
+    lse = torch.empty(p.cfg.n_seq, p.cfg.n_q_heads, n, device="cuda")
+    got = p.pk.pk_fp8_attention(p.cfg, p.cache, q[0], scale, lse=lse, slopes=sl, **how).double().cpu().numpy()
+    lse = lse.double().cpu().numpy()
+    r = p.cfg.n_q_heads // p.cfg.n_kv_heads
+    for b, s in enumerate(p.seqs):
+        want, want_lse, soft, mag, size = s.attention(q[1][b], scale, slopes=None if sl is None else sl.double().cpu().numpy(), **how)
+        off = (p.cfg.head_dim + 8) * 2.0 ** -24 * size
+        small = np.minimum(soft, 2.0 ** -30 * soft.max(2, keepdims=True))
+        lost = np.stack([small[h] @ np.abs(s.v[h // r].values()) for h in range(p.cfg.n_q_heads)])
+        tol = EPS[p.dtype] * np.abs(want) + (2.0 ** -11 + 2.0 ** -14 + 2 * off[..., None]) * mag + lost + 2.0 ** -25 * (p.dtype == torch.float16)
+        # a bound that could fail: a hundredth of the result in most places
+        assert np.median(tol / np.abs(want)) < 0.01, np.median(tol / np.abs(want))
+        bad = ~(np.abs(got[b] - want) <= tol)
+        assert not bad.any(), (b, np.argwhere(bad)[:4], (np.abs(got[b] - want) / tol)[bad][:4])
+        assert (np.abs(lse[b] - want_lse) <= off + 2.0 ** -14 + 2.0 ** -22 * (np.abs(want_lse) + 2)).all(), b
+
+
+@pytest.mark.parametrize("d,n", [(64, 1), (128, 200), (256, 3)])
+def test_values_near_the_largest(pk, d, n):
+    """Values up to a quarter of bfloat16's largest: the weighted mean of many of them is finite, though their sum is not."""
+    p = Pair(pk, 29, n_seq=1, hkv=1, r=2, d=d, cap=8192, bf16=True, spread=0.0)
+    k, v = p.vectors(8000, 1), p.vectors(8000, 1)
+    v[0].abs_().clamp_(max=3.0).add_(1.0).mul_(2.0 ** 124)
+    p.append(8000, k=k, v=(v[0], v[0].double().cpu().numpy()))
+    attend_closely(p, n, p.vectors(n, 2))
+
+
 EVICTS = [(128, 64, 0, 0, 100, 4, 16), (64, 32, 128, 0, 64, 0, 0), (96, 32, 0, 128, 77, 0, 77), (256, 128, 256, 128, 129, 1, 0), (128, 64, 0, 0, 1, 0, 0), (64, 64, 0, 0, 63, 31, 32)]
 
 
