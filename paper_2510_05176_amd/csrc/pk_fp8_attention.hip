@@ -365,7 +365,10 @@ __device__ __forceinline__ void store_lse(const Fp8AttentionArgs &a, const Place
 {
     if (!a.lse) return;
     const int i = row / a.in.r, h = row - i * a.in.r;
-    a.lse[((int64_t)p.seq * a.in.c.n_kv_heads * a.in.r + p.kvh * a.in.r + h) * a.in.n_query + i] = l == 0.f ? -INFINITY : (m + log2f(l)) * kLn2;
+    // l's power of two joins the reference first: their sum is small where the log-sum-exp is, and takes no rounding of l's whole logarithm
+    int e;
+    const float part = frexpf(l, &e);
+    a.lse[((int64_t)p.seq * a.in.c.n_kv_heads * a.in.r + p.kvh * a.in.r + h) * a.in.n_query + i] = l == 0.f ? -INFINITY : (m + (float)e + log2f(part)) * kLn2;
 }
 
 // 64 tokens as operands of both products, for the four waves of a workgroup that walk the same keys: two read and convert K, two V, half of
@@ -579,11 +582,11 @@ __global__ __launch_bounds__(64 * NW, 2) void fp8_attention_kernel(Fp8AttentionA
     const int pos_most = p.next - p.count + min((row0 + 16 * RT - 1) / a.in.r, p.count - 1);
     const int32_t *pos = OPT && (a.in.slopes || a.in.window > 0) ? a.in.c.pos + (int64_t)p.stream * a.in.c.t_capacity : nullptr;
 
-    float m[RT], l[RT];
+    float m[RT], m_most[RT], l[RT];   // the numerators' reference, the largest score that it serves, the numerators' sum
     float4v o[RT][S::kTiles];
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-        m[rt] = -INFINITY;
+        m[rt] = m_most[rt] = -INFINITY;
         l[rt] = 0.f;
 #pragma unroll
         for (int ct = 0; ct < S::kTiles; ++ct) o[rt][ct] = float4v{0.f, 0.f, 0.f, 0.f};
@@ -680,11 +683,15 @@ __global__ __launch_bounds__(64 * NW, 2) void fp8_attention_kernel(Fp8AttentionA
             }
             const float one[1] = {most};
             most = fold_rows(one, MaxF());
-            // the reference moves when a score is far above it: numerators stay below 2^4 and need no other care
+            // The reference moves when a score is far above the last ones: to 2^11 below it, so that numerators stay below 2^15 and fp16's smallest step is
+            // 2^-35 of the largest or less (2^-24 of it, with the reference at the score, leaves nothing of many tokens of 2^-26 each).
+            // Scores of 2^20 and more, whose own steps are large, are the reference themselves.
             by[rt] = 1.f;
-            if (most > m[rt] + 4.f) {
-                by[rt] = exp2_(m[rt] - most);
-                m[rt] = most;
+            if (most > m_most[rt]) {
+                m_most[rt] = most + 4.f;
+                const float to = fabsf(most) < 0x1p20f ? most - 11.f : most;
+                by[rt] = exp2_(m[rt] - to);
+                m[rt] = to;
                 l[rt] *= by[rt];
             }
             moved |= by[rt] != 1.f;
@@ -693,18 +700,18 @@ __global__ __launch_bounds__(64 * NW, 2) void fp8_attention_kernel(Fp8AttentionA
         for (int half = 0; half < 2; ++half) {
             if (t0 + 32 * half >= hi) break;
             if constexpr (BY_ROWS) read_first<64>(ahead, &sm_tile[turn].v[half][0][lane]);
-            // o is in units of a block's scale.  Blocks of a scale up to 2^6 smaller enter with numerators that are smaller by as much (their
-            // fp16 keeps 2^-24 of the reference); others bring o to their unit, up or down, but no further down from the largest scale so far
-            // than a binary32 has room for (2^80, beside 2^38 for the sum itself).
+            // o is in units of a block's scale.  Blocks of a scale up to 2^6 smaller enter with numerators that are smaller by as much (a power of two,
+            // which costs bits only below 2^-19 of the largest numerator); others bring o to their unit, up or down, but no further down from the
+            // largest scale so far than a binary32 has room for (2^68, beside 2^49 for the sum itself).
             const int field = field_of_scale(vs[half]);
             int shift = 0;
             if (field > unit || field < unit - 6) {
                 unit_most = max(unit_most, field);
-                const int to = max(field, unit_most - 80);
+                const int to = max(field, unit_most - 68);
                 shift = unit - to;
                 unit = to;
             }
-            const int fold = min(unit - field, 60);   // from 29 on fp16 leaves nothing of the numerators
+            const int fold = min(unit - field, 60);   // from 40 on fp16 leaves nothing of the numerators
             if (half == 0 ? shift != 0 || __any(moved) : shift != 0) {
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) {

@@ -458,6 +458,39 @@ def test_value_scales_of_every_size(pk, bf16, cap):
     p.attend(1, q=q)
 
 
+@pytest.mark.parametrize("bf16", [False, True])
+@pytest.mark.parametrize("d,r,n,how", [(64, 1, 1, {}), (64, 4, 1, dict(cap=1e6)), (128, 1, 1, dict(window=1 << 20)), (64, 3, 9, {}), (64, 1, 300, {}), (256, 2, 9, {}), (64, 64, 512, {})])
+def test_many_tokens_of_little_weight(pk, d, r, n, how, bf16):
+    """One token with all but the weight of 2^19 others, each 2^-26 of it: in channels where that token has nothing the result is theirs.  A
+    numerator is off by 2^-11 of itself, or by half of fp16's smallest step, 2^-36 of the largest numerator."""
+    T, count = (1 << 19) + 70, (1 << 19)
+    cfg = pk.Fp8Config(n_seq=1, n_kv_heads=1, n_q_heads=r, head_dim=d, t_capacity=(1 << 19) + 128, dtype=pk.DTYPE_BF16 if bf16 else pk.DTYPE_FP16)
+    cache = pk.Fp8Cache(cfg, track_weight=False)
+    for first in (0, 64 * 5000 + 7):      # where the token is
+        cache.states.zero_()
+        k = torch.zeros((1, 1, T, d), dtype=cfg.torch_dtype, device="cuda")
+        v = torch.ones_like(k)
+        k[0, 0, first, 0] = 18.0
+        v[0, 0, first, : d // 2] = 0.0
+        v[0, 0, :, 1] *= 208.0
+        pk.pk_fp8_append(cfg, cache, k, v)
+        q = torch.zeros((1, r, n, d), dtype=cfg.torch_dtype, device="cuda")
+        q[..., 0] = 1.0
+        out = pk.pk_fp8_attention(cfg, cache, q, 1.0, **how).double().cpu().numpy()[0]
+        # the capped score: 18 - 18^3 / 3e12 and less
+        for i in range(n):
+            small = (T - n + i) * math.exp(-18.0)
+            want = np.ones(d)
+            want[:d // 2] = small / (1 + small)
+            want[1] *= 208.0
+            # bounds: the score's rounding (18 in units of log2 e: 26, three roundings), the numerators', the sum's over runs of at most
+            # 2^13 tokens, the result's
+            rel = EPS[cfg.torch_dtype] + 26 * 3 * 2.0 ** -24 + 2.0 ** -11 + 2.0 ** -36 * math.exp(18.0) + 2.0 ** -11
+            bad = np.abs(out[:, i] - want) > rel * want
+            assert not bad.any(), (i, np.argwhere(bad)[:3], out[0, i, :3], want[:3])
+
+
+
 def attend_closely(p, n, q, scale=None, **how):
     """The attention against the definition where a bound by the largest value would say nothing: a numerator is off by 2^-11 of itself or by
     2^-36 of the row's largest (2^6 more where its block's scale of V is up to 2^6 smaller), sums by the roundings of 1024 additions."""
