@@ -513,6 +513,27 @@ def attend_closely(p, n, q, scale=None, **how):
         assert (np.abs(lse[b] - want_lse) <= off + 2.0 ** -14 + 2.0 ** -22 * (np.abs(want_lse) + 2)).all(), b
 
 
+@pytest.mark.parametrize("cap", [512, 4096])
+@pytest.mark.parametrize("d,n", [(64, 1), (128, 9), (96, 200), (64, 200), (256, 100)])
+@pytest.mark.parametrize("bf16", [False, True])
+def test_value_scales_of_every_size_closely(pk, bf16, d, n, cap):
+    """Blocks whose V scales differ by up to 2^24 (bfloat16: 2^70) in both orders, the large ones with little softmax weight, against bounds of
+    the rest's size: one row and many."""
+    p = Pair(pk, 27, n_seq=1, hkv=1, r=2, d=d, block=32, cap=cap, bf16=bf16, spread=0.0)
+    k, v = p.vectors(512, 1, 0.25), p.vectors(512, 1)
+    v[0].abs_()
+    sizes = [0, 3, -4, 10, 2, -9, 12, 1, 0, 5, -3, 8, 4, 0, 11, 2] if not bf16 else [0, 3, -40, 30, 2, -9, 12, 1, 0, 25, -35, 8, 4, 0, 11, 2]
+    far = [i for i, e in enumerate(sizes) if e >= 8]
+    for i, e in enumerate(sizes):
+        v[0][0, 0, 32 * i:32 * i + 32] *= 2.0 ** e
+    q, _ = p.vectors(1, 2, 4.0)
+    for i in far:       # the keys of the large blocks point away from both queries
+        k[0][0, 0, 32 * i:32 * i + 32] -= (q[0, 0, 0] + q[0, 1, 0]) * (40.0 * d ** -0.5 / 4.0 / 4.0)
+    p.append(512, k=(k[0], k[0].double().cpu().numpy()), v=(v[0], v[0].double().cpu().numpy()))
+    q = q.expand(-1, -1, n, -1)
+    attend_closely(p, n, (q, q.double().cpu().numpy()))
+
+
 @pytest.mark.parametrize("d,n", [(64, 1), (128, 200), (256, 3)])
 def test_values_near_the_largest(pk, d, n):
     """Values up to a quarter of bfloat16's largest: the weighted mean of many of them is finite, though their sum is not."""
