@@ -534,6 +534,22 @@ def test_value_scales_of_every_size_closely(pk, bf16, d, n, cap):
     attend_closely(p, n, (q, q.double().cpu().numpy()))
 
 
+@pytest.mark.parametrize("d,r,n,bf16,page,how", [
+    (64, 1, 1, False, 0, {}), (64, 8, 1, True, 256, {}), (128, 8, 3, False, 0, dict(cap=30.0)), (64, 1, 300, False, 0, {}), (96, 5, 3, True, 0, dict(window=30000)),
+    (256, 8, 1, False, 128, {}), (256, 8, 4, True, 0, dict(window=20000))])
+@pytest.mark.parametrize("at", [700, 32900])
+def test_more_pieces_than_lanes(pk, d, r, n, bf16, page, how, at):
+    """One KV head over 33k tokens: more runs of its keys than a wave that merges them has lanes; the largest score in one of the first of
+    them, or of the last."""
+    p = Pair(pk, 28, n_seq=1, hkv=1, r=r, d=d, block=128, cap=33280, bf16=bf16, page=page, spread=0.3)
+    k, v = p.vectors(33100, 1), p.vectors(33100, 1)
+    v[0].add_(2.0)
+    q = p.vectors(n, r)
+    k[0][0, 0, at] = q[0][0, 0, 0] * 1.5
+    p.append(33100, k=(k[0], k[0].double().cpu().numpy()), v=(v[0], v[0].double().cpu().numpy()))
+    attend_closely(p, n, q, **how)
+
+
 @pytest.mark.parametrize("d,n", [(64, 1), (128, 200), (256, 3)])
 def test_values_near_the_largest(pk, d, n):
     """Values up to a quarter of bfloat16's largest: the weighted mean of many of them is finite, though their sum is not."""
