@@ -498,11 +498,12 @@ def pk_fp8_cache_layout(cfg: Fp8Config) -> dict:
 
 def pk_fp8_workspace_bytes(cfg: Fp8Config, op: int, a: int, b: int = 0) -> int:
     key = (op, a, b)
-    if key not in cfg._workspaces:
+    need = cfg._workspaces.get(key)   # (another thread may clear them at any point)
+    if need is None:
         if len(cfg._workspaces) > 4096:
             cfg._workspaces.clear()
-        cfg._workspaces[key] = int(_lib.pk_fp8_workspace_bytes(cfg.packed, op, a, b))
-    return cfg._workspaces[key]
+        need = cfg._workspaces[key] = int(_lib.pk_fp8_workspace_bytes(cfg.packed, op, a, b))
+    return need
 
 
 class Fp8Cache:

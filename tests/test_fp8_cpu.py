@@ -168,6 +168,29 @@ def test_binding_refuses(pk):
         pk.Fp8Cache(cfg, device="cpu", states=torch.zeros(2, 4))
 
 
+def test_workspace_size_while_another_thread_forgets_it(pk):
+    """The sizes that a configuration remembers may be cleared by another thread at any point."""
+    class Racing(dict):
+        def __contains__(self, key):
+            there = dict.__contains__(self, key)
+            self.clear()
+            return there
+
+        def __len__(self):
+            return 1 << 20
+
+        def __setitem__(self, key, value):
+            pass
+
+    cfg = pk.Fp8Config(**BASE)
+    need = pk.pk_fp8_workspace_bytes(cfg, pk.FP8_OP_EVICT, 100)
+    racing = Racing({(pk.FP8_OP_EVICT, 100, 0): need})
+    object.__setattr__(cfg, "_workspaces", racing)
+    assert pk.pk_fp8_workspace_bytes(cfg, pk.FP8_OP_EVICT, 100) == need
+    racing.clear()
+    assert pk.pk_fp8_workspace_bytes(cfg, pk.FP8_OP_EVICT, 100) == need
+
+
 def test_reference_codes_are_e4m3():
     x = torch.arange(256, dtype=torch.uint8)
     got = x.view(torch.float8_e4m3fn).double().numpy()
