@@ -506,6 +506,11 @@ def pk_fp8_workspace_bytes(cfg: Fp8Config, op: int, a: int, b: int = 0) -> int:
     return need
 
 
+def _fp8_need(true, what):
+    if not true:   # (an assert statement would be dropped by python -O, and what it checks keeps the kernels in bounds)
+        raise AssertionError(what)
+
+
 class Fp8Cache:
     """Device memory of an 8-bit cache: the arrays of pk_fp8_cache_layout (`buf`), `states` int32 [n_seq, 4] (tokens held, next position, 0, 0)
     and, if paged, `page_table` int32 [n_seq, t_capacity / page_tokens], which the caller fills.  `arrays`, `states` and
@@ -524,24 +529,24 @@ class Fp8Cache:
         for n in _FP8_ARRAYS:
             t = self.buf.get(n)
             if t is None:
-                assert n == "weight", f"the cache needs {n}"
+                _fp8_need(n == "weight", f"the cache needs {n}")
                 continue
-            assert t.dtype == _FP8_TYPES[n] and t.is_contiguous() and t.numel() * t.element_size() >= lay[n], n
+            _fp8_need(t.dtype == _FP8_TYPES[n] and t.is_contiguous() and t.numel() * t.element_size() >= lay[n], n)
         if states is None:
             states = torch.zeros((cfg.n_seq, 4), dtype=torch.int32, device=self.buf["k_codes"].device)
-        assert states.dtype == torch.int32 and tuple(states.shape) == (cfg.n_seq, 4) and states.is_contiguous()
+        _fp8_need(states.dtype == torch.int32 and tuple(states.shape) == (cfg.n_seq, 4) and states.is_contiguous(), "states")
         self.states = states
         if cfg.page_tokens > 0:
             shape = (cfg.n_seq, cfg.t_capacity // cfg.page_tokens)
             if page_table is None:
                 page_table = torch.zeros(shape, dtype=torch.int32, device=states.device)
-            assert page_table.dtype == torch.int32 and tuple(page_table.shape) == shape and page_table.is_contiguous()
+            _fp8_need(page_table.dtype == torch.int32 and tuple(page_table.shape) == shape and page_table.is_contiguous(), "page_table")
         else:
             page_table = None
         self.page_table = page_table
         tensors = [self.buf.get(n) for n in _FP8_ARRAYS] + [page_table]
         self.device = states.device
-        assert all(t is None or t.device == self.device for t in tensors), "the tensors of a cache are on one device"
+        _fp8_need(all(t is None or t.device == self.device for t in tensors), "the tensors of a cache are on one device")
         self.packed = _pack_fp8_cache(*[0 if t is None else t.data_ptr() for t in tensors])
 
     @property

@@ -3,6 +3,7 @@
 import os
 import shutil
 import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -189,6 +190,32 @@ def test_workspace_size_while_another_thread_forgets_it(pk):
     assert pk.pk_fp8_workspace_bytes(cfg, pk.FP8_OP_EVICT, 100) == need
     racing.clear()
     assert pk.pk_fp8_workspace_bytes(cfg, pk.FP8_OP_EVICT, 100) == need
+
+
+def test_cache_is_checked_under_optimization():
+    """`python -O` drops assert statements, and a cache whose arrays are too small is written out of bounds: its checks are none."""
+    code = """
+import torch
+from paper_2510_05176_amd import patternkv as pk
+cfg = pk.Fp8Config(n_seq=2, n_kv_heads=2, n_q_heads=8, t_capacity=1024)
+paged = pk.Fp8Config(n_seq=2, n_kv_heads=2, n_q_heads=8, t_capacity=1024, page_tokens=128, n_pages=16)
+good = pk.Fp8Cache(cfg, device="cpu")
+table = pk.Fp8Cache(paged, device="cpu").page_table
+bad = [(cfg, dict(arrays={**good.buf, "pos": good.buf["pos"][:-1]})), (cfg, dict(arrays={k: v for k, v in good.buf.items() if k != "k_scale"})),
+       (cfg, dict(arrays={**good.buf, "weight": good.buf["weight"].double()})), (cfg, dict(states=torch.zeros(2, 4))),
+       (cfg, dict(states=torch.zeros(2, 8, dtype=torch.int32)[:, ::2])), (paged, dict(page_table=table[:1])), (paged, dict(page_table=table.long())),
+       (cfg, dict(states=good.states.to("meta")))]
+for c, kw in bad:
+    try:
+        pk.Fp8Cache(c, device="cpu", **kw)
+    except AssertionError:
+        continue
+    raise SystemExit(str(list(kw)))
+print("ok", __debug__)
+"""
+    for flag, debug in (("-O", "False"), ("-B", "True")):
+        r = subprocess.run([sys.executable, flag, "-c", code], capture_output=True, text=True, cwd=ROOT, timeout=300)
+        assert r.returncode == 0 and r.stdout.split() == ["ok", debug], (flag, r.stdout, r.stderr[-2000:])
 
 
 def test_reference_codes_are_e4m3():
