@@ -592,6 +592,8 @@ def _fp8_counts(cfg: Fp8Config, cache: Fp8Cache, counts):
 
 
 def _fp8_scores(cfg: Fp8Config, cache: Fp8Cache, softmax_scale, cap, window, slopes) -> bytes:
+    if window:
+        _fp8_int(window, "window")
     if slopes is None:
         return _pack_fp8_scores(softmax_scale, cap, window, 0)
     if slopes.dtype != torch.float32 or tuple(slopes.shape) != (cfg.n_q_heads,) or not slopes.is_contiguous() or slopes.device != cache.device:
@@ -603,6 +605,13 @@ def _fp8_lse(cfg: Fp8Config, cache: Fp8Cache, lse: torch.Tensor, n: int):
     if lse.dtype != torch.float32 or tuple(lse.shape) != (cfg.n_seq, cfg.n_q_heads, n) or not lse.is_contiguous() or lse.device != cache.device:
         raise ValueError(f"lse: expected contiguous float32 [{cfg.n_seq}, {cfg.n_q_heads}, {n}] on {cache.device}")
     return lse.data_ptr()
+
+
+def _fp8_int(value, name: str):
+    """A number that the library takes as an int32, of which ctypes would keep the low bits."""
+    if not -(1 << 31) <= value < 1 << 31:
+        raise ValueError(f"{name}: {value} is not an int32")
+    return value
 
 
 def _fp8_workspace(cfg: Fp8Config, cache: Fp8Cache, workspace, op: int, a: int, b: int):
@@ -651,7 +660,7 @@ def pk_fp8_attention(cfg: Fp8Config, cache: Fp8Cache, q: torch.Tensor, softmax_s
         if o.shape != q.shape:
             raise ValueError(f"out: expected {list(q.shape)}, got {list(o.shape)}")
     os_ = qs if out is None and o.stride() == q.stride() else _fp8_vectors(cfg, cache, o, cfg.n_q_heads, "out")
-    bound = cfg.t_capacity if bound is None else bound
+    bound = cfg.t_capacity if bound is None else _fp8_int(bound, "bound")
     workspace = _fp8_workspace(cfg, cache, workspace, FP8_OP_ATTENTION, n, bound)
     _check(_lib.pk_fp8_attention(cfg.packed, cache.packed, cache.states.data_ptr(), bound, q.data_ptr(), qs, n, _fp8_counts(cfg, cache, counts),
                                  _fp8_scores(cfg, cache, softmax_scale, cap, window, slopes), o.data_ptr(), os_,
@@ -669,7 +678,7 @@ def pk_fp8_weights(cfg: Fp8Config, cache: Fp8Cache, q: torch.Tensor, lse: torch.
         q = q.unsqueeze(2)
     qs = _fp8_vectors(cfg, cache, q, cfg.n_q_heads, "q")
     n = q.shape[2]
-    bound = cfg.t_capacity if bound is None else bound
+    bound = cfg.t_capacity if bound is None else _fp8_int(bound, "bound")
     _check(_lib.pk_fp8_weights(cfg.packed, cache.packed, cache.states.data_ptr(), bound, q.data_ptr(), qs, n, _fp8_counts(cfg, cache, counts),
                                _fp8_scores(cfg, cache, softmax_scale, cap, window, slopes), _fp8_lse(cfg, cache, lse, n), 1 if accumulate else 0,
                                _fp8_stream(cfg, cache)), "pk_fp8_weights")
@@ -681,6 +690,7 @@ def pk_fp8_evict(cfg: Fp8Config, cache: Fp8Cache, to_cfg: Fp8Config, to: Fp8Cach
     with the largest weight."""
     if to.device != cache.device or (to_cfg is not to.cfg and to_cfg != to.cfg):
         raise ValueError(f"the caches are on {cache.device} and {to.device}; each goes with its own configuration")
+    _fp8_int(budget, "budget"), _fp8_int(keep_first, "keep_first"), _fp8_int(keep_last, "keep_last")
     workspace = _fp8_workspace(cfg, cache, workspace, FP8_OP_EVICT, budget, 0)
     _check(_lib.pk_fp8_evict(cfg.packed, cache.packed, cache.states.data_ptr(), to_cfg.packed, to.packed, to.states.data_ptr(), budget, keep_first,
                              keep_last, None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.numel(),

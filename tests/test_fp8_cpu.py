@@ -218,6 +218,23 @@ print("ok", __debug__)
         assert r.returncode == 0 and r.stdout.split() == ["ok", debug], (flag, r.stdout, r.stderr[-2000:])
 
 
+def test_evict_refuses_numbers_of_more_than_32_bits(pk):
+    """ctypes would cut them off: 2^32 + 64 tokens to 64."""
+    cfg = pk.Fp8Config(**BASE)
+    a, b = pk.Fp8Cache(cfg, device="cpu"), pk.Fp8Cache(cfg, device="cpu")
+    ws = torch.zeros(1 << 16, dtype=torch.uint8)
+    for name in ("budget", "keep_first", "keep_last"):
+        for value in ((1 << 32) + 64, 1 << 31, -(1 << 32)):
+            with pytest.raises(ValueError, match=name):
+                pk.pk_fp8_evict(cfg, a, cfg, b, **{"budget": 64, name: value}, workspace=ws)
+    for kw in (dict(bound=(1 << 32) + 64), dict(window=1 << 31)):
+        q = torch.zeros(2, 8, 1, 128, dtype=torch.float16)
+        with pytest.raises(ValueError, match=list(kw)[0]):
+            pk.pk_fp8_attention(cfg, a, q, 1.0, **kw)
+        with pytest.raises(ValueError, match=list(kw)[0]):
+            pk.pk_fp8_weights(cfg, a, q, torch.zeros(2, 8, 1), 1.0, **kw)
+
+
 def test_reference_codes_are_e4m3():
     x = torch.arange(256, dtype=torch.uint8)
     got = x.view(torch.float8_e4m3fn).double().numpy()
