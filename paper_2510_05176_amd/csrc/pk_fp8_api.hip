@@ -216,8 +216,9 @@ pk_status pk_fp8_attention(const pk_fp8_config *cfg, const pk_fp8_cache *cache, 
     if (st != PK_OK) return st;
     if (!out && n_query > 0) return PK_ERR_INVALID_ARG;
     if ((st = check_strides(os)) != PK_OK) return st;
-    // a row of the output has one place
-    if ((cfg->n_seq > 1 && os->seq == 0) || (n_query > 1 && os->token == 0) || (cfg->n_q_heads > 1 && os->head == 0)) return PK_ERR_SHAPE;
+    // rows of the output do not lie within each other
+    const auto within = [&](int64_t n, int64_t stride) { return n > 1 && stride > -cfg->head_dim && stride < cfg->head_dim; };
+    if (within(cfg->n_seq, os->seq) || within(n_query, os->token) || within(cfg->n_q_heads, os->head)) return PK_ERR_SHAPE;
     if (!aligned16(out) || !aligned16(lse) || !aligned16(workspace)) return PK_ERR_ALIGNMENT;
     if (n_query == 0) return PK_OK;
     const AttentionPlan p = plan_attention(cfg, n_query, bound);

@@ -235,6 +235,12 @@ def test_evict_refuses_numbers_of_more_than_32_bits(pk):
             pk.pk_fp8_weights(cfg, a, q, torch.zeros(2, 8, 1), 1.0, **kw)
 
 
+def test_attention_refuses_rows_of_the_output_within_each_other(pk):
+    """Strides of the output shorter than a vector, where there is more than one: whichever row is written last would win."""
+    for s, n in (((8192, 256, 64), 1), ((8192, 120, 2048), 2), ((64, 1024, 128), 1), ((-64, 1024, 128), 1), ((8192, 1024, -120), 1)):
+        assert attention(pk, n=n, os_=strides(pk, *s)) == SHAPE, (s, n)
+
+
 def test_reference_codes_are_e4m3():
     x = torch.arange(256, dtype=torch.uint8)
     got = x.view(torch.float8_e4m3fn).double().numpy()
