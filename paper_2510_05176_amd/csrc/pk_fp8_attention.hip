@@ -9,10 +9,13 @@
 // permutes before the conversion to fp16.  Block scales are powers of two and stay outside both products.  (e4m3 operands as they are, with the
 // queries in two or three e4m3 terms, would save K's conversion but not V's, which needs the numerators in as many terms.)
 //
-// One token over long caches is bound by HBM (16 sequences x 32k tokens, 8 KV heads of 128 channels: 185 us, 5.8 TB/s, where a plain
-// read reaches 5.5), many rows by what a wave can issue beside its matrix instructions (1024 queries of 32 heads over 16k tokens: 331 us, 0.81
-// PFLOP/s; 656 with 256 channels, 0.82.  Per 64 tokens and 32 rows 64 matrix instructions beside about 290 vector ones, 32 of them exponentials).
+// One token over long caches is bound by HBM (16 sequences x 32k tokens, 8 KV heads of 128 channels: 189 us, 5.7 TB/s, where a plain
+// read reaches 5.5).  Many rows are far from the matrix cores' rate (1024 queries of 32 heads over 16k tokens: 332 to 338 us, 0.80 PFLOP/s; 256 channels
+// 651 us, 0.82): per 64 tokens and 32 rows 64 matrix instructions beside about 290 vector ones, 32 of them exponentials, and of a SIMD's time 35 % are
+// matrix and some 52 % vector instructions, which hardly overlap: its two waves go through the same phases at the same time.
 // There the operands of a tile are converted once for four waves and lie in LDS (each wave converting for itself: 385 us, and 1121 with 256 channels).
+// With two row tiles and at 256 channels a few registers are spilled (22 at 128 channels, 28 at 96, 6 at 256, with options 28, 42, 14), before and
+// behind the loop over the keys.
 #include "pk_fp8.h"
 
 namespace pk {
@@ -26,7 +29,7 @@ __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(
 
 // x[i] = m * tanh(x[i] * c[i / 8]) in binary32.  Below 0.55 the odd Taylor series, above it 1 - 2 / (e^{2y} + 1), whose rounding is no longer
 // magnified there; how far the series goes, and whether the other form is computed at all, is the wave's largest argument's to say (the first term
-// left out is 2e-9 of the result at 0.25 and 4e-8 at 0.55).  tanh y = y + y^3 s(y^2), s from 2^(2k) (2^(2k) - 1) B_2k / (2k)!.
+// left out is 2e-10 of the result at 0.25 and 4e-8 at 0.55).  tanh y = y + y^3 s(y^2), s from 2^(2k) (2^(2k) - 1) B_2k / (2k)!.
 __device__ __forceinline__ void capped(float (&x)[16], const float (&c)[2], float m)
 {
     float most = 0.f;
@@ -1006,7 +1009,7 @@ __device__ __forceinline__ double log2e_of(float scale)
 
 // A wave takes 64 tokens at a time, their K operands in registers, against the rows in LDS; the sums over rows stay in registers
 // until all tiles are done.  More rows than fit go in rounds that add to what the first wrote, each token in the same lane.
-// One query over 16 x 32k tokens: 104 us, 5.3 TB/s of K.  32 queries of four heads over 8k: 97 us, 0.72 PFLOP/s; per pair a multiply-add, an
+// One query over 16 x 32k tokens: 104 us, 5.3 TB/s of K.  32 queries of four heads over 8k: 95 us, 0.73 PFLOP/s; per pair a multiply-add, an
 // exponential and an addition beside the products, and vector and matrix instructions of the two waves of a SIMD hide each other only in part.
 template <int D, bool OPT>
 __global__ __launch_bounds__(kThreads, 2) void fp8_weights_kernel(Fp8WeightsArgs a)
