@@ -12,7 +12,7 @@
 // One token over long caches is bound by HBM (16 sequences x 32k tokens, 8 KV heads of 128 channels: 189 us, 5.7 TB/s, where a plain
 // read reaches 5.5).  Many rows are far from the matrix cores' rate (1024 queries of 32 heads over 16k tokens: 332 to 338 us, 0.80 PFLOP/s; 256 channels
 // 651 us, 0.82): per 64 tokens and 32 rows 64 matrix instructions beside about 290 vector ones, 32 of them exponentials, and of a SIMD's time 35 % are
-// matrix and some 52 % vector instructions, which hardly overlap: its two waves go through the same phases at the same time.
+// matrix and some 52 % vector instructions, which hardly overlap (nothing sets its two waves against each other).
 // There the operands of a tile are converted once for four waves and lie in LDS (each wave converting for itself: 385 us, and 1121 with 256 channels).
 // With two row tiles and at 256 channels a few registers are spilled (22 at 128 channels, 28 at 96, 6 at 256, with options 28, 42, 14), before and
 // behind the loop over the keys.
