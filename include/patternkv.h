@@ -483,11 +483,13 @@ pk_status pk_fp8_append(const pk_fp8_config *cfg, const pk_fp8_cache *cache, int
  *              workspace.  Results do not depend on sequences staying below it, only the balance of the work does.
  *   q, qs      queries, (seq, token, head) as above; out, os: results in the same type
  *   lse        optional float [n_seq][n_q_heads][n_query]: log-sum-exp of the scores
- * A query that sees no token has out = 0 and lse = -inf.  Strides of 0 are taken in the inputs; in `out` none is shorter than a vector.  Masked tokens never contribute, whatever their codes are.
+ * A query that sees no token has out = 0 and lse = -inf.  Strides of 0 are taken in the inputs; in `out` none is shorter than a
+ * vector.  Masked tokens never contribute, whatever their codes are.
  * Scores and outputs are accumulated in binary32 (e4m3 codes and the queries are exact in the fp16 operands of the matrix
  * instructions; bfloat16 queries are brought to fp16's range by a power of two per query first, which drops what lies under
  * 2^-31 of a query's largest element); softmax numerators are rounded to fp16 (off by up to 2^-11 of themselves, or 2^-36 of the
- * largest one where they are smaller than 2^-25 of it), their sum is not: it makes the log-sum-exp.
+ * largest one where they are smaller than 2^-25 of it; both limits up to 2^6 higher for tokens whose V scale is up to 2^6 below
+ * others', and 2^11 for scores beyond 2^19), their sum is not: it makes the log-sum-exp.
  */
 pk_status pk_fp8_attention(const pk_fp8_config *cfg, const pk_fp8_cache *cache, const int32_t *states, int32_t bound, const void *q,
                            const pk_strides *qs, int32_t n_query, const int32_t *counts, const pk_fp8_scores *scores, void *out,
