@@ -594,6 +594,7 @@ __global__ __launch_bounds__(64 * NW, 2) void fp8_attention_kernel(Fp8AttentionA
 #pragma unroll
         for (int ct = 0; ct < S::kTiles; ++ct) o[rt][ct] = float4v{0.f, 0.f, 0.f, 0.f};
     }
+    bool large = false;   // a row of the wave has scores of 2^20 or more
     int unit = 0, unit_most = 0;   // exponent field of the V scale that o is in units of, and the largest one (0: none yet, o = 0)
 
     const uint32_t k_off = n * D + g * (D / 4), v_off = 4 * g * D + n * (D == 96 ? 4 : D / 16);
@@ -699,6 +700,28 @@ __global__ __launch_bounds__(64 * NW, 2) void fp8_attention_kernel(Fp8AttentionA
             }
             moved |= by[rt] != 1.f;
         }
+        const bool some_moved = __any(moved);
+        if constexpr (!OPT) {
+            // Of scores whose steps are large, rounded ones, as their largest is: the exponent's multiply-add takes their factor in unrounded, and half a
+            // step above the reference is beyond fp16 from scores of 2^28 on.
+            if (some_moved) {
+                bool now = false;
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) now |= fabsf(m[rt]) >= 0x1p20f && m[rt] != -INFINITY;
+                large |= __any(now);
+            }
+            if (large) {
+#pragma unroll
+                for (int rt = 0; rt < RT; ++rt) {
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        x[rt][i] *= f[rt][i >> 3];
+                        asm volatile("" : "+v"(x[rt][i]));   // (not contracted, and not computed without the branch)
+                    }
+                    f[rt][0] = f[rt][1] = 1.f;
+                }
+            }
+        }
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
             if (t0 + 32 * half >= hi) break;
@@ -715,7 +738,7 @@ __global__ __launch_bounds__(64 * NW, 2) void fp8_attention_kernel(Fp8AttentionA
                 unit = to;
             }
             const int fold = min(unit - field, 60);   // from 40 on fp16 leaves nothing of the numerators
-            if (half == 0 ? shift != 0 || __any(moved) : shift != 0) {
+            if (half == 0 ? shift != 0 || some_moved : shift != 0) {
 #pragma unroll
                 for (int rt = 0; rt < RT; ++rt) {
                     const float f = ldexpf(half == 0 ? by[rt] : 1.f, shift);

@@ -560,6 +560,33 @@ def test_values_near_the_largest(pk, d, n):
     attend_closely(p, n, p.vectors(n, 2))
 
 
+@pytest.mark.parametrize("d,r,n,cap", [(64, 1, 1, 1024), (128, 4, 1, 8192), (64, 2, 200, 1024), (256, 1, 20, 1024), (128, 20, 1, 1024)])
+@pytest.mark.parametrize("how", [{}, dict(window=1 << 20)])
+def test_scores_whose_steps_are_large(pk, d, r, n, cap, how):
+    """Scores around 2^18 to 2^40 of both signs, whose own binary32 steps are up to 2^17: results are means of the values and the log-sum-exp is the
+    largest score's, whatever the order of the scores."""
+    cfg = pk.Fp8Config(n_seq=4, n_kv_heads=1, n_q_heads=r, head_dim=d, t_capacity=cap, dtype=pk.DTYPE_BF16)
+    g = torch.Generator().manual_seed(31)
+    for e in range(18, 41, 2):
+        cache = pk.Fp8Cache(cfg, track_weight=False)
+        k = torch.zeros(4, 1, 900, d)
+        k[:2, 0, :, 0], k[2:, 0, :, 0] = 1.0, -1.0
+        rise = torch.randint(0, 16, (900,), generator=g).float() / 16            # 1 .. 1.9 in steps that e4m3 has
+        k[:, 0, :, 0] *= 1 + (rise * 8).floor() / 8
+        k[1::2, 0] = k[1::2, 0].flip(1).sort(1).values                           # every second sequence in order
+        v = torch.rand(4, 1, 900, d, generator=g) + 1.0
+        pk.pk_fp8_append(cfg, cache, k.bfloat16().cuda(), v.bfloat16().cuda())
+        q = torch.zeros(4, r, n, d)
+        q[..., 0] = 1.37 * 2.0 ** e
+        q[..., 1] = 1.0
+        lse = torch.empty(4, r, n, device="cuda")
+        out = pk.pk_fp8_attention(cfg, cache, q.bfloat16().cuda(), 1.0, lse=lse, **how).float().cpu()
+        assert torch.isfinite(out).all() and (out >= 1 - 2.0 ** -4).all() and (out <= 2 + 2.0 ** -3).all(), (e, out.min(), out.max())
+        top = torch.stack([k[..., : 900 - n + i + 1, 0].amax(-1).expand(-1, r) for i in range(n)], 2) * q[..., 0].bfloat16().float()
+        # e4m3 and the values' own rounding aside, a row's mean lies among its largest scores' values; the sum of up to 900 of them adds 10
+        assert ((lse.cpu() - top).abs() <= 10 + top.abs() * 2.0 ** -20).all(), e
+
+
 EVICTS = [(128, 64, 0, 0, 100, 4, 16), (64, 32, 128, 0, 64, 0, 0), (96, 32, 0, 128, 77, 0, 77), (256, 128, 256, 128, 129, 1, 0), (128, 64, 0, 0, 1, 0, 0), (64, 64, 0, 0, 63, 31, 32)]
 
 
