@@ -19,6 +19,10 @@
  *   pk_fp8_append, pk_fp8_attention, pk_fp8_weights, pk_fp8_evict
  *                         a cache of 8-bit codes with a scale per block of tokens, for
  *                         what 2 or 4 bits do not serve (its own section below)
+ *   pk_pages_update       page tables and slot maps of a step, built on the device
+ *   pk_kv16_append, pk_kv16_attention
+ *                         a paged cache of 16-bit vectors, for what is not quantized
+ *   pk_prompt_attention   causal attention of packed prompts
  *
  * Conventions shared by every call
  *   - All tensor pointers are DEVICE pointers unless marked "host".  Structs
@@ -518,6 +522,129 @@ pk_status pk_fp8_weights(const pk_fp8_config *cfg, const pk_fp8_cache *cache, co
 pk_status pk_fp8_evict(const pk_fp8_config *cfg, const pk_fp8_cache *cache, const int32_t *states, const pk_fp8_config *to_cfg,
                        const pk_fp8_cache *to, int32_t *to_states, int32_t budget, int32_t keep_first, int32_t keep_last,
                        void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * A paged cache of 16-bit vectors, for what is not quantized (layers that do not bear it, a window before it is, the plain cache to compare
+ * with): page tables and slot maps built on the device, append by slot, attention of one token per sequence; and attention of whole prompts, on the
+ * vectors that a prefill has in hand before any cache takes them.
+ *
+ * Pages
+ *   A pool of n_pages pages of page_tokens tokens; token t of a sequence lies in page table[sequence][t / page_tokens], at t % page_tokens.
+ *   slot = page * page_tokens + t % page_tokens (the same for every KV head).  free_pages[0 .. n_free[0]) is a stack of the free pages.
+ *   The tables serve every paged cache of this library whose states are device memory (pk_kv16_*, pk_fp8_*).
+ * Format of the 16-bit cache
+ *   k, v [n_pages][n_kv_heads][page_tokens][d] fp16 or bf16
+ * States: DEVICE int32 [n_seq][4], 16-byte aligned, as for the 8-bit cache: tokens held (clamped to [0, capacity] where it is read), position of the next token, 0, 0.
+ * Packed tensors hold the tokens of a step one sequence after the other: those of sequence i are rows starts[i] .. starts[i + 1]; starts is
+ *   DEVICE int32 [n_seq + 1], growing.  Their strides are pk_strides whose `seq` is not used; the d elements of a vector are contiguous,
+ *   strides are multiples of 8, pointers 16-byte aligned.
+ */
+typedef struct {
+    int32_t n_seq;         /* 1 .. 65535                                                          */
+    int32_t page_tokens;   /* a power of two                                                      */
+    int32_t n_pages;       /* >= 1; n_pages * page_tokens < 2^31                                  */
+    int32_t pages_per_seq; /* >= 1: entries of a row of the table; pages_per_seq * page_tokens <= 2^25 */
+} pk_pages_config;
+
+typedef struct {
+    int32_t *table;        /* DEVICE [n_seq][pages_per_seq]                                       */
+    int32_t *free_pages;   /* DEVICE [n_pages]                                                    */
+    const int32_t *n_free; /* DEVICE [4]: their number (clamped to [0, n_pages]), 0, 0, 0         */
+    int32_t *n_free_out;   /* DEVICE [4], the same afterwards; NULL or n_free itself: in place    */
+} pk_pages;
+
+/* Bytes of workspace of pk_pages_update.  0 for an invalid configuration.  Host-only. */
+size_t pk_pages_workspace_bytes(const pk_pages_config *cfg);
+
+/*
+ * A step's page tables, slots and states from its counts of tokens.  counts[i] > 0: sequence i gets that many new tokens; < 0: it gives its
+ * last -counts[i] tokens back (all of them at the most); 0: it stays as it is.
+ * First the pages that hold no token any more go on the stack, in order of (sequence, logical page); then the pages that the new tokens need are taken
+ * from its top, sequence after sequence.  Tokens for which there is no page, or no room in the sequence's row of the table, are left out, behind those of
+ * their sequence that have a place.
+ *   states      DEVICE in; states_out DEVICE out, the states afterwards; NULL or `states` itself: in place.  With states_out and n_free_out of their
+ *               own, what was before stays valid (nothing that belongs to it is overwritten), until pages change hands in a step from it.
+ *   counts      DEVICE int32 [n_seq]
+ *   n_tokens    host: rows of the step's packed tensors.  New tokens beyond it are not there (counts are cut at it).
+ *   starts      DEVICE int32 [n_seq + 1]: where each sequence's new tokens begin in the packed tensors: sums of the positive counts
+ *   slots       DEVICE int32 [n_tokens]: the slot of every row; -1 for tokens that were left out and for rows behind the last sequence
+ *   positions   DEVICE int32 [n_tokens] or NULL: their positions (next position of the sequence, and so on); 0 behind the last sequence
+ *   taken       DEVICE int32 [n_seq]: how many of its new tokens each sequence got a place for, 0 where it got none or gave tokens back (what an
+ *               append to the 8-bit cache takes as `counts`)
+ * Entries of the table that no new token needs are left as they are.  Entries and stack are taken as they come, clamped to the pool.
+ * Arrays that are written do not overlap with others.
+ */
+pk_status pk_pages_update(const pk_pages_config *cfg, const pk_pages *pages, const int32_t *states, int32_t *states_out, const int32_t *counts,
+                          int32_t n_tokens, int32_t *starts, int32_t *slots, int32_t *positions, int32_t *taken, void *workspace,
+                          size_t workspace_bytes, void *stream);
+
+typedef struct {
+    int32_t n_seq;       /* >= 1; n_seq * n_kv_heads at most 65535                                     */
+    int32_t n_kv_heads;  /* >= 1                                                                       */
+    int32_t n_q_heads;   /* multiple of n_kv_heads, at most 64 of them per KV head                     */
+    int32_t head_dim;    /* 64, 96, 128 or 256                                                         */
+    int32_t t_capacity;  /* tokens per sequence, a multiple of page_tokens, at most 2^25               */
+    int32_t dtype;       /* pk_dtype of the cache, of queries and outputs                              */
+    int32_t page_tokens; /* a power of two >= 16                                                       */
+    int32_t n_pages;     /* pages in the pool, >= 1; n_pages * page_tokens < 2^31                      */
+} pk_kv16_config;
+
+typedef struct {
+    void *k, *v;
+    const int32_t *page_table; /* DEVICE int32 [n_seq][t_capacity / page_tokens], entries clamped to the pool */
+} pk_kv16_cache;
+
+/* Bytes of one of k and v.  0 for an invalid configuration.  Host-only. */
+uint64_t pk_kv16_cache_bytes(const pk_kv16_config *cfg);
+
+/* Bytes of workspace of pk_kv16_attention with that bound, not shrinking as the bound grows.  0 for an invalid configuration or bound.  Host-only. */
+size_t pk_kv16_workspace_bytes(const pk_kv16_config *cfg, int64_t bound);
+
+/*
+ * Put the vectors of a packed step in their slots: K and V of row i, head h go to slot slots[i] (as pk_pages_update leaves them) of head h.
+ * Rows whose slot is not in [0, n_pages * page_tokens) are left out.  Reads neither page table nor states.  A slot that two rows share gets one
+ * of them, or parts of both.
+ *   k_new, v_new  (token, head) at token * ks.token + head * ks.head
+ */
+pk_status pk_kv16_append(const pk_kv16_config *cfg, const pk_kv16_cache *cache, const void *k_new, const void *v_new, const pk_strides *ks,
+                         const pk_strides *vs, const int32_t *slots, int32_t n_tokens, void *stream);
+
+/*
+ * Attention of one token per sequence, the last one that the cache holds, over the tokens held: out = softmax(scores) V.
+ *   bound      host: no sequence holds more tokens than this (t_capacity is always right); sizes the launch and the workspace.  Results do not depend
+ *              on sequences staying below it, only the balance of the work does.
+ *   q, qs      queries, (seq, head) at seq * qs.seq + head * qs.head; out, os: results in the same type; `token` is not used
+ *   scores     as for the 8-bit cache; positions are the tokens' numbers in the sequence
+ *   lse        optional float [n_seq][n_q_heads]: log-sum-exp of the scores
+ * A sequence that holds no token has out = 0 and lse = -inf.  Slots behind the tokens held never contribute, whatever they hold, nor do tokens that the window masks.
+ * Strides of 0 are taken in the inputs; in `out` none is shorter than a vector.  Scores and outputs are accumulated in binary32; softmax
+ * numerators are rounded to the 16-bit type (fp16: off by up to 2^-11 of themselves, or 2^-36 of the largest one where they are smaller; bf16: 2^-8), their
+ * sum, which makes the log-sum-exp, is not.
+ */
+pk_status pk_kv16_attention(const pk_kv16_config *cfg, const pk_kv16_cache *cache, const int32_t *states, int32_t bound, const void *q,
+                            const pk_strides *qs, const pk_fp8_scores *scores, void *out, const pk_strides *os, float *lse, void *workspace,
+                            size_t workspace_bytes, void *stream);
+
+typedef struct {
+    int32_t n_seq;       /* 1 .. 4096                                                                  */
+    int32_t n_kv_heads;  /* >= 1                                                                       */
+    int32_t n_q_heads;   /* multiple of n_kv_heads, at most 64 of them per KV head                     */
+    int32_t head_dim;    /* 64, 96, 128 or 256                                                         */
+    int32_t dtype;       /* pk_dtype of q, k, v and out                                                */
+} pk_prompt_config;
+
+/*
+ * Causal attention of whole prompts in packed tensors: token i of a sequence sees its tokens 0 .. i, less what the window masks.
+ *   q, k, v    (token, head) as above, n_tokens rows; out in the same type
+ *   starts     DEVICE int32 [n_seq + 1], as pk_pages_update leaves it (from pk_pages_update's counts >= 0).  Values are clamped to [0, n_tokens]; sequences may be empty
+ *   scores     as for the 8-bit cache; positions are the tokens' numbers in their sequence
+ *   lse        optional float [n_q_heads][n_tokens]: log-sum-exp of the scores
+ * Rows of out and lse that belong to no sequence are left as they were.  A token that is masked for a query does not contribute to it, whatever
+ * K and V hold there.  Strides, accumulation and rounding as for pk_kv16_attention.  Needs no workspace.  `out` does not overlap with the inputs.
+ */
+pk_status pk_prompt_attention(const pk_prompt_config *cfg, const void *q, const void *k, const void *v, const pk_strides *qs, const pk_strides *ks,
+                              const pk_strides *vs, const int32_t *starts, int32_t n_tokens, const pk_fp8_scores *scores, void *out,
+                              const pk_strides *os, float *lse, void *stream);
 
 #ifdef __cplusplus
 }

@@ -56,6 +56,8 @@ struct Fp8AttentionArgs {
 int64_t fp8_attention_parts(int64_t n_seq, int64_t n_kv_heads, int64_t r, int64_t n_query, int d, int64_t bound);
 inline int64_t fp8_attention_slots(int64_t n_seq, int64_t parts) { return n_seq + parts; }
 hipError_t launch_fp8_attention(Fp8AttentionArgs &a, hipStream_t s);
+// The pieces of every row together; the pieces are as pk_attention.h deals them out.
+hipError_t launch_attention_merge(const Fp8AttentionArgs &a, hipStream_t s);
 
 struct Fp8WeightsArgs {
     Fp8Queries in;

@@ -1,0 +1,75 @@
+// The paged 16-bit cache, its pages and the attention of prompts (pk_pages_*, pk_kv16_*, pk_prompt_attention of include/patternkv.h): what the
+// translation units share.
+#pragma once
+
+#include "pk_fp8.h"
+
+namespace pk {
+
+typedef short short4v __attribute__((ext_vector_type(4)));
+typedef short short8v __attribute__((ext_vector_type(8)));   // 16-bit operands of a matrix instruction, of either type
+typedef __bf16 bf8v __attribute__((ext_vector_type(8)));
+typedef float float16v __attribute__((ext_vector_type(16)));
+
+struct PagesArgs {
+    int32_t n_seq, page_shift, n_pages, pages_per_seq, n_tokens;
+    int32_t *table, *free_pages;
+    const int32_t *n_free;
+    int32_t *n_free_out;      // may be n_free
+    const int32_t *states;
+    int32_t *states_out;      // may be states
+    const int32_t *counts;
+    int32_t *starts, *slots, *positions, *taken;   // positions may be null
+    int32_t *first;           // workspace [n_seq + 1]: where on the stack the pages of a sequence come from; the number of pages that are free with those given back
+};
+hipError_t launch_pages(const PagesArgs &a, hipStream_t s);
+
+struct Kv16AppendArgs {
+    void *k, *v;
+    const void *k_new, *v_new;
+    int64_t k_token, k_head, v_token, v_head;      // strides in elements
+    const int32_t *slots;
+    int32_t n_tokens, n_kv_heads, d, page_shift, n_slots;
+};
+hipError_t launch_kv16_append(const Kv16AppendArgs &a, hipStream_t s);
+
+// The 8-bit cache's arguments with 16-bit vectors in the places of the codes; n_query is 1.
+int64_t kv16_attention_parts(int64_t n_seq, int64_t n_kv_heads, int64_t r, int d, int64_t bound);
+hipError_t launch_kv16_attention(Fp8AttentionArgs &a, hipStream_t s);
+
+struct PromptArgs {
+    const void *q, *k, *v;
+    void *out;
+    float *lse;               // or null
+    const int32_t *starts;
+    const float *slopes;      // or null
+    int64_t q_token, q_head, k_token, k_head, v_token, v_head, o_token, o_head;   // strides in elements
+    float scale, cap;
+    int32_t window;
+    int32_t n_seq, n_kv_heads, r, d, bf16, n_tokens;
+};
+hipError_t launch_prompt(const PromptArgs &a, hipStream_t s);
+// Workgroups of the launch: row tiles of all sequences and KV heads at most
+int64_t prompt_workgroups(int64_t n_seq, int64_t n_kv_heads, int64_t r, int64_t n_tokens, int d);
+
+// ---- device helpers ---------------------------------------------------------------------------------------------------
+
+template <bool BF16>
+__device__ __forceinline__ float4v mfma16(short8v a, short8v b, float4v c)   // 16 x 16 x 32
+{
+    if constexpr (BF16) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf8v, a), __builtin_bit_cast(bf8v, b), c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(half8v, a), __builtin_bit_cast(half8v, b), c, 0, 0, 0);
+}
+template <bool BF16>
+__device__ __forceinline__ float16v mfma32(short8v a, short8v b, float16v c)   // 32 x 32 x 16
+{
+    if constexpr (BF16) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf8v, a), __builtin_bit_cast(bf8v, b), c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8v, a), __builtin_bit_cast(half8v, b), c, 0, 0, 0);
+}
+
+// Softmax numerators are 2^(score - reference).  fp16's smallest step is 2^-24, so that its numerators go up to 2^11 (a token counts down to
+// 2^-36 of the largest one); bf16 has the exponents of binary32.
+template <bool BF16>
+constexpr float kAbove = BF16 ? 0.f : 11.f;
+
+}  // namespace pk

@@ -695,3 +695,273 @@ def pk_fp8_evict(cfg: Fp8Config, cache: Fp8Cache, to_cfg: Fp8Config, to: Fp8Cach
     _check(_lib.pk_fp8_evict(cfg.packed, cache.packed, cache.states.data_ptr(), to_cfg.packed, to.packed, to.states.data_ptr(), budget, keep_first,
                              keep_last, None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.numel(),
                              _fp8_stream(cfg, cache)), "pk_fp8_evict")
+
+
+# ---- the paged 16-bit cache, its pages, prompts ------------------------------------------------------------------------------
+
+_pack_pages_config = struct.Struct("@4i").pack
+_pack_pages = struct.Struct("@4P").pack
+_pack_kv16_config = struct.Struct("@8i").pack
+_pack_kv16_cache = struct.Struct("@3P").pack
+_pack_prompt_config = struct.Struct("@5i").pack
+
+_lib.pk_pages_workspace_bytes.restype = C.c_size_t
+_lib.pk_pages_workspace_bytes.argtypes = [C.c_void_p]
+_lib.pk_pages_update.restype = C.c_int
+_lib.pk_pages_update.argtypes = [C.c_void_p] * 5 + [C.c_int32] + [C.c_void_p] * 5 + [C.c_size_t, C.c_void_p]
+_lib.pk_kv16_cache_bytes.restype = C.c_uint64
+_lib.pk_kv16_cache_bytes.argtypes = [C.c_void_p]
+_lib.pk_kv16_workspace_bytes.restype = C.c_size_t
+_lib.pk_kv16_workspace_bytes.argtypes = [C.c_void_p, C.c_int64]
+_lib.pk_kv16_append.restype = C.c_int
+_lib.pk_kv16_append.argtypes = [C.c_void_p] * 7 + [C.c_int32, C.c_void_p]
+_lib.pk_kv16_attention.restype = C.c_int
+_lib.pk_kv16_attention.argtypes = [C.c_void_p] * 3 + [C.c_int32] + [C.c_void_p] * 7 + [C.c_size_t, C.c_void_p]
+_lib.pk_prompt_attention.restype = C.c_int
+_lib.pk_prompt_attention.argtypes = [C.c_void_p] * 8 + [C.c_int32] + [C.c_void_p] * 5
+
+
+def _need(true, what):
+    if not true:
+        raise ValueError(what)
+
+
+def _numbers(t: torch.Tensor, shape: tuple, device, name: str, dtype=torch.int32):
+    """The pointer of a contiguous tensor of that shape."""
+    if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous() or t.device != device:
+        raise ValueError(f"{name}: expected contiguous {dtype} {list(shape)} on {device}, got {t.dtype} {list(t.shape)} on {t.device}")
+    return t.data_ptr()
+
+
+def _stream_of(device):
+    # the launches go to the current device's stream, so the memory has to be that device's
+    if device.type != "cuda" or device.index != torch.cuda.current_device():
+        raise ValueError(f"the tensors are on {device}, which is not the current device")
+    return _raw_stream(device.index)
+
+
+def _workspace_of(workspace, need: int, device):
+    if workspace is None:
+        return torch.empty(need, dtype=torch.uint8, device=device) if need else None
+    if workspace.dtype != torch.uint8 or not workspace.is_contiguous() or workspace.device != device:
+        raise ValueError(f"workspace: expected contiguous uint8 on {device}")
+    return workspace
+
+
+def _packed_strides(t: torch.Tensor, shape: tuple, dtype, device, name: str) -> bytes:
+    """The strides of a [tokens (or sequences), heads, d] tensor, those of dimensions of one element (which carry no meaning) 0."""
+    if t.dtype != dtype or tuple(t.shape) != shape or t.device != device:
+        raise ValueError(f"{name}: expected {dtype} {list(shape)} on {device}, got {t.dtype} {list(t.shape)} on {t.device}")
+    s = t.stride()
+    if s[2] != 1:
+        raise ValueError(f"{name}: the elements of a vector must be adjacent")
+    first = s[0] if shape[0] > 1 else 0
+    return _pack_strides(first, first, s[1] if shape[1] > 1 else 0)
+
+
+def _scores_of(n_q_heads: int, device, softmax_scale, cap, window, slopes) -> bytes:
+    if window:
+        _fp8_int(window, "window")
+    return _pack_fp8_scores(softmax_scale, cap, window, 0 if slopes is None else _numbers(slopes, (n_q_heads,), device, "slopes", torch.float32))
+
+
+@dataclass(frozen=True)
+class PagesConfig:
+    n_seq: int = 1
+    page_tokens: int = 128
+    n_pages: int = 1
+    pages_per_seq: int = 1   # entries of a sequence's row of the table
+
+    def __post_init__(self):
+        object.__setattr__(self, "packed", _pack_pages_config(self.n_seq, self.page_tokens, self.n_pages, self.pages_per_seq))
+        object.__setattr__(self, "workspace_bytes", int(_lib.pk_pages_workspace_bytes(self.packed)))
+
+
+class PagePool:
+    """A pool of pages: `table` int32 [n_seq, pages_per_seq] (what the caches take as page_table), `free` int32 [n_pages], a stack of the free pages, and
+    `n_free` int32 [4] (how many there are, 0, 0, 0).  A new pool has all pages free.  The tensors may be ones that the caller has; they
+    stay the same for the pool's life."""
+
+    def __init__(self, cfg: PagesConfig, device="cuda", table: torch.Tensor | None = None, free: torch.Tensor | None = None, n_free: torch.Tensor | None = None):
+        self.cfg = cfg
+        if table is not None:
+            device = table.device
+        self.table = torch.zeros((cfg.n_seq, cfg.pages_per_seq), dtype=torch.int32, device=device) if table is None else table
+        self.device = self.table.device
+        _need((free is None) == (n_free is None), "free and n_free belong together")
+        if free is None:
+            free = torch.arange(cfg.n_pages - 1, -1, -1, dtype=torch.int32, device=self.device)
+            n_free = torch.tensor([cfg.n_pages, 0, 0, 0], dtype=torch.int32, device=self.device)
+        self.free, self.n_free = free, n_free
+        self._pointers = (_numbers(self.table, (cfg.n_seq, cfg.pages_per_seq), self.device, "table"), _numbers(free, (cfg.n_pages,), self.device, "free"),
+                          _numbers(n_free, (4,), self.device, "n_free"))
+        self.packed = _pack_pages(*self._pointers, 0)
+
+
+@dataclass
+class PagesPlan:
+    """What pk_pages_update leaves for a step's other calls, int32 on the device: starts [n_seq + 1], slots and positions [n_tokens], taken [n_seq]."""
+    starts: torch.Tensor
+    slots: torch.Tensor
+    positions: torch.Tensor
+    taken: torch.Tensor
+
+
+def pk_pages_plan(cfg: PagesConfig, n_tokens: int, device="cuda") -> PagesPlan:
+    """Memory for a plan (to be passed to pk_pages_update as `out`, where a step is captured once and replayed)."""
+    # one allocation, parts at multiples of 16 bytes
+    up = lambda n: -(-n // 4) * 4   # noqa: E731
+    at = [0, up(cfg.n_seq + 1), up(cfg.n_seq), up(n_tokens), up(n_tokens)]
+    for i in range(1, 5):
+        at[i] += at[i - 1]
+    buf = torch.empty(at[4], dtype=torch.int32, device=device)
+    return PagesPlan(starts=buf[:cfg.n_seq + 1], taken=buf[at[1]:at[1] + cfg.n_seq], slots=buf[at[2]:at[2] + n_tokens], positions=buf[at[3]:at[3] + n_tokens])
+
+
+def pk_pages_update(cfg: PagesConfig, pool: PagePool, states: torch.Tensor, counts: torch.Tensor, n_tokens: int, states_out: torch.Tensor | None = None,
+                    n_free_out: torch.Tensor | None = None, out: PagesPlan | None = None, workspace: torch.Tensor | None = None) -> PagesPlan:
+    """Tables, slots and states of a step: counts int32 [n_seq] on the device, new tokens of every sequence (negative: its last tokens are given back),
+    n_tokens the rows of the step's packed tensors.  states int32 [n_seq, 4]; the new ones go there, or to states_out, and the number of
+    free pages to the pool's n_free, or to n_free_out [4], in which cases the old ones stay as they are."""
+    if cfg is not pool.cfg and cfg != pool.cfg:
+        raise ValueError("the pool was made for another configuration")
+    dev, n = pool.device, cfg.n_seq
+    _need(0 <= _fp8_int(n_tokens, "n_tokens"), "n_tokens: negative")
+    if out is None:
+        out = pk_pages_plan(cfg, n_tokens, dev)
+    workspace = _workspace_of(workspace, cfg.workspace_bytes, dev)
+    packed = pool.packed if n_free_out is None else _pack_pages(*pool._pointers, _numbers(n_free_out, (4,), dev, "n_free_out"))
+    _check(_lib.pk_pages_update(cfg.packed, packed, _numbers(states, (n, 4), dev, "states"),
+                                None if states_out is None else _numbers(states_out, (n, 4), dev, "states_out"), _numbers(counts, (n,), dev, "counts"),
+                                n_tokens, _numbers(out.starts, (n + 1,), dev, "starts"), _numbers(out.slots, (n_tokens,), dev, "slots"),
+                                _numbers(out.positions, (n_tokens,), dev, "positions"), _numbers(out.taken, (n,), dev, "taken"),
+                                None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.numel(),
+                                _stream_of(dev)), "pk_pages_update")
+    return out
+
+
+@dataclass(frozen=True)
+class Kv16Config:
+    n_seq: int = 1
+    n_kv_heads: int = 1
+    n_q_heads: int = 1
+    head_dim: int = 128
+    t_capacity: int = 0
+    dtype: int = DTYPE_FP16
+    page_tokens: int = 128
+    n_pages: int = 1
+
+    def __post_init__(self):
+        object.__setattr__(self, "packed", _pack_kv16_config(self.n_seq, self.n_kv_heads, self.n_q_heads, self.head_dim, self.t_capacity, self.dtype,
+                                                             self.page_tokens, self.n_pages))
+        object.__setattr__(self, "torch_dtype", torch.bfloat16 if self.dtype == DTYPE_BF16 else torch.float16)
+        object.__setattr__(self, "_workspaces", {})
+
+
+def pk_kv16_cache_bytes(cfg: Kv16Config) -> int:
+    return int(_lib.pk_kv16_cache_bytes(cfg.packed))
+
+
+def pk_kv16_workspace_bytes(cfg: Kv16Config, bound: int) -> int:
+    need = cfg._workspaces.get(bound)   # (another thread may clear them at any point)
+    if need is None:
+        if len(cfg._workspaces) > 4096:
+            cfg._workspaces.clear()
+        need = cfg._workspaces[bound] = int(_lib.pk_kv16_workspace_bytes(cfg.packed, bound))
+    return need
+
+
+class Kv16Cache:
+    """Device memory of a paged 16-bit cache: `k`, `v` [n_pages, n_kv_heads, page_tokens, d], `states` int32 [n_seq, 4] (tokens held, next position, 0, 0)
+    and `page_table` int32 [n_seq, t_capacity / page_tokens] (a PagePool's `table`).  They may be tensors that the caller has; they stay the same for the
+    cache's life."""
+
+    def __init__(self, cfg: Kv16Config, device="cuda", k: torch.Tensor | None = None, v: torch.Tensor | None = None, states: torch.Tensor | None = None,
+                 page_table: torch.Tensor | None = None):
+        self.cfg = cfg
+        _need(pk_kv16_cache_bytes(cfg) > 0, f"not a configuration of a 16-bit cache: {cfg}")
+        shape = (cfg.n_pages, cfg.n_kv_heads, cfg.page_tokens, cfg.head_dim)
+        if k is not None:
+            device = k.device
+        self.k = torch.zeros(shape, dtype=cfg.torch_dtype, device=device) if k is None else k
+        self.device = self.k.device
+        self.v = torch.zeros(shape, dtype=cfg.torch_dtype, device=self.device) if v is None else v
+        self.states = torch.zeros((cfg.n_seq, 4), dtype=torch.int32, device=self.device) if states is None else states
+        table_shape = (cfg.n_seq, cfg.t_capacity // cfg.page_tokens)
+        self.page_table = torch.zeros(table_shape, dtype=torch.int32, device=self.device) if page_table is None else page_table
+        _numbers(self.states, (cfg.n_seq, 4), self.device, "states")
+        self.packed = _pack_kv16_cache(_numbers(self.k, shape, self.device, "k", cfg.torch_dtype), _numbers(self.v, shape, self.device, "v", cfg.torch_dtype),
+                                       _numbers(self.page_table, table_shape, self.device, "page_table"))
+
+    @property
+    def lengths(self) -> torch.Tensor:
+        """Tokens held by every sequence (a view of the states)."""
+        return self.states[:, 0]
+
+
+def _kv16_same(cfg: Kv16Config, cache: Kv16Cache):
+    if cfg is not cache.cfg and cfg != cache.cfg:
+        raise ValueError("the cache was made for another configuration")
+
+
+def pk_kv16_append(cfg: Kv16Config, cache: Kv16Cache, k_new: torch.Tensor, v_new: torch.Tensor, slots: torch.Tensor):
+    """Put k_new, v_new [n_tokens, n_kv_heads, d] (strides in multiples of 8; elements of a vector adjacent) in the slots [n_tokens] that
+    pk_pages_update gave them; rows with slot -1 are left out.  The states are pk_pages_update's to move."""
+    _kv16_same(cfg, cache)
+    n, dev = k_new.shape[0], cache.device
+    shape = (n, cfg.n_kv_heads, cfg.head_dim)
+    ks, vs = _packed_strides(k_new, shape, cfg.torch_dtype, dev, "k_new"), _packed_strides(v_new, shape, cfg.torch_dtype, dev, "v_new")
+    _check(_lib.pk_kv16_append(cfg.packed, cache.packed, k_new.data_ptr(), v_new.data_ptr(), ks, vs, _numbers(slots, (n,), dev, "slots"), n,
+                               _stream_of(dev)), "pk_kv16_append")
+
+
+def pk_kv16_attention(cfg: Kv16Config, cache: Kv16Cache, q: torch.Tensor, softmax_scale: float, cap: float = 0.0, window: int = 0,
+                      slopes: torch.Tensor | None = None, bound: int | None = None, out: torch.Tensor | None = None, lse: torch.Tensor | None = None,
+                      workspace: torch.Tensor | None = None) -> torch.Tensor:
+    """Attention of the last token of every sequence, q [n_seq, n_q_heads, d], over the tokens that the cache holds -> out, the same shape and type, laid out
+    like q.  Strides, cap, window and slopes as in pk_fp8_attention.  bound: no sequence holds more tokens than this (default: the
+    capacity); sizes the launch.  lse float32 [n_seq, n_q_heads] receives the log-sum-exp."""
+    _kv16_same(cfg, cache)
+    dev, shape = cache.device, (cfg.n_seq, cfg.n_q_heads, cfg.head_dim)
+    qs = _packed_strides(q, shape, cfg.torch_dtype, dev, "q")
+    o = torch.empty_like(q) if out is None else out   # laid out like q where q is dense (then its strides serve for both)
+    os_ = qs if out is None and o.stride() == q.stride() else _packed_strides(o, shape, cfg.torch_dtype, dev, "out")
+    bound = cfg.t_capacity if bound is None else _fp8_int(bound, "bound")
+    workspace = _workspace_of(workspace, pk_kv16_workspace_bytes(cfg, bound), dev)
+    _check(_lib.pk_kv16_attention(cfg.packed, cache.packed, cache.states.data_ptr(), bound, q.data_ptr(), qs,
+                                  _scores_of(cfg.n_q_heads, dev, softmax_scale, cap, window, slopes), o.data_ptr(), os_,
+                                  None if lse is None else _numbers(lse, shape[:2], dev, "lse", torch.float32),
+                                  None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.numel(), _stream_of(dev)),
+           "pk_kv16_attention")
+    return o
+
+
+@dataclass(frozen=True)
+class PromptConfig:
+    n_seq: int = 1
+    n_kv_heads: int = 1
+    n_q_heads: int = 1
+    head_dim: int = 128
+    dtype: int = DTYPE_FP16
+
+    def __post_init__(self):
+        object.__setattr__(self, "packed", _pack_prompt_config(self.n_seq, self.n_kv_heads, self.n_q_heads, self.head_dim, self.dtype))
+        object.__setattr__(self, "torch_dtype", torch.bfloat16 if self.dtype == DTYPE_BF16 else torch.float16)
+
+
+def pk_prompt_attention(cfg: PromptConfig, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, starts: torch.Tensor, softmax_scale: float, cap: float = 0.0,
+                        window: int = 0, slopes: torch.Tensor | None = None, out: torch.Tensor | None = None, lse: torch.Tensor | None = None) -> torch.Tensor:
+    """Causal attention of whole prompts, packed: q [n_tokens, n_q_heads, d], k and v [n_tokens, n_kv_heads, d], sequence i in rows
+    starts[i] .. starts[i + 1] (int32 [n_seq + 1] on the device) -> out, the same shape and type as q.  Strides, cap, window and slopes as in pk_fp8_attention.
+    lse float32 [n_q_heads, n_tokens] receives the log-sum-exp.  Rows of no sequence are left as they were in out and lse (without `out`: undefined)."""
+    dev, n = q.device, q.shape[0]
+    shape, kv_shape = (n, cfg.n_q_heads, cfg.head_dim), (n, cfg.n_kv_heads, cfg.head_dim)
+    qs = _packed_strides(q, shape, cfg.torch_dtype, dev, "q")
+    ks, vs = _packed_strides(k, kv_shape, cfg.torch_dtype, dev, "k"), _packed_strides(v, kv_shape, cfg.torch_dtype, dev, "v")
+    o = torch.empty(shape, dtype=q.dtype, device=dev) if out is None else out
+    os_ = _packed_strides(o, shape, cfg.torch_dtype, dev, "out")
+    _check(_lib.pk_prompt_attention(cfg.packed, q.data_ptr(), k.data_ptr(), v.data_ptr(), qs, ks, vs, _numbers(starts, (cfg.n_seq + 1,), dev, "starts"), n,
+                                    _scores_of(cfg.n_q_heads, dev, softmax_scale, cap, window, slopes), o.data_ptr(), os_,
+                                    None if lse is None else _numbers(lse, (cfg.n_q_heads, n), dev, "lse", torch.float32), _stream_of(dev)),
+           "pk_prompt_attention")
+    return o
