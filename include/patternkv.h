@@ -619,7 +619,8 @@ pk_status pk_kv16_append(const pk_kv16_config *cfg, const pk_kv16_cache *cache, 
  * A sequence that holds no token has out = 0 and lse = -inf.  Slots behind the tokens held never contribute, whatever they hold, nor do tokens that the window masks.
  * Strides of 0 are taken in the inputs; in `out` none is shorter than a vector.  Scores and outputs are accumulated in binary32; softmax
  * numerators are rounded to the 16-bit type (fp16: off by up to 2^-11 of themselves, or 2^-36 of the largest one where they are smaller; bf16: 2^-8), their
- * sum, which makes the log-sum-exp, is not.
+ * sum, which makes the log-sum-exp, is not.  Finite values have no result beyond the type's
+ * largest; an infinite one that is seen makes it infinite, or NaN where its numerator rounds to 0.
  */
 pk_status pk_kv16_attention(const pk_kv16_config *cfg, const pk_kv16_cache *cache, const int32_t *states, int32_t bound, const void *q,
                             const pk_strides *qs, const pk_fp8_scores *scores, void *out, const pk_strides *os, float *lse, void *workspace,

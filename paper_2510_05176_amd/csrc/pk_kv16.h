@@ -67,9 +67,21 @@ __device__ __forceinline__ float16v mfma32(short8v a, short8v b, float16v c)   /
     else return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8v, a), __builtin_bit_cast(half8v, b), c, 0, 0, 0);
 }
 
-// Softmax numerators are 2^(score - reference).  fp16's smallest step is 2^-24, so that its numerators go up to 2^11 (a token counts down to
-// 2^-36 of the largest one); bf16 has the exponents of binary32.
+// Softmax numerators are 2^(score - reference).  The reference for a largest score `top`: fp16's smallest step is 2^-24, so that its numerators go up to
+// 2^11 (a token counts down to 2^-36 of the largest one); scores of 2^20 and more, whose own steps are large, are the reference themselves.  bf16 has
+// the exponents of binary32: numerators of up to 2^-25, so that values up to the type's largest times 2^25 tokens stay finite.
 template <bool BF16>
-constexpr float kAbove = BF16 ? 0.f : 11.f;
+__device__ __forceinline__ float reference_of(float top)
+{
+    if constexpr (BF16) return top + 25.f;
+    else return fabsf(top) < 0x1p20f ? top - 11.f : top;
+}
+// A mean of values of the type is none beyond its largest, but the numerators' rounding may bring it there.
+template <bool BF16>
+__device__ __forceinline__ float mean_of(float x)
+{
+    constexpr float most = BF16 ? 0x1.fep127f : 65504.f;
+    return fabsf(x) < INFINITY ? fminf(fmaxf(x, -most), most) : x;
+}
 
 }  // namespace pk

@@ -50,7 +50,8 @@ __device__ __forceinline__ void load_values(uint32_t (&v)[Part<D>::kWords], cons
     }
 }
 
-// Pairs of numerators in the 16-bit type
+// Numerators as an operand.  (For bf16 a second term of what the first leaves would take its rounding out of the result, 2.1e-3 -> 1.7e-3 of it in the root mean
+// square beside the 1.7e-3 of the result's own, but makes NaN of an infinite value that is seen.)
 template <bool BF16>
 __device__ __forceinline__ short8v numerators(const float (&p)[8])
 {
@@ -186,8 +187,7 @@ __global__ __launch_bounds__(64 * NW, 2) void kv16_attention_kernel(Fp8Attention
                 by[rt] = 1.f;
                 if (top > most[rt]) {
                     most[rt] = top;
-                    // (of scores whose own steps are large, the largest is the reference itself)
-                    const float to = fabsf(top) < 0x1p20f ? top - kAbove<BF16> : top;
+                    const float to = reference_of<BF16>(top);
                     by[rt] = exp2_(m[rt] - to);
                     m[rt] = to;
                     l[rt] *= by[rt];
@@ -249,7 +249,9 @@ __global__ __launch_bounds__(64 * NW, 2) void kv16_attention_kernel(Fp8Attention
             l[rt] = fold_rows(one, AddF());
             const float inv = l[rt] == 0.f ? 0.f : 1.f / l[rt];
 #pragma unroll
-            for (int ct = 0; ct < S::kTiles; ++ct) o[rt][ct] *= inv;
+            for (int ct = 0; ct < S::kTiles; ++ct)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[rt][ct][i] = mean_of<BF16>(o[rt][ct][i] * inv);
         }
         constexpr int kAtOnce = (D == 256 ? 8 : 16) * 4 / NW, kPad = 4;   // rows at a time: 32 to 34 KB of LDS
         __shared__ float sm_o[NW][kAtOnce][D + kPad];

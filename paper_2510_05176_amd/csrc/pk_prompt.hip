@@ -278,8 +278,7 @@ __global__ __launch_bounds__(PromptShape<D>::kThreads, D == 256 ? 1 : 2) void pr
             float by = 1.f;
             if (top > most) {
                 most = top;
-                // (of scores whose own steps are large, the largest is the reference itself)
-                const float to = fabsf(top) < 0x1p20f ? top - kAbove<BF16> : top;
+                const float to = reference_of<BF16>(top);
                 by = exp2_(m - to);
                 m = to;
                 l *= by;
@@ -370,9 +369,12 @@ __global__ __launch_bounds__(PromptShape<D>::kThreads, D == 256 ? 1 : 2) void pr
 #pragma unroll
     for (int ct = 0; ct < S::kTiles; ++ct)
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-            *reinterpret_cast<uint2 *>(to + 2 * (32 * ct + 8 * i)) = make_uint2(narrow(o[ct][4 * i] * inv, o[ct][4 * i + 1] * inv, BF16),
-                                                                               narrow(o[ct][4 * i + 2] * inv, o[ct][4 * i + 3] * inv, BF16));
+        for (int i = 0; i < 4; ++i) {
+            float y[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) y[e] = mean_of<BF16>(o[ct][4 * i + e] * inv);
+            *reinterpret_cast<uint2 *>(to + 2 * (32 * ct + 8 * i)) = make_uint2(narrow(y[0], y[1], BF16), narrow(y[2], y[3], BF16));
+        }
     if (a.lse && h == 0) {
         // l's power of two joins the reference first: their sum is small where the log-sum-exp is, and takes no rounding of l's whole logarithm
         int e;
