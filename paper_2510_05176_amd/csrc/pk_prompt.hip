@@ -6,6 +6,7 @@
 // so softmax numerators go from one product to the other in registers.  K and V lie in LDS, row major, in tiles of 64 keys that all waves
 // walk together; V's operands are read transposed.  Rows are padded so that neither read has bank conflicts.
 #include <cfloat>
+#include <type_traits>
 
 #include "pk_attention.h"
 #include "pk_kv16.h"
@@ -16,9 +17,12 @@ namespace {
 
 constexpr int kKeys = 64;   // of a tile
 
+typedef uint32_t word4 __attribute__((ext_vector_type(4)));
+
 template <int D>
 struct PromptShape {
-    static constexpr int kWaves = 4, kThreads = 64 * kWaves, kRows = 32 * kWaves;   // of a workgroup
+    static constexpr int kGroups = D == 256 ? 1 : 2;   // of four waves
+    static constexpr int kWaves = 4 * kGroups, kThreads = 64 * kWaves, kRows = 32 * kWaves;   // of a workgroup
     static constexpr int kSteps = D / 16;    // of the contraction over channels
     static constexpr int kTiles = D / 32;    // of channels of the result
     static constexpr int kPieces = kKeys * D / 8, kPer = (kPieces + kThreads - 1) / kThreads;   // 16-byte pieces of a tile, per thread
@@ -123,23 +127,25 @@ __device__ __forceinline__ bool find_tile(const PromptArgs &a, int w, int *sm, i
     return true;
 }
 
-// Whether a 32-bit word has a 16-bit value that is infinite or NaN
+// A word's 16-bit values that are infinite or NaN
 template <bool BF16>
-__device__ __forceinline__ bool not_finite(uint32_t w)
+__device__ __forceinline__ uint32_t not_finite(uint32_t w)
 {
     constexpr uint32_t e = BF16 ? 0x7f80u : 0x7c00u;
-    return (w & e) == e || ((w >> 16) & e) == e;
+    return ((w & e) == e ? 0xffffu : 0u) | (((w >> 16) & e) == e ? 0xffff0000u : 0u);
 }
 
+// Groups of four waves, one wave of each on every SIMD.  With two of them a step of the loop has two phases, barriers between them: one group is at its
+// matrix instructions (the products with V of the last tile and with K of the next) while the other one computes softmax numerators, then they change places.
 template <int D, bool BF16, bool OPT>
-__global__ __launch_bounds__(PromptShape<D>::kThreads, D == 256 ? 1 : 2) void prompt_kernel(PromptArgs a)
+__global__ __launch_bounds__(PromptShape<D>::kThreads, PromptShape<D>::kGroups) void prompt_kernel(PromptArgs a)
 {
     using S = PromptShape<D>;
     const int tid = threadIdx.x, lane = tid & 63, n = lane & 31, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     __shared__ __attribute__((aligned(16))) char sm_k[2][kKeys * S::kKRow];
     __shared__ __attribute__((aligned(16))) char sm_v[2][kKeys * S::kVRow];
-    __shared__ int sm_bad[2][S::kWaves];   // whether V of the tile has infinities or NaN, looked at where some row does not see all of the tile
+    __shared__ int sm_special;   // V has infinities or NaN in a tile that some row does not see all of
     // heads next to each other: with eight of them every XCD has one head's keys in its cache
     const int kvh = blockIdx.x % a.n_kv_heads;
     int seq, tile;
@@ -149,14 +155,36 @@ __global__ __launch_bounds__(PromptShape<D>::kThreads, D == 256 ? 1 : 2) void pr
     const Prompt p = prompt_of(a, seq);
     const int start = __builtin_amdgcn_readfirstlane(p.start), len = __builtin_amdgcn_readfirstlane(p.len);
     const int rows = len * a.r, row0 = tile * S::kRows, wave_row = row0 + 32 * wave;
-    const bool has_rows = wave_row < rows;
 
     // the row (those behind the last one stand in for it, and are not stored)
     const int row = min(wave_row + n, rows - 1), tok = row / a.r, head = kvh * a.r + row - tok * a.r;
-    const auto token_of = [&](int at) { return min(at, rows - 1) / a.r; };
+    const auto token_of = [&](int at) { return __builtin_amdgcn_readfirstlane(min(at, rows - 1) / a.r); };
     const int first_tok = token_of(row0), last_tok = token_of(row0 + S::kRows - 1), wave_first = token_of(wave_row), wave_last = token_of(wave_row + 31);
     const auto first_key = [&](int token) { return a.window > 0 ? max(token - a.window + 1, 0) : 0; };
-    const int lo = first_key(first_tok) & ~(kKeys - 1), hi = last_tok + 1;
+    const int lo = first_key(first_tok) & ~(kKeys - 1), hi = last_tok + 1, tiles = (hi - lo + kKeys - 1) / kKeys;
+
+    const char *k_from = static_cast<const char *>(a.k) + 2 * (start * a.k_token + kvh * a.k_head);
+    const char *v_from = static_cast<const char *>(a.v) + 2 * (start * a.v_token + kvh * a.v_head);
+    // pieces of a tile that are on their way: of K, of V
+    word4 k_new[S::kPer], v_new[S::kPer];
+    const auto fetch = [&](word4 (&to)[S::kPer], const char *from, int64_t token, int t0) {
+#pragma unroll
+        for (int j = 0; j < S::kPer; ++j) {
+            const int piece = tid + j * S::kThreads;
+            if (S::kPieces % S::kThreads != 0 && piece >= S::kPieces) break;
+            const int64_t t = min(t0 + piece / (D / 8), len - 1);   // (behind the last token: it again; those keys are masked)
+            to[j] = *reinterpret_cast<const word4 *>(from + 2 * t * token + piece % (D / 8) * 16);
+        }
+    };
+    const auto lay_down = [&](const word4 (&from)[S::kPer], char *to, int row_bytes) {
+#pragma unroll
+        for (int j = 0; j < S::kPer; ++j) {
+            const int piece = tid + j * S::kThreads;
+            if (S::kPieces % S::kThreads != 0 && piece >= S::kPieces) break;
+            *reinterpret_cast<word4 *>(to + piece / (D / 8) * row_bytes + piece % (D / 8) * 16) = from[j];
+        }
+    };
+    fetch(k_new, k_from, a.k_token, lo);
 
     short8v q[S::kSteps];
     {
@@ -174,207 +202,229 @@ __global__ __launch_bounds__(PromptShape<D>::kThreads, D == 256 ? 1 : 2) void pr
     const float slope = OPT && a.slopes ? a.slopes[head] * kLog2e : 0.f;
 
     float m = -INFINITY, most = -INFINITY, l = 0.f;   // the numerators' reference, the largest score that it serves, their sum in this lane
-    float16v o[S::kTiles];
+    float16v o[S::kTiles], s[2];
+    short8v pf[4];
 #pragma unroll
     for (int ct = 0; ct < S::kTiles; ++ct)
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[ct][i] = 0.f;
 
-    const char *k_from = static_cast<const char *>(a.k) + 2 * (start * a.k_token + kvh * a.k_head);
-    const char *v_from = static_cast<const char *>(a.v) + 2 * (start * a.v_token + kvh * a.v_head);
-    // pieces of a tile that are on their way: of K, of V
-    uint4 k_new[S::kPer], v_new[S::kPer];
-    const auto fetch = [&](int t0) {
-#pragma unroll
-        for (int j = 0; j < S::kPer; ++j) {
-            const int piece = tid + j * S::kThreads;
-            if (S::kPieces % S::kThreads != 0 && piece >= S::kPieces) break;
-            const int64_t t = min(t0 + piece / (D / 8), len - 1);   // (behind the last token: it again; those keys are masked)
-            const int at = piece % (D / 8) * 16;
-            k_new[j] = *reinterpret_cast<const uint4 *>(k_from + 2 * t * a.k_token + at);
-            v_new[j] = *reinterpret_cast<const uint4 *>(v_from + 2 * t * a.v_token + at);
-        }
-    };
-    const auto lay_down = [&](int t0, int buf) {
-        bool bad = false;
-        const bool look = t0 + kKeys - 1 > first_tok || t0 < first_key(last_tok);
-#pragma unroll
-        for (int j = 0; j < S::kPer; ++j) {
-            const int piece = tid + j * S::kThreads;
-            if (S::kPieces % S::kThreads != 0 && piece >= S::kPieces) break;
-            const int key = piece / (D / 8), at = piece % (D / 8) * 16;
-            *reinterpret_cast<uint4 *>(sm_k[buf] + key * S::kKRow + at) = k_new[j];
-            *reinterpret_cast<uint4 *>(sm_v[buf] + key * S::kVRow + at) = v_new[j];
-            if (look) bad |= not_finite<BF16>(v_new[j].x) || not_finite<BF16>(v_new[j].y) || not_finite<BF16>(v_new[j].z) || not_finite<BF16>(v_new[j].w);
-        }
-        if (look) {
-            const bool any = __any(bad);
-            if (lane == 0) sm_bad[buf][wave] = any;
-        }
-    };
-
     const int k_at = n * S::kKRow + 16 * h, v_at = (4 * h + ((lane & 15) >> 2)) * S::kVRow + 32 * ((lane >> 4) & 1) + 8 * (lane & 3);
-    const auto v_operand = [&](int buf, int t, int ct) {   // of keys 16 t + 8 (j / 4) + 4 h + j % 4, channels 32 ct + n
+    const auto k_operand = [&](int buf, int i, int j) -> short8v { return *reinterpret_cast<const short8v *>(sm_k[buf] + k_at + 32 * j * S::kKRow + 32 * i); };
+    const auto v_operand = [&](int buf, int t, int ct) -> short8v {   // of keys 16 t + 8 (j / 4) + 4 h + j % 4, channels 32 ct + n
         typedef __attribute__((address_space(3))) short4v *lds4;
         const char *at = sm_v[buf] + v_at + 16 * t * S::kVRow + 64 * ct;
         const short4v x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(at));
         const short4v y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(at + 8 * S::kVRow));
         return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
     };
+    const auto sees = [&](int t) { return t <= tok && (a.window <= 0 || tok - t < a.window); };
 
-    fetch(lo);
-    lay_down(lo, 0);
-    int buf = 0;
-    for (int t0 = lo; t0 < hi; t0 += kKeys, buf ^= 1) {
-        __syncthreads();
-        const bool more = t0 + kKeys < hi;
-        if (more) fetch(t0 + kKeys);
-        if (has_rows && t0 <= wave_last && t0 + kKeys > first_key(wave_first)) {
-            float16v s[2];
+    // Products with V of tile i - 1 (WITH_V) and with K of tile i (WITH_K).  Operands are read from LDS kAhead products ahead.
+    const auto multiply = [&](int i, auto with_v, auto with_k) {
+        constexpr bool kV = decltype(with_v)::value, kK = decltype(with_k)::value;
+        constexpr int kOfV = kV ? 4 * S::kTiles : 0, kAll = kOfV + (kK ? 2 * S::kSteps : 0), kAhead = 4;
+        const int k_buf = i & 1, v_buf = k_buf ^ 1;
+        const auto operand = [&](int u) -> short8v {
+            if (u < kOfV) return v_operand(v_buf, u / S::kTiles, u % S::kTiles);
+            return k_operand(k_buf, (u - kOfV) / 2, (u - kOfV) % 2);
+        };
+        short8v ahead[kAhead];
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) ahead[u] = operand(u);
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (kK)
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
-                for (int i = 0; i < 16; ++i) s[j][i] = 0.f;
+                for (int e = 0; e < 16; ++e) s[j][e] = 0.f;
 #pragma unroll
-            for (int i = 0; i < S::kSteps; ++i)
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-                    s[j] = mfma32<BF16>(*reinterpret_cast<const short8v *>(sm_k[buf] + k_at + 32 * j * S::kKRow + 32 * i), q[i], s[j]);
-
-            const bool edge = t0 + kKeys - 1 > wave_first || t0 < first_key(wave_last);
-            const auto sees = [&](int t) { return t <= tok && (a.window <= 0 || tok - t < a.window); };
-            float x[2][16], f = c;
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) x[j][i] = s[j][i];
-            if constexpr (OPT) {
-                const float inv = a.cap > 0.f ? fminf(fabsf(a.scale) / a.cap, FLT_MAX) : 0.f, both[2] = {inv, inv};
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    if (a.cap > 0.f) {
-                        capped(x[j], both, a.cap * kLog2e);
-                    } else {
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) x[j][i] *= c;
-                    }
-                    if (a.slopes) {
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) x[j][i] = fmaf(-slope, (float)(tok - (t0 + 32 * j + 8 * (i >> 2) + 4 * h + (i & 3))), x[j][i]);
-                    }
-                }
-                f = 1.f;
-            }
-            if (edge) {
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) x[j][i] = sees(t0 + 32 * j + 8 * (i >> 2) + 4 * h + (i & 3)) ? x[j][i] : -INFINITY;
-            }
-            float top = x[0][0];
-#pragma unroll
-            for (int i = 1; i < 32; ++i) top = fmaxf(top, x[i >> 4][i & 15]);
-            top = op_rows(swap32(bits_of(top), bits_of(top)), MaxF()) * f;
-            float by = 1.f;
-            if (top > most) {
-                most = top;
-                const float to = reference_of<BF16>(top);
-                by = exp2_(m - to);
-                m = to;
-                l *= by;
-            }
-            if (__any(by != 1.f)) {
-#pragma unroll
-                for (int ct = 0; ct < S::kTiles; ++ct) o[ct] *= by;
-            }
-            const float ref = m == -INFINITY ? 0.f : m;
-            float sum = 0.f;
-            if (__any(fabsf(ref) >= 0x1p20f)) {
-                // scores of large steps as their largest is, rounded; the multiply-add would take their factor in unrounded
-#pragma unroll
-                for (int i = 0; i < 32; ++i) {
-                    float y = x[i >> 4][i & 15] * f;
-                    asm volatile("" : "+v"(y));   // (not contracted)
-                    x[i >> 4][i & 15] = exp2_(y - ref);
-                }
-            } else {
-#pragma unroll
-                for (int i = 0; i < 32; ++i) x[i >> 4][i & 15] = exp2_(fmaf(x[i >> 4][i & 15], f, -ref));
-            }
-#pragma unroll
-            for (int i = 0; i < 32; ++i) sum += x[i >> 4][i & 15];
-            l += sum;
-            short8v pf[4];
-#pragma unroll
-            for (int t = 0; t < 4; ++t) {
-                const float *y = &x[t >> 1][8 * (t & 1)];
-                const uint4 w = make_uint4(narrow(y[0], y[1], BF16), narrow(y[2], y[3], BF16), narrow(y[4], y[5], BF16), narrow(y[6], y[7], BF16));
-                pf[t] = __builtin_bit_cast(short8v, w);
-            }
-
-            bool bad = false;
-            if (edge) {
-                int any = 0;
-#pragma unroll
-                for (int w = 0; w < S::kWaves; ++w) any |= sm_bad[buf][w];
-                bad = __builtin_amdgcn_readfirstlane(any) != 0;
-            }
-            if (!bad) {
-#pragma unroll
-                for (int t = 0; t < 4; ++t)
-#pragma unroll
-                    for (int ct = 0; ct < S::kTiles; ++ct) o[ct] = mfma32<BF16>(v_operand(buf, t, ct), pf[t], o[ct]);
-            } else {
-                // Values that are not finite reach only the rows that see them: they are taken out, and products of marks (1.0 for +inf or NaN, for -inf
-                // or NaN) and of who sees whom say which results have one.
-                constexpr short kOne = BF16 ? 0x3f80 : 0x3c00;
-                constexpr int kExp = BF16 ? 0x7f80 : 0x7c00, kMant = BF16 ? 0x007f : 0x03ff;
-#pragma unroll 1
-                for (int t = 0; t < 4; ++t) {
-                    short8v see, pt;
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) see[i] = sees(t0 + 16 * t + 8 * (i >> 2) + 4 * h + (i & 3)) ? kOne : (short)0;
-                    pt = t == 0 ? pf[0] : t == 1 ? pf[1] : t == 2 ? pf[2] : pf[3];
-#pragma unroll
-                    for (int ct = 0; ct < S::kTiles; ++ct) {
-                        short8v v = v_operand(buf, t, ct), up, down;
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const bool odd = (v[i] & kExp) == kExp, nan = odd && (v[i] & kMant) != 0;
-                            up[i] = odd && (nan || v[i] >= 0) ? kOne : (short)0;
-                            down[i] = odd && (nan || v[i] < 0) ? kOne : (short)0;
-                            v[i] = odd ? (short)0 : v[i];
-                        }
-                        float16v none;
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) none[i] = 0.f;
-                        const float16v ups = mfma32<BF16>(up, see, none), downs = mfma32<BF16>(down, see, none);
-                        o[ct] = mfma32<BF16>(v, pt, o[ct]);
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            if (ups[i] > 0.f) o[ct][i] += INFINITY;
-                            if (downs[i] > 0.f) o[ct][i] -= INFINITY;
-                        }
-                    }
-                }
-            }
+        for (int u = 0; u < kAll; ++u) {
+            if (u < kOfV) o[u % S::kTiles] = mfma32<BF16>(ahead[u % kAhead], pf[u / S::kTiles], o[u % S::kTiles]);
+            else s[(u - kOfV) % 2] = mfma32<BF16>(ahead[u % kAhead], q[(u - kOfV) / 2], s[(u - kOfV) % 2]);
+            if (u + kAhead < kAll) ahead[u % kAhead] = operand(u + kAhead);
+            __builtin_amdgcn_sched_barrier(0x6);   // (arithmetic may be moved across)
         }
-        if (more) lay_down(t0 + kKeys, buf ^ 1);
+    };
+
+    // From the products with K of tile i to its numerators
+    const auto soften = [&](int i) {
+        const int t0 = lo + i * kKeys;
+        const bool edge = t0 + kKeys - 1 > wave_first || t0 < first_key(wave_last);
+        float f = c;
+        if constexpr (OPT) {
+            const float inv = a.cap > 0.f ? fminf(fabsf(a.scale) / a.cap, FLT_MAX) : 0.f, both[2] = {inv, inv};
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                float x[16];
+#pragma unroll
+                for (int e = 0; e < 16; ++e) x[e] = s[j][e];
+                if (a.cap > 0.f) {
+                    capped(x, both, a.cap * kLog2e);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) x[e] *= c;
+                }
+                if (a.slopes) {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) x[e] = fmaf(-slope, (float)(tok - (t0 + 32 * j + 8 * (e >> 2) + 4 * h + (e & 3))), x[e]);
+                }
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[j][e] = x[e];
+            }
+            f = 1.f;
+        }
+        if (edge) {
+#pragma unroll
+            for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int e = 0; e < 16; ++e) s[j][e] = sees(t0 + 32 * j + 8 * (e >> 2) + 4 * h + (e & 3)) ? s[j][e] : -INFINITY;
+        }
+        float top = s[0][0];
+#pragma unroll
+        for (int e = 1; e < 32; ++e) top = fmaxf(top, s[e >> 4][e & 15]);
+        top = op_rows(swap32(bits_of(top), bits_of(top)), MaxF()) * f;
+        float by = 1.f;
+        if (top > most) {
+            most = top;
+            const float to = reference_of<BF16>(top);
+            by = exp2_(m - to);
+            m = to;
+            l *= by;
+        }
+        if (__any(by != 1.f)) {
+#pragma unroll
+            for (int ct = 0; ct < S::kTiles; ++ct) o[ct] *= by;
+        }
+        const float ref = m == -INFINITY ? 0.f : m;
+        float sum = 0.f;
+        if (__any(fabsf(ref) >= 0x1p20f)) {
+            // scores of large steps as their largest is, rounded; the multiply-add would take their factor in unrounded
+#pragma unroll
+            for (int e = 0; e < 32; ++e) {
+                float y = s[e >> 4][e & 15] * f;
+                asm volatile("" : "+v"(y));   // (not contracted)
+                s[e >> 4][e & 15] = exp2_(y - ref);
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) s[e >> 4][e & 15] = exp2_(fmaf(s[e >> 4][e & 15], f, -ref));
+        }
+#pragma unroll
+        for (int e = 0; e < 32; ++e) sum += s[e >> 4][e & 15];
+        l += sum;
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            const float16v &y = s[t >> 1];
+            const int e = 8 * (t & 1);
+            const uint4 w = make_uint4(narrow(y[e], y[e + 1], BF16), narrow(y[e + 2], y[e + 3], BF16), narrow(y[e + 4], y[e + 5], BF16), narrow(y[e + 6], y[e + 7], BF16));
+            pf[t] = __builtin_bit_cast(short8v, w);
+        }
+    };
+    // K of tile i + 1 and V of tile i: asked for, and (a phase later) put where tile i - 1's and i - 2's were
+    const auto ask = [&](int i) {
+        fetch(k_new, k_from, a.k_token, lo + (i + 1) * kKeys);
+        fetch(v_new, v_from, a.v_token, lo + i * kKeys);
+    };
+    // whether a tile is seen in part by some row of the workgroup
+    const auto in_part = [&](int t0) { return t0 + kKeys - 1 > first_tok || t0 < first_key(last_tok); };
+    const auto put = [&](int i) {
+        if (in_part(lo + i * kKeys)) {
+            // Values that are not finite would make NaN of a masked key's numerator of 0: they are taken out, and rows that see them get them afterwards.
+            uint32_t bad = 0;
+#pragma unroll
+            for (int j = 0; j < S::kPer; ++j) {
+                if (S::kPieces % S::kThreads != 0 && tid + j * S::kThreads >= S::kPieces) break;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t out = not_finite<BF16>(v_new[j][e]);
+                    v_new[j][e] &= ~out;
+                    bad |= out;
+                }
+            }
+            if (bad) sm_special = 1;
+        }
+        lay_down(k_new, sm_k[(i + 1) & 1], S::kKRow);
+        lay_down(v_new, sm_v[i & 1], S::kVRow);
+    };
+    constexpr auto yes = std::integral_constant<bool, true>();
+    constexpr auto no = std::integral_constant<bool, false>();
+    const auto change = [&] {
+        __builtin_amdgcn_sched_barrier(0);
+        __syncthreads();
+        __builtin_amdgcn_sched_barrier(0);
+    };
+
+    if (tid == 0) sm_special = 0;
+    lay_down(k_new, sm_k[0], S::kKRow);
+    if (S::kGroups == 1 || wave < 4) {
+        change();
+        ask(0);
+        multiply(0, no, yes);
+        change();
+        soften(0);
+        put(0);
+        change();
+        for (int i = 1; i < tiles; ++i) {
+            ask(i);
+            multiply(i, yes, yes);
+            change();
+            soften(i);
+            put(i);
+            change();
+        }
+        multiply(tiles, yes, no);
+    } else {
+        change();
+        ask(0);
+        change();
+        multiply(0, no, yes);
+        put(0);
+        change();
+        for (int i = 1; i < tiles; ++i) {
+            ask(i);
+            soften(i - 1);
+            change();
+            multiply(i, yes, yes);
+            put(i);
+            change();
+        }
+        soften(tiles - 1);
+        multiply(tiles, yes, no);
     }
 
-    if (!has_rows || wave_row + n >= rows) return;
     l = op_rows(swap32(bits_of(l), bits_of(l)), AddF());
     const float inv = l == 0.f ? 0.f : 1.f / l;
+#pragma unroll
+    for (int ct = 0; ct < S::kTiles; ++ct)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) o[ct][i] = mean_of<BF16>(o[ct][i] * inv);
+    if (sm_special) {   // (written before a barrier that all have passed)
+        for (int t = lo; t < hi; ++t) {
+            if (!in_part(t & ~(kKeys - 1)) || !sees(t)) continue;
+            const char *at = v_from + 2 * ((int64_t)t * a.v_token + 4 * h);
+#pragma unroll
+            for (int ct = 0; ct < S::kTiles; ++ct)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint2 w = *reinterpret_cast<const uint2 *>(at + 2 * (32 * ct + 8 * i));
+                    const uint32_t x = not_finite<BF16>(w.x), y = not_finite<BF16>(w.y);
+                    if ((x | y) == 0) continue;
+                    float v[4];
+                    widen(w.x & x, BF16, v[0], v[1]);
+                    widen(w.y & y, BF16, v[2], v[3]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[ct][4 * i + e] += v[e];
+                }
+        }
+    }
+    if (wave_row + n >= rows) return;
     char *to = static_cast<char *>(a.out) + 2 * ((start + tok) * a.o_token + head * a.o_head + 4 * h);
 #pragma unroll
     for (int ct = 0; ct < S::kTiles; ++ct)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            float y[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) y[e] = mean_of<BF16>(o[ct][4 * i + e] * inv);
-            *reinterpret_cast<uint2 *>(to + 2 * (32 * ct + 8 * i)) = make_uint2(narrow(y[0], y[1], BF16), narrow(y[2], y[3], BF16));
-        }
+        for (int i = 0; i < 4; ++i)
+            *reinterpret_cast<uint2 *>(to + 2 * (32 * ct + 8 * i)) = make_uint2(narrow(o[ct][4 * i], o[ct][4 * i + 1], BF16), narrow(o[ct][4 * i + 2], o[ct][4 * i + 3], BF16));
     if (a.lse && h == 0) {
         // l's power of two joins the reference first: their sum is small where the log-sum-exp is, and takes no rounding of l's whole logarithm
         int e;
