@@ -67,15 +67,20 @@ __device__ __forceinline__ float16v mfma32(short8v a, short8v b, float16v c)   /
     else return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(half8v, a), __builtin_bit_cast(half8v, b), c, 0, 0, 0);
 }
 
-// Softmax numerators are 2^(score - reference).  The reference for a largest score `top`: fp16's smallest step is 2^-24, so that its numerators go up to
-// 2^11 (a token counts down to 2^-36 of the largest one); scores of 2^20 and more, whose own steps are large, are the reference themselves.  bf16 has
-// the exponents of binary32: numerators of up to 2^-25, so that values up to the type's largest times 2^25 tokens stay finite.
+// Softmax numerators are 2^(score - reference).  The reference for a largest score `top` serves scores up to kRoom above it, so that it moves a few times in a
+// row, not with every larger score.  fp16's smallest step is 2^-24, so that its numerators go up to 2^11, 2^15 with the room (a token counts down to 2^-36 of the
+// largest one); scores of 2^20 and more, whose own steps are large, are the reference themselves.  bf16 has the exponents of binary32: numerators
+// of up to 2^-25 with the room, so that values up to the type's largest times 2^25 tokens stay finite.
+constexpr float kRoom = 4.f;
 template <bool BF16>
 __device__ __forceinline__ float reference_of(float top)
 {
-    if constexpr (BF16) return top + 25.f;
+    if constexpr (BF16) return top + (25.f + kRoom);
     else return fabsf(top) < 0x1p20f ? top - 11.f : top;
 }
+// From here on scores are rounded before the reference is taken off, as their largest is: the multiply-add would take the factor in unrounded, and the numerator
+// of a row's only token would be no power of two, which the 16-bit type holds exactly.
+constexpr float kLarge = 0x1p12f;
 // A mean of values of the type is none beyond its largest, but the numerators' rounding may bring it there.
 template <bool BF16>
 __device__ __forceinline__ float mean_of(float x)

@@ -186,7 +186,7 @@ __global__ __launch_bounds__(64 * NW, 2) void kv16_attention_kernel(Fp8Attention
                 top = fold_rows(one, MaxF());
                 by[rt] = 1.f;
                 if (top > most[rt]) {
-                    most[rt] = top;
+                    most[rt] = fabsf(top) < 0x1p20f ? top + kRoom : top;
                     const float to = reference_of<BF16>(top);
                     by[rt] = exp2_(m[rt] - to);
                     m[rt] = to;
@@ -195,8 +195,8 @@ __global__ __launch_bounds__(64 * NW, 2) void kv16_attention_kernel(Fp8Attention
                 moved |= by[rt] != 1.f;
                 const float ref = m[rt] == -INFINITY ? 0.f : m[rt];
                 float e[8], sum = 0.f;
-                if (__any(fabsf(ref) >= 0x1p20f)) {
-                    // scores of large steps as their largest is, rounded; the multiply-add would take their factor in unrounded
+                if (__any(fabsf(ref) >= kLarge)) {
+                    // (see kLarge)
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         x[i] *= f;

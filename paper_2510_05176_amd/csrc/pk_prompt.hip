@@ -7,6 +7,7 @@
 // walk together; V's operands are read transposed.  Rows are padded so that neither read has bank conflicts.
 #include <cfloat>
 #include <type_traits>
+#include <utility>
 
 #include "pk_attention.h"
 #include "pk_kv16.h"
@@ -25,10 +26,21 @@ struct PromptShape {
     static constexpr int kWaves = 4 * kGroups, kThreads = 64 * kWaves, kRows = 32 * kWaves;   // of a workgroup
     static constexpr int kSteps = D / 16;    // of the contraction over channels
     static constexpr int kTiles = D / 32;    // of channels of the result
-    static constexpr int kPieces = kKeys * D / 8, kPer = (kPieces + kThreads - 1) / kThreads;   // 16-byte pieces of a tile, per thread
-    static constexpr int kKRow = 2 * D + 16;   // bytes between rows in LDS: 16 rows from any 16-byte column on lie in 64 different banks,
-    static constexpr int kVRow = 2 * D + (D == 96 ? 0 : 64);   // and four rows of 64 bytes do
+    static constexpr int kRow = D == 96 ? 256 : 2 * D;   // bytes of a key in LDS
+    static constexpr int kSlots = kRow / 16, kTileBytes = kKeys * kRow;
+    static constexpr int kLoaders = 256, kPer = kKeys * kSlots / kLoaders;   // threads that bring the tiles in: the first group's; 16-byte pieces of a tile for each
+    // Which piece of a key's vector lies in which slot of its row: piece ^ swizzle, so that 16 keys' pieces of the same number (K's operands) and 64
+    // bytes of four keys (V's) lie in 64 different banks.
+    static __device__ __forceinline__ int k_swizzle(int key) { return D == 64 ? (key >> 1) & 7 : key & 15; }
+    static __device__ __forceinline__ int v_swizzle(int key) { return D == 64 ? ((key >> 1) & 1) << 2 : (key & 3) << 2; }
 };
+
+// f(0), f(1), ..: unrolled whatever its size
+template <typename F, int... I>
+__device__ __forceinline__ void for_each(F &&f, std::integer_sequence<int, I...>)
+{
+    (f(std::integral_constant<int, I>()), ...);
+}
 
 // Sum of an int over the wave, in every lane
 __device__ __forceinline__ int wave_sum(int x)
@@ -143,14 +155,13 @@ __global__ __launch_bounds__(PromptShape<D>::kThreads, PromptShape<D>::kGroups) 
     using S = PromptShape<D>;
     const int tid = threadIdx.x, lane = tid & 63, n = lane & 31, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    __shared__ __attribute__((aligned(16))) char sm_k[2][kKeys * S::kKRow];
-    __shared__ __attribute__((aligned(16))) char sm_v[2][kKeys * S::kVRow];
+    __shared__ __attribute__((aligned(16))) char sm[4][S::kTileBytes];   // K of two tiles, V of two
     __shared__ int sm_special;   // V has infinities or NaN in a tile that some row does not see all of
     // heads next to each other: with eight of them every XCD has one head's keys in its cache
     const int kvh = blockIdx.x % a.n_kv_heads;
     int seq, tile;
-    static_assert(sizeof(sm_k) >= (4096 + S::kWaves) * 4, "numbers of find_tile");
-    if (!find_tile<S::kRows, S::kThreads>(a, blockIdx.x / a.n_kv_heads, reinterpret_cast<int *>(sm_k), seq, tile)) return;
+    static_assert(sizeof(sm) >= (4096 + S::kWaves) * 4, "numbers of find_tile");
+    if (!find_tile<S::kRows, S::kThreads>(a, blockIdx.x / a.n_kv_heads, reinterpret_cast<int *>(sm), seq, tile)) return;
     seq = __builtin_amdgcn_readfirstlane(seq);
     const Prompt p = prompt_of(a, seq);
     const int start = __builtin_amdgcn_readfirstlane(p.start), len = __builtin_amdgcn_readfirstlane(p.len);
@@ -165,26 +176,37 @@ __global__ __launch_bounds__(PromptShape<D>::kThreads, PromptShape<D>::kGroups) 
 
     const char *k_from = static_cast<const char *>(a.k) + 2 * (start * a.k_token + kvh * a.k_head);
     const char *v_from = static_cast<const char *>(a.v) + 2 * (start * a.v_token + kvh * a.v_head);
-    // pieces of a tile that are on their way: of K, of V
-    word4 k_new[S::kPer], v_new[S::kPer];
-    const auto fetch = [&](word4 (&to)[S::kPer], const char *from, int64_t token, int t0) {
+    // A tile's way into LDS, without registers in between.  Lane l of a wave's request writes 16 l bytes behind the request's place; what it reads is its to choose.
+    // (The compiler would wait for it before every read from LDS that follows, whatever tile that is of; it has no registers to wait for, and arrive() waits for it.  m0 is a reserved register, set before each use.)
+    // A lane's part of the addresses is the same for every whole tile, where strides let it fit 32 bits.
+    uint32_t k_lane[S::kPer], v_lane[S::kPer];
 #pragma unroll
+    for (int j = 0; j < S::kPer; ++j) {
+        const int slot = tid + j * S::kLoaders, key = slot / S::kSlots;
+        k_lane[j] = 2 * key * (uint32_t)a.k_token + 16 * ((slot % S::kSlots) ^ S::k_swizzle(key));
+        v_lane[j] = 2 * key * (uint32_t)a.v_token + 16 * ((slot % S::kSlots) ^ S::v_swizzle(key));
+    }
+    const bool k_fits = a.k_token >= 0 && a.k_token <= 1 << 24, v_fits = a.v_token >= 0 && a.v_token <= 1 << 24;
+    const auto place_of_piece = [&](const char *tile_at, int j) {
+        return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char *)tile_at) + 1024 * (wave + 4 * j);
+    };
+    const auto has_piece = [&](int j, bool v) {   // (96 channels leave four of sixteen slots empty)
+        const int slot = tid + j * S::kLoaders, key = slot / S::kSlots;
+        return D != 96 || ((slot % S::kSlots) ^ (v ? S::v_swizzle(key) : S::k_swizzle(key))) < D / 8;
+    };
+    const auto request_whole = [&](int j, const char *tile_from, const uint32_t (&lane_at)[S::kPer], const char *to, bool v) {
+        if (has_piece(j, v)) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(place_of_piece(to, j)), "v"(lane_at[j]), "s"(tile_from) : "memory");
+    };
+    // a tile that the sequence ends in, or with strides that do not fit: all of it
+    const auto request_slowly = [&](const char *from, int64_t token, int t0, const char *to, bool v) {
+#pragma unroll 1
         for (int j = 0; j < S::kPer; ++j) {
-            const int piece = tid + j * S::kThreads;
-            if (S::kPieces % S::kThreads != 0 && piece >= S::kPieces) break;
-            const int64_t t = min(t0 + piece / (D / 8), len - 1);   // (behind the last token: it again; those keys are masked)
-            to[j] = *reinterpret_cast<const word4 *>(from + 2 * t * token + piece % (D / 8) * 16);
+            const int slot = tid + j * S::kLoaders, key = slot / S::kSlots, piece = (slot % S::kSlots) ^ (v ? S::v_swizzle(key) : S::k_swizzle(key));
+            const int64_t t = min(t0 + key, len - 1);   // (behind the last token: it again; those keys are masked)
+            if (has_piece(j, v)) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(place_of_piece(to, j)), "v"(from + 2 * t * token + 16 * piece) : "memory");
         }
     };
-    const auto lay_down = [&](const word4 (&from)[S::kPer], char *to, int row_bytes) {
-#pragma unroll
-        for (int j = 0; j < S::kPer; ++j) {
-            const int piece = tid + j * S::kThreads;
-            if (S::kPieces % S::kThreads != 0 && piece >= S::kPieces) break;
-            *reinterpret_cast<word4 *>(to + piece / (D / 8) * row_bytes + piece % (D / 8) * 16) = from[j];
-        }
-    };
-    fetch(k_new, k_from, a.k_token, lo);
+    if (S::kGroups == 1 || wave < 4) request_slowly(k_from, a.k_token, lo, sm[0], false);
 
     short8v q[S::kSteps];
     {
@@ -209,19 +231,45 @@ __global__ __launch_bounds__(PromptShape<D>::kThreads, PromptShape<D>::kGroups) 
 #pragma unroll
         for (int i = 0; i < 16; ++i) o[ct][i] = 0.f;
 
-    const int k_at = n * S::kKRow + 16 * h, v_at = (4 * h + ((lane & 15) >> 2)) * S::kVRow + 32 * ((lane >> 4) & 1) + 8 * (lane & 3);
-    const auto k_operand = [&](int buf, int i, int j) -> short8v { return *reinterpret_cast<const short8v *>(sm_k[buf] + k_at + 32 * j * S::kKRow + 32 * i); };
+    const int k_at = n * S::kRow, k_piece = 16 * (S::k_swizzle(n) ^ h);
+    const int v_key = 4 * h + ((lane & 15) >> 2), v_at = v_key * S::kRow + 32 * ((lane >> 4) & 1) + 8 * (lane & 3), v_piece = 16 * S::v_swizzle(v_key);
+    const auto k_operand = [&](int buf, int i, int j) -> short8v {
+        return *reinterpret_cast<const short8v *>(sm[buf] + k_at + 32 * j * S::kRow + (k_piece ^ (32 * i)));
+    };
     const auto v_operand = [&](int buf, int t, int ct) -> short8v {   // of keys 16 t + 8 (j / 4) + 4 h + j % 4, channels 32 ct + n
         typedef __attribute__((address_space(3))) short4v *lds4;
-        const char *at = sm_v[buf] + v_at + 16 * t * S::kVRow + 64 * ct;
+        const char *at = sm[2 + buf] + v_at + 16 * t * S::kRow + (v_piece ^ (64 * ct));
         const short4v x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(at));
-        const short4v y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(at + 8 * S::kVRow));
+        const short4v y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(at + 8 * S::kRow));
         return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
     };
     const auto sees = [&](int t) { return t <= tok && (a.window <= 0 || tok - t < a.window); };
 
+    // K of tile i + 1 and V of tile i: asked for piece by piece between the first group's matrix instructions (requests at once stand in line for their addresses,
+    // and beside the numerators each costs some 140 cycles), and a phase later there, where tile i - 1's and i - 2's were
+    constexpr int kRequests = 2 * S::kPer;
+    const auto asking = [&](int i) {
+        const int k_t0 = lo + (i + 1) * kKeys, v_t0 = lo + i * kKeys;
+        const char *k_to = sm[(i + 1) & 1], *v_to = sm[2 + (i & 1)];
+        const bool k_whole = k_fits && k_t0 + kKeys <= len, v_whole = v_fits && v_t0 + kKeys <= len;
+        if (!k_whole) request_slowly(k_from, a.k_token, k_t0, k_to, false);
+        if (!v_whole) request_slowly(v_from, a.v_token, v_t0, v_to, true);
+        return [=, &k_lane, &v_lane, &request_whole, k_at = k_from + 2 * k_t0 * a.k_token, v_at = v_from + 2 * v_t0 * a.v_token](int from, int to) {
+#pragma unroll
+            for (int j = 0; j < kRequests; ++j) {
+                if ((2 * j + 1) * 32 / kRequests < from || (2 * j + 1) * 32 / kRequests >= to) continue;
+                if (j < S::kPer) {
+                    if (k_whole) request_whole(j, k_at, k_lane, k_to, false);
+                } else {
+                    if (v_whole) request_whole(j - S::kPer, v_at, v_lane, v_to, true);
+                }
+            }
+        };
+    };
+    const auto nothing = [](int, int) {};
+
     // Products with V of tile i - 1 (WITH_V) and with K of tile i (WITH_K).  Operands are read from LDS kAhead products ahead.
-    const auto multiply = [&](int i, auto with_v, auto with_k) {
+    const auto multiply = [&](int i, auto with_v, auto with_k, auto &&between) {   // between(x, y): from the x-th to the y-th 64th of it
         constexpr bool kV = decltype(with_v)::value, kK = decltype(with_k)::value;
         constexpr int kOfV = kV ? 4 * S::kTiles : 0, kAll = kOfV + (kK ? 2 * S::kSteps : 0), kAhead = 4;
         const int k_buf = i & 1, v_buf = k_buf ^ 1;
@@ -238,13 +286,14 @@ __global__ __launch_bounds__(PromptShape<D>::kThreads, PromptShape<D>::kGroups) 
             for (int j = 0; j < 2; ++j)
 #pragma unroll
                 for (int e = 0; e < 16; ++e) s[j][e] = 0.f;
-#pragma unroll
-        for (int u = 0; u < kAll; ++u) {
-            if (u < kOfV) o[u % S::kTiles] = mfma32<BF16>(ahead[u % kAhead], pf[u / S::kTiles], o[u % S::kTiles]);
+        for_each([&](auto at) {
+            constexpr int u = decltype(at)::value;
+            if constexpr (u < kOfV) o[u % S::kTiles] = mfma32<BF16>(ahead[u % kAhead], pf[u / S::kTiles], o[u % S::kTiles]);
             else s[(u - kOfV) % 2] = mfma32<BF16>(ahead[u % kAhead], q[(u - kOfV) / 2], s[(u - kOfV) % 2]);
-            if (u + kAhead < kAll) ahead[u % kAhead] = operand(u + kAhead);
+            if constexpr (u + kAhead < kAll) ahead[u % kAhead] = operand(u + kAhead);
+            between(u * 64 / kAll, (u + 1) * 64 / kAll);
             __builtin_amdgcn_sched_barrier(0x6);   // (arithmetic may be moved across)
-        }
+        }, std::make_integer_sequence<int, kAll>());
     };
 
     // From the products with K of tile i to its numerators
@@ -280,13 +329,17 @@ __global__ __launch_bounds__(PromptShape<D>::kThreads, PromptShape<D>::kGroups) 
 #pragma unroll
                 for (int e = 0; e < 16; ++e) s[j][e] = sees(t0 + 32 * j + 8 * (e >> 2) + 4 * h + (e & 3)) ? s[j][e] : -INFINITY;
         }
-        float top = s[0][0];
+        float top = s[0][0], other = s[1][0];
 #pragma unroll
-        for (int e = 1; e < 32; ++e) top = fmaxf(top, s[e >> 4][e & 15]);
+        for (int e = 1; e < 16; ++e) {
+            top = fmaxf(top, s[0][e]);
+            other = fmaxf(other, s[1][e]);
+        }
+        top = fmaxf(top, other);
         top = op_rows(swap32(bits_of(top), bits_of(top)), MaxF()) * f;
         float by = 1.f;
         if (top > most) {
-            most = top;
+            most = fabsf(top) < 0x1p20f ? top + kRoom : top;
             const float to = reference_of<BF16>(top);
             by = exp2_(m - to);
             m = to;
@@ -297,55 +350,60 @@ __global__ __launch_bounds__(PromptShape<D>::kThreads, PromptShape<D>::kGroups) 
             for (int ct = 0; ct < S::kTiles; ++ct) o[ct] *= by;
         }
         const float ref = m == -INFINITY ? 0.f : m;
-        float sum = 0.f;
-        if (__any(fabsf(ref) >= 0x1p20f)) {
-            // scores of large steps as their largest is, rounded; the multiply-add would take their factor in unrounded
+        float sum[2] = {0.f, 0.f};
+        if (__any(fabsf(ref) >= kLarge)) {
+            // (see kLarge)
 #pragma unroll
             for (int e = 0; e < 32; ++e) {
                 float y = s[e >> 4][e & 15] * f;
                 asm volatile("" : "+v"(y));   // (not contracted)
-                s[e >> 4][e & 15] = exp2_(y - ref);
+                s[e >> 4][e & 15] = y - ref;
             }
         } else {
 #pragma unroll
-            for (int e = 0; e < 32; ++e) s[e >> 4][e & 15] = exp2_(fmaf(s[e >> 4][e & 15], f, -ref));
+            for (int e = 0; e < 32; ++e) s[e >> 4][e & 15] = fmaf(s[e >> 4][e & 15], f, -ref);
         }
 #pragma unroll
-        for (int e = 0; e < 32; ++e) sum += s[e >> 4][e & 15];
-        l += sum;
-#pragma unroll
         for (int t = 0; t < 4; ++t) {
-            const float16v &y = s[t >> 1];
+            float16v &y = s[t >> 1];
+#pragma unroll
+            for (int x = 8 * (t & 1); x < 8 * (t & 1) + 8; ++x) {
+                y[x] = exp2_(y[x]);
+                sum[x & 1] += y[x];
+            }
             const int e = 8 * (t & 1);
             const uint4 w = make_uint4(narrow(y[e], y[e + 1], BF16), narrow(y[e + 2], y[e + 3], BF16), narrow(y[e + 4], y[e + 5], BF16), narrow(y[e + 6], y[e + 7], BF16));
             pf[t] = __builtin_bit_cast(short8v, w);
         }
-    };
-    // K of tile i + 1 and V of tile i: asked for, and (a phase later) put where tile i - 1's and i - 2's were
-    const auto ask = [&](int i) {
-        fetch(k_new, k_from, a.k_token, lo + (i + 1) * kKeys);
-        fetch(v_new, v_from, a.v_token, lo + i * kKeys);
+        l += sum[0] + sum[1];
+        // here, not behind the barrier, where the compiler would put what is not needed before
+        asm volatile("" : "+v"(l), "+v"(pf[0]), "+v"(pf[1]), "+v"(pf[2]), "+v"(pf[3]));
     };
     // whether a tile is seen in part by some row of the workgroup
     const auto in_part = [&](int t0) { return t0 + kKeys - 1 > first_tok || t0 < first_key(last_tok); };
-    const auto put = [&](int i) {
+    const auto arrive = [&](int i) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         if (in_part(lo + i * kKeys)) {
             // Values that are not finite would make NaN of a masked key's numerator of 0: they are taken out, and rows that see them get them afterwards.
             uint32_t bad = 0;
 #pragma unroll
             for (int j = 0; j < S::kPer; ++j) {
-                if (S::kPieces % S::kThreads != 0 && tid + j * S::kThreads >= S::kPieces) break;
+                const int slot = tid + j * S::kLoaders;   // (this thread's own)
+                if (D == 96 && ((slot % S::kSlots) ^ S::v_swizzle(slot / S::kSlots)) >= D / 8) continue;
+                word4 *at = reinterpret_cast<word4 *>(sm[2 + (i & 1)] + 16 * slot);
+                word4 w = *at;
+                uint32_t here = 0;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const uint32_t out = not_finite<BF16>(v_new[j][e]);
-                    v_new[j][e] &= ~out;
-                    bad |= out;
+                    const uint32_t out = not_finite<BF16>(w[e]);
+                    w[e] &= ~out;
+                    here |= out;
                 }
+                if (here) *at = w;
+                bad |= here;
             }
             if (bad) sm_special = 1;
         }
-        lay_down(k_new, sm_k[(i + 1) & 1], S::kKRow);
-        lay_down(v_new, sm_v[i & 1], S::kVRow);
     };
     constexpr auto yes = std::integral_constant<bool, true>();
     constexpr auto no = std::integral_constant<bool, false>();
@@ -356,41 +414,35 @@ __global__ __launch_bounds__(PromptShape<D>::kThreads, PromptShape<D>::kGroups) 
     };
 
     if (tid == 0) sm_special = 0;
-    lay_down(k_new, sm_k[0], S::kKRow);
     if (S::kGroups == 1 || wave < 4) {
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         change();
-        ask(0);
-        multiply(0, no, yes);
+        multiply(0, no, yes, asking(0));
         change();
         soften(0);
-        put(0);
+        arrive(0);
         change();
         for (int i = 1; i < tiles; ++i) {
-            ask(i);
-            multiply(i, yes, yes);
+            multiply(i, yes, yes, asking(i));
             change();
             soften(i);
-            put(i);
+            arrive(i);
             change();
         }
-        multiply(tiles, yes, no);
+        multiply(tiles, yes, no, nothing);
     } else {
         change();
-        ask(0);
         change();
-        multiply(0, no, yes);
-        put(0);
+        multiply(0, no, yes, nothing);
         change();
         for (int i = 1; i < tiles; ++i) {
-            ask(i);
             soften(i - 1);
             change();
-            multiply(i, yes, yes);
-            put(i);
+            multiply(i, yes, yes, nothing);
             change();
         }
         soften(tiles - 1);
-        multiply(tiles, yes, no);
+        multiply(tiles, yes, no, nothing);
     }
 
     l = op_rows(swap32(bits_of(l), bits_of(l)), AddF());
