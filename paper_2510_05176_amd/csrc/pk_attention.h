@@ -15,14 +15,15 @@ __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(
 // x[i] = m * tanh(x[i] * c[i / 8]) in binary32.  Below 0.55 the odd Taylor series, above it 1 - 2 / (e^{2y} + 1), whose rounding is no longer
 // magnified there; how far the series goes, and whether the other form is computed at all, is the wave's largest argument's to say (the first term
 // left out is 2e-10 of the result at 0.25 and 4e-8 at 0.55).  tanh y = y + y^3 s(y^2), s from 2^(2k) (2^(2k) - 1) B_2k / (2k)!.
-__device__ __forceinline__ void capped(float (&x)[16], const float (&c)[2], float m)
+template <int N>
+__device__ __forceinline__ void capped(float (&x)[N], const float (&c)[N / 8], float m)
 {
     float most = 0.f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) most = fmaxf(most, fabsf(x[i]) * c[i >> 3]);   // (a NaN does not count and comes out of the series as one)
+    for (int i = 0; i < N; ++i) most = fmaxf(most, fabsf(x[i]) * c[i >> 3]);   // (a NaN does not count and comes out of the series as one)
     if (!__any(most >= 0.25f)) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
+        for (int i = 0; i < N; ++i) {
             const float y = x[i] * c[i >> 3], y2 = y * y;
             float s = fmaf(-1382.f / 155925.f, y2, 62.f / 2835.f);
             s = fmaf(s, y2, -17.f / 315.f);
@@ -35,7 +36,7 @@ __device__ __forceinline__ void capped(float (&x)[16], const float (&c)[2], floa
     }
     const bool far = __any(most >= 0.55f);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
+    for (int i = 0; i < N; ++i) {
         const float y = x[i] * c[i >> 3], y2 = y * y;
         float s = fmaf(-929569.f / 638512875.f, y2, 21844.f / 6081075.f);
         s = fmaf(s, y2, -1382.f / 155925.f);

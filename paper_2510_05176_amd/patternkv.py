@@ -728,7 +728,7 @@ def _need(true, what):
 
 def _numbers(t: torch.Tensor, shape: tuple, device, name: str, dtype=torch.int32):
     """The pointer of a contiguous tensor of that shape."""
-    if t.dtype != dtype or tuple(t.shape) != shape or not t.is_contiguous() or t.device != device:
+    if t.dtype != dtype or t.shape != shape or not t.is_contiguous() or t.device != device:
         raise ValueError(f"{name}: expected contiguous {dtype} {list(shape)} on {device}, got {t.dtype} {list(t.shape)} on {t.device}")
     return t.data_ptr()
 
@@ -750,7 +750,7 @@ def _workspace_of(workspace, need: int, device):
 
 def _packed_strides(t: torch.Tensor, shape: tuple, dtype, device, name: str) -> bytes:
     """The strides of a [tokens (or sequences), heads, d] tensor, those of dimensions of one element (which carry no meaning) 0."""
-    if t.dtype != dtype or tuple(t.shape) != shape or t.device != device:
+    if t.dtype != dtype or t.shape != shape or t.device != device:
         raise ValueError(f"{name}: expected {dtype} {list(shape)} on {device}, got {t.dtype} {list(t.shape)} on {t.device}")
     s = t.stride()
     if s[2] != 1:
@@ -775,6 +775,7 @@ class PagesConfig:
     def __post_init__(self):
         object.__setattr__(self, "packed", _pack_pages_config(self.n_seq, self.page_tokens, self.n_pages, self.pages_per_seq))
         object.__setattr__(self, "workspace_bytes", int(_lib.pk_pages_workspace_bytes(self.packed)))
+        object.__setattr__(self, "_parts", {})
 
 
 class PagePool:
@@ -807,15 +808,28 @@ class PagesPlan:
     taken: torch.Tensor
 
 
+def _pages_parts(cfg: PagesConfig, n_tokens: int):
+    """Where starts, taken, slots, positions and the workspace begin in one allocation of int32, each at a multiple of 16 bytes, and its size."""
+    parts = cfg._parts.get(n_tokens)   # (another thread may clear them at any point)
+    if parts is None:
+        at = [0]
+        for n in (cfg.n_seq + 1, cfg.n_seq, n_tokens, n_tokens, cfg.workspace_bytes // 4):
+            at.append(at[-1] + -(-n // 4) * 4)
+        if len(cfg._parts) > 4096:
+            cfg._parts.clear()
+        parts = cfg._parts[n_tokens] = tuple(at)
+    return parts
+
+
+def _pages_views(cfg: PagesConfig, n_tokens: int, buf: torch.Tensor, at) -> PagesPlan:
+    n = cfg.n_seq
+    return PagesPlan(buf[:n + 1], buf[at[2]:at[2] + n_tokens], buf[at[3]:at[3] + n_tokens], buf[at[1]:at[1] + n])
+
+
 def pk_pages_plan(cfg: PagesConfig, n_tokens: int, device="cuda") -> PagesPlan:
     """Memory for a plan (to be passed to pk_pages_update as `out`, where a step is captured once and replayed)."""
-    # one allocation, parts at multiples of 16 bytes
-    up = lambda n: -(-n // 4) * 4   # noqa: E731
-    at = [0, up(cfg.n_seq + 1), up(cfg.n_seq), up(n_tokens), up(n_tokens)]
-    for i in range(1, 5):
-        at[i] += at[i - 1]
-    buf = torch.empty(at[4], dtype=torch.int32, device=device)
-    return PagesPlan(starts=buf[:cfg.n_seq + 1], taken=buf[at[1]:at[1] + cfg.n_seq], slots=buf[at[2]:at[2] + n_tokens], positions=buf[at[3]:at[3] + n_tokens])
+    at = _pages_parts(cfg, n_tokens)
+    return _pages_views(cfg, n_tokens, torch.empty(at[5], dtype=torch.int32, device=device), at)
 
 
 def pk_pages_update(cfg: PagesConfig, pool: PagePool, states: torch.Tensor, counts: torch.Tensor, n_tokens: int, states_out: torch.Tensor | None = None,
@@ -827,16 +841,26 @@ def pk_pages_update(cfg: PagesConfig, pool: PagePool, states: torch.Tensor, coun
         raise ValueError("the pool was made for another configuration")
     dev, n = pool.device, cfg.n_seq
     _need(0 <= _fp8_int(n_tokens, "n_tokens"), "n_tokens: negative")
-    if out is None:
-        out = pk_pages_plan(cfg, n_tokens, dev)
-    workspace = _workspace_of(workspace, cfg.workspace_bytes, dev)
     packed = pool.packed if n_free_out is None else _pack_pages(*pool._pointers, _numbers(n_free_out, (4,), dev, "n_free_out"))
-    _check(_lib.pk_pages_update(cfg.packed, packed, _numbers(states, (n, 4), dev, "states"),
-                                None if states_out is None else _numbers(states_out, (n, 4), dev, "states_out"), _numbers(counts, (n,), dev, "counts"),
-                                n_tokens, _numbers(out.starts, (n + 1,), dev, "starts"), _numbers(out.slots, (n_tokens,), dev, "slots"),
-                                _numbers(out.positions, (n_tokens,), dev, "positions"), _numbers(out.taken, (n,), dev, "taken"),
-                                None if workspace is None else workspace.data_ptr(), 0 if workspace is None else workspace.numel(),
-                                _stream_of(dev)), "pk_pages_update")
+    before, step = _numbers(states, (n, 4), dev, "states"), _numbers(counts, (n,), dev, "counts")
+    after = None if states_out is None else _numbers(states_out, (n, 4), dev, "states_out")
+    need, stream = cfg.workspace_bytes, _stream_of(dev)
+    if workspace is not None:
+        workspace = _workspace_of(workspace, need, dev)
+    if out is None:
+        at = _pages_parts(cfg, n_tokens)
+        buf = torch.empty(at[5], dtype=torch.int32, device=dev)
+        base = buf.data_ptr()
+        starts, taken, slots, positions, ws = base, base + 4 * at[1], base + 4 * at[2], base + 4 * at[3], base + 4 * at[4]
+        out = _pages_views(cfg, n_tokens, buf, at)
+    else:
+        starts, slots = _numbers(out.starts, (n + 1,), dev, "starts"), _numbers(out.slots, (n_tokens,), dev, "slots")
+        positions, taken = _numbers(out.positions, (n_tokens,), dev, "positions"), _numbers(out.taken, (n,), dev, "taken")
+        if workspace is None:
+            workspace = _workspace_of(None, need, dev)
+    if workspace is not None:
+        ws, need = workspace.data_ptr(), workspace.numel()
+    _check(_lib.pk_pages_update(cfg.packed, packed, before, after, step, n_tokens, starts, slots, positions, taken, ws, need, stream), "pk_pages_update")
     return out
 
 
