@@ -49,8 +49,8 @@ struct PromptArgs {
     int32_t n_seq, n_kv_heads, r, d, bf16, n_tokens;
 };
 hipError_t launch_prompt(const PromptArgs &a, hipStream_t s);
-// Workgroups of the launch: row tiles of all sequences and KV heads at most
-int64_t prompt_workgroups(int64_t n_seq, int64_t n_kv_heads, int64_t r, int64_t n_tokens, int d);
+// Workgroups of the launch at most: row tiles of all sequences and KV heads
+int64_t prompt_workgroups(int64_t n_seq, int64_t n_kv_heads, int64_t r, int64_t n_tokens);
 
 // ---- device helpers ---------------------------------------------------------------------------------------------------
 

@@ -265,7 +265,7 @@ pk_status pk_prompt_attention(const pk_prompt_config *cfg, const void *q, const 
     if (n_tokens == 0) return PK_OK;
     const int64_t r = cfg->n_q_heads / cfg->n_kv_heads;
     if (n_tokens > kMostTokens || n_tokens * r > (1 << 28)) return PK_ERR_UNSUPPORTED;   // rows of a KV head, counted in 32 bits
-    if (prompt_workgroups(cfg->n_seq, cfg->n_kv_heads, r, n_tokens, cfg->head_dim) > kMostGroups) return PK_ERR_UNSUPPORTED;
+    if (prompt_workgroups(cfg->n_seq, cfg->n_kv_heads, r, n_tokens) > kMostGroups) return PK_ERR_UNSUPPORTED;
     PromptArgs a;
     std::memset(&a, 0, sizeof(a));
     a.q = q;

@@ -20,9 +20,9 @@ constexpr int kKeys = 64;   // of a tile
 
 typedef uint32_t word4 __attribute__((ext_vector_type(4)));
 
-template <int D>
+template <int D, int GROUPS>
 struct PromptShape {
-    static constexpr int kGroups = D == 256 ? 1 : 2;   // of four waves
+    static constexpr int kGroups = GROUPS;   // of four waves
     static constexpr int kWaves = 4 * kGroups, kThreads = 64 * kWaves, kRows = 32 * kWaves;   // of a workgroup
     static constexpr int kSteps = D / 16;    // of the contraction over channels
     static constexpr int kTiles = D / 32;    // of channels of the result
@@ -149,10 +149,11 @@ __device__ __forceinline__ uint32_t not_finite(uint32_t w)
 
 // Groups of four waves, one wave of each on every SIMD.  With two of them a step of the loop has two phases, barriers between them: one group is at its
 // matrix instructions (the products with V of the last tile and with K of the next) while the other one computes softmax numerators, then they change places.
-template <int D, bool BF16, bool OPT>
-__global__ __launch_bounds__(PromptShape<D>::kThreads, PromptShape<D>::kGroups) void prompt_kernel(PromptArgs a)
+// With one, what overlaps is left to the workgroups of a CU (two; three at 64 channels, one at 256).
+template <int D, int GROUPS, bool BF16, bool OPT>
+__global__ __launch_bounds__((PromptShape<D, GROUPS>::kThreads), D == 256 ? 1 : 2) void prompt_kernel(PromptArgs a)
 {
-    using S = PromptShape<D>;
+    using S = PromptShape<D, GROUPS>;
     const int tid = threadIdx.x, lane = tid & 63, n = lane & 31, h = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     __shared__ __attribute__((aligned(16))) char sm[4][S::kTileBytes];   // K of two tiles, V of two
@@ -418,13 +419,13 @@ __global__ __launch_bounds__(PromptShape<D>::kThreads, PromptShape<D>::kGroups) 
         asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         change();
         multiply(0, no, yes, asking(0));
-        change();
+        if constexpr (S::kGroups == 2) change();
         soften(0);
         arrive(0);
         change();
         for (int i = 1; i < tiles; ++i) {
             multiply(i, yes, yes, asking(i));
-            change();
+            if constexpr (S::kGroups == 2) change();
             soften(i);
             arrive(i);
             change();
@@ -485,38 +486,50 @@ __global__ __launch_bounds__(PromptShape<D>::kThreads, PromptShape<D>::kGroups) 
     }
 }
 
-template <int D>
-hipError_t launch_d(const PromptArgs &a, uint32_t grid, hipStream_t s)
+// Two groups where the matrix instructions are as long as the numerators (96 and 128 channels) and there are enough rows for two workgroups of 256 per CU: one
+// prompt of 32k tokens, 32 heads of 128 channels 7.69 ms, one group 8.24; 16 of 512 tokens 79 and 81 us; but one of 1000 tokens 32 and 29, 2048 tokens of
+// one KV head 52 and 46.  With 64 channels (a packed batch 779 and 713 us) or a cap and distance bias (8k tokens 1146 and 907) the numerators are longer, and
+// two groups that wait for each other waste the matrix unit's time; 256 channels leave registers for one wave per SIMD.
+int groups_of(int64_t rows, int d, bool opt) { return (d == 96 || d == 128) && !opt && rows >= 512 * 256 ? 2 : 1; }
+
+template <int D, int GROUPS>
+void launch_groups(const PromptArgs &a, uint32_t grid, bool opt, hipStream_t s)
 {
-    constexpr int threads = PromptShape<D>::kThreads;
-    const bool opt = a.cap > 0.f || a.slopes;
-    if (a.bf16) {
-        if (opt) prompt_kernel<D, true, true><<<grid, threads, 0, s>>>(a);
-        else prompt_kernel<D, true, false><<<grid, threads, 0, s>>>(a);
-    } else {
-        if (opt) prompt_kernel<D, false, true><<<grid, threads, 0, s>>>(a);
-        else prompt_kernel<D, false, false><<<grid, threads, 0, s>>>(a);
+    constexpr int threads = PromptShape<D, GROUPS>::kThreads;
+    if constexpr (GROUPS == 1) {
+        if (opt) {
+            if (a.bf16) prompt_kernel<D, GROUPS, true, true><<<grid, threads, 0, s>>>(a);
+            else prompt_kernel<D, GROUPS, false, true><<<grid, threads, 0, s>>>(a);
+            return;
+        }
     }
+    if (a.bf16) prompt_kernel<D, GROUPS, true, false><<<grid, threads, 0, s>>>(a);
+    else prompt_kernel<D, GROUPS, false, false><<<grid, threads, 0, s>>>(a);
+}
+
+template <int D>
+hipError_t launch_d(const PromptArgs &a, hipStream_t s)
+{
+    const bool opt = a.cap > 0.f || a.slopes;
+    const int groups = groups_of((int64_t)a.n_tokens * a.r * a.n_kv_heads, D, opt), rows = 128 * groups;
+    const uint32_t grid = (uint32_t)(((int64_t)a.n_tokens * a.r + (int64_t)a.n_seq * (rows - 1)) / rows * a.n_kv_heads);
+    if constexpr (D == 96 || D == 128) {
+        if (groups == 2) {
+            launch_groups<D, 2>(a, grid, opt, s);
+            return hipGetLastError();
+        }
+    }
+    launch_groups<D, 1>(a, grid, opt, s);
     return hipGetLastError();
 }
 
-int rows_of(int d) { return d == 64 ? PromptShape<64>::kRows : d == 96 ? PromptShape<96>::kRows : d == 128 ? PromptShape<128>::kRows : PromptShape<256>::kRows; }
-
 }  // namespace
 
-int64_t prompt_workgroups(int64_t n_seq, int64_t n_kv_heads, int64_t r, int64_t n_tokens, int d)
-{
-    const int64_t rows = rows_of(d);
-    return (n_tokens * r + n_seq * (rows - 1)) / rows * n_kv_heads;
-}
+int64_t prompt_workgroups(int64_t n_seq, int64_t n_kv_heads, int64_t r, int64_t n_tokens) { return (n_tokens * r + n_seq * 127) / 128 * n_kv_heads; }
 
 hipError_t launch_prompt(const PromptArgs &a, hipStream_t s)
 {
-    const uint32_t grid = (uint32_t)prompt_workgroups(a.n_seq, a.n_kv_heads, a.r, a.n_tokens, a.d);
-    return a.d == 64    ? launch_d<64>(a, grid, s)
-           : a.d == 96  ? launch_d<96>(a, grid, s)
-           : a.d == 128 ? launch_d<128>(a, grid, s)
-                        : launch_d<256>(a, grid, s);
+    return a.d == 64 ? launch_d<64>(a, s) : a.d == 96 ? launch_d<96>(a, s) : a.d == 128 ? launch_d<128>(a, s) : launch_d<256>(a, s);
 }
 
 }  // namespace pk

@@ -16,7 +16,7 @@ hipError_t launch_kv16_append(const Kv16AppendArgs &a, hipStream_t) { ++g_launch
 int64_t kv16_attention_parts(int64_t n_seq, int64_t, int64_t, int, int64_t bound) { return bound > 512 ? 3 * n_seq : 0; }
 hipError_t launch_kv16_attention(Fp8AttentionArgs &a, hipStream_t) { ++g_launches; g_attention = a; return hipErrorInvalidValue; }
 hipError_t launch_prompt(const PromptArgs &a, hipStream_t) { ++g_launches; g_prompt = a; return hipSuccess; }
-int64_t prompt_workgroups(int64_t n_seq, int64_t n_kv_heads, int64_t r, int64_t n_tokens, int) { return (n_tokens * r + n_seq * 127) / 128 * n_kv_heads; }
+int64_t prompt_workgroups(int64_t n_seq, int64_t n_kv_heads, int64_t r, int64_t n_tokens) { return (n_tokens * r + n_seq * 127) / 128 * n_kv_heads; }
 }  // namespace pk
 
 #define CHECK(cond)                                                  \

@@ -437,6 +437,20 @@ def test_many_prompts(pk, n_seq, most):
     run_prompts(pk, lens, hkv=1, r=3, d=64, behind=2, dtype=torch.bfloat16)
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("d", [64, 96, 128, 256])
+@pytest.mark.parametrize("how", [dict(), dict(window=50), dict(scale=-0.1)])
+def test_prompts_of_many_rows(pk, dtype, d, how):
+    """Rows enough (160000) for workgroups of two groups of waves where the rule takes them; sequences around their 16 tokens and around tiles of 64 keys, one that ends
+    inside of both, and values that are not finite."""
+    lens = [1, 15, 16, 17, 0, 63, 64, 65, 127, 129, 640] + [61] * 23
+
+    def spoil(kt, vt, starts):
+        for i, t in ((9, 100), (10, 0), (10, 333), (10, 639), (11, 60)):
+            vt[starts[i] + t, t % 4, 7] = (math.nan, math.inf, -math.inf)[t % 3]
+    run_prompts(pk, lens, hkv=4, r=16, d=d, dtype=dtype, behind=5, spoil=spoil, **how)
+
+
 def test_a_long_prompt(pk):
     for dtype, d, kw in ((torch.float16, 64, {}), (torch.bfloat16, 128, {}), (torch.bfloat16, 64, dict(window=500, slopes=True))):
         run_prompts(pk, [2500, 40], hkv=1, r=2, d=d, dtype=dtype, **kw)
