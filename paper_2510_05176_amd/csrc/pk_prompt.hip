@@ -207,7 +207,8 @@ __global__ __launch_bounds__((PromptShape<D, GROUPS>::kThreads), D == 256 ? 1 : 
             if (has_piece(j, v)) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(place_of_piece(to, j)), "v"(from + 2 * t * token + 16 * piece) : "memory");
         }
     };
-    if (S::kGroups == 1 || wave < 4) request_slowly(k_from, a.k_token, lo, sm[0], false);
+    const bool loads = S::kGroups == 1 || wave < 4;
+    if (loads) request_slowly(k_from, a.k_token, lo, sm[0], false);
 
     short8v q[S::kSteps];
     {
@@ -220,6 +221,7 @@ __global__ __launch_bounds__((PromptShape<D, GROUPS>::kThreads), D == 256 ? 1 : 
             q[s] = __builtin_bit_cast(short8v, w);
         }
     }
+    if (loads) request_slowly(v_from, a.v_token, lo, sm[2], true);
     // the products' factor; never 0, so that a masked -inf stays one
     const float c = fmaxf(fabsf(a.scale) * kLog2e, 0x1p-126f);
     const float slope = OPT && a.slopes ? a.slopes[head] * kLog2e : 0.f;
@@ -254,7 +256,7 @@ __global__ __launch_bounds__((PromptShape<D, GROUPS>::kThreads), D == 256 ? 1 : 
         const char *k_to = sm[(i + 1) & 1], *v_to = sm[2 + (i & 1)];
         const bool k_whole = k_fits && k_t0 + kKeys <= len, v_whole = v_fits && v_t0 + kKeys <= len;
         if (!k_whole) request_slowly(k_from, a.k_token, k_t0, k_to, false);
-        if (!v_whole) request_slowly(v_from, a.v_token, v_t0, v_to, true);
+        if (!v_whole && i > 0) request_slowly(v_from, a.v_token, v_t0, v_to, true);   // (the first tile's is on its way)
         return [=, &k_lane, &v_lane, &request_whole, k_at = k_from + 2 * k_t0 * a.k_token, v_at = v_from + 2 * v_t0 * a.v_token](int from, int to) {
 #pragma unroll
             for (int j = 0; j < kRequests; ++j) {
@@ -262,7 +264,7 @@ __global__ __launch_bounds__((PromptShape<D, GROUPS>::kThreads), D == 256 ? 1 : 
                 if (j < S::kPer) {
                     if (k_whole) request_whole(j, k_at, k_lane, k_to, false);
                 } else {
-                    if (v_whole) request_whole(j - S::kPer, v_at, v_lane, v_to, true);
+                    if (v_whole && i > 0) request_whole(j - S::kPer, v_at, v_lane, v_to, true);
                 }
             }
         };
@@ -415,8 +417,8 @@ __global__ __launch_bounds__((PromptShape<D, GROUPS>::kThreads), D == 256 ? 1 : 
     };
 
     if (tid == 0) sm_special = 0;
-    if (S::kGroups == 1 || wave < 4) {
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    if (loads) {
+        asm volatile("s_waitcnt vmcnt(%0)" : : "n"(S::kPer) : "memory");   // all but V's
         change();
         multiply(0, no, yes, asking(0));
         if constexpr (S::kGroups == 2) change();
