@@ -7,8 +7,8 @@
 // (pages hold 16 or more).  All heads of the call see the same tokens of a sequence, so that what is masked for one of them is so for all, and
 // V is cleared there before it reaches the product.
 //
-// HBM bounds it, 4 d bytes per token and KV head: 16 sequences x 32k tokens of 8 heads of 128 channels 358 us, 6.0 TB/s.  (The next tile asked for before this one is
-// taken: 357, and 15.0 -> 16.0 for one sequence of 1.1k tokens.)  Groups of rows over the same keys in one XCD's cache: 20 heads of 256 channels 52 -> 41 us.
+// HBM bounds it, 4 d bytes per token and KV head: 16 sequences x 32k tokens of 8 heads of 128 channels 354 us, 6.1 TB/s.  (The next tile asked for before this one is
+// taken, with two workgroups per CU: 359 -> 357, and 15.0 -> 16.0 for one sequence of 1.1k tokens.)  Groups of rows over the same keys in one XCD's cache: 20 heads of 256 channels 52 -> 41 us.
 #include <cfloat>
 
 #include "pk_attention.h"
@@ -336,12 +336,13 @@ hipError_t launch_d(Fp8AttentionArgs &a, hipStream_t s)
 
 }  // namespace
 
-// As many runs as make one round of resident workgroups, two per CU.  (Short caches whole by eight waves, with nothing to merge, 22.5 us for 2k tokens of 8
-// heads where runs of 256 take 14.7.)
+// Runs for one workgroup per CU where a run stays in one or two sequences (16 sequences x 32k tokens 354 us, 361 with two workgroups per CU; one of 32k 31 and 35, of
+// 128k 103 and 107), for two where it goes through more, each with its end (64 sequences of up to 6000 tokens 130 and 121; of up to 2000 56 and 53).  Three and four
+// per CU: 364 and 362, 122 and 126.  (Short caches whole by eight waves, with nothing to merge: 22.5 us for 2k tokens of 8 heads where runs of 256 take 14.7.)
 int64_t kv16_attention_parts(int64_t n_seq, int64_t n_kv_heads, int64_t r, int d, int64_t bound)
 {
     const int64_t rows = 16 * tiles_of(r, d), across = n_kv_heads * ((r + rows - 1) / rows);   // workgroups per run
-    int64_t parts = 512 / across;
+    int64_t parts = (256 / across >= n_seq ? 256 : 512) / across;
     if (parts < 1) parts = 1;
     if (n_seq > kMostSeqs || n_seq >= 4 * parts) return 0;
     const int64_t most = n_seq * ((bound + 64 * kLeastUnits - 1) / (64 * kLeastUnits));
