@@ -536,7 +536,7 @@ pk_status pk_fp8_evict(const pk_fp8_config *cfg, const pk_fp8_cache *cache, cons
  *   k, v [n_pages][n_kv_heads][page_tokens][d] fp16 or bf16
  * States: DEVICE int32 [n_seq][4], 16-byte aligned, as for the 8-bit cache: tokens held (clamped to [0, capacity] where it is read), position of the next token, 0, 0.
  * Packed tensors hold the tokens of a step one sequence after the other: those of sequence i are rows starts[i] .. starts[i + 1]; starts is
- *   DEVICE int32 [n_seq + 1], growing.  Their strides are pk_strides whose `seq` is not used; the d elements of a vector are contiguous,
+ *   DEVICE int32 [n_seq + 1], not falling (where they fall, rows of `out` may be left as they were or be of either sequence).  Their strides are pk_strides whose `seq` is not used; the d elements of a vector are contiguous,
  *   strides are multiples of 8, pointers 16-byte aligned.
  */
 typedef struct {
@@ -620,7 +620,7 @@ pk_status pk_kv16_append(const pk_kv16_config *cfg, const pk_kv16_cache *cache, 
  * Strides of 0 are taken in the inputs; in `out` none is shorter than a vector.  Scores and outputs are accumulated in binary32; softmax
  * numerators are rounded to the 16-bit type (fp16: off by up to 2^-11 of themselves, or 2^-36 of the largest one where they are smaller; bf16: 2^-8), their
  * sum, which makes the log-sum-exp, is not.  Finite values have no result beyond the type's
- * largest; an infinite one that is seen makes it infinite, or NaN where its numerator rounds to 0.
+ * largest; an infinite one that is seen makes it infinite, or NaN where its numerator rounds to 0.  `out` does not overlap with the inputs.
  */
 pk_status pk_kv16_attention(const pk_kv16_config *cfg, const pk_kv16_cache *cache, const int32_t *states, int32_t bound, const void *q,
                             const pk_strides *qs, const pk_fp8_scores *scores, void *out, const pk_strides *os, float *lse, void *workspace,
@@ -642,6 +642,7 @@ typedef struct {
  *   lse        optional float [n_q_heads][n_tokens]: log-sum-exp of the scores
  * Rows of out and lse that belong to no sequence are left as they were.  A token that is masked for a query does not contribute to it, whatever
  * K and V hold there.  Strides, accumulation and rounding as for pk_kv16_attention.  Needs no workspace.  `out` does not overlap with the inputs.
+ * With r query heads per KV head: n_tokens <= 2^25, n_tokens * r <= 2^28, and n_kv_heads * (n_tokens * r + 127 * n_seq) / 128 < 2^23; more is PK_ERR_UNSUPPORTED.
  */
 pk_status pk_prompt_attention(const pk_prompt_config *cfg, const void *q, const void *k, const void *v, const pk_strides *qs, const pk_strides *ks,
                               const pk_strides *vs, const int32_t *starts, int32_t n_tokens, const pk_fp8_scores *scores, void *out,

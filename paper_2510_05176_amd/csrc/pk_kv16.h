@@ -20,7 +20,7 @@ struct PagesArgs {
     int32_t *states_out;      // may be states
     const int32_t *counts;
     int32_t *starts, *slots, *positions, *taken;   // positions may be null
-    int32_t *first;           // workspace [n_seq + 1]: where on the stack the pages of a sequence come from; the number of pages that are free with those given back
+    int32_t *first;           // workspace [n_seq]: where on the stack the pages of a sequence come from
 };
 hipError_t launch_pages(const PagesArgs &a, hipStream_t s);
 
