@@ -253,7 +253,8 @@ __global__ __launch_bounds__((PromptShape<D, GROUPS>::kThreads), D == 256 ? 1 : 
         const short4v y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4)(at + 8 * S::kRow));
         return __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
     };
-    const auto sees = [&](int t) { return t <= tok && (a.window <= 0 || tok - t < a.window); };
+    const uint32_t reach = a.window > 0 ? (uint32_t)a.window : 0x80000000u;   // a token sees those less than this before it, and none behind (a difference below 0 is larger)
+    const auto sees = [&](int t) { return (uint32_t)(tok - t) < reach; };
 
     // K of tile i + 1 and V of tile i: asked for piece by piece between the first group's matrix instructions (requests at once stand in line for their addresses,
     // and beside the numerators each costs some 140 cycles), and a phase later there, where tile i - 1's and i - 2's were
@@ -319,7 +320,7 @@ __global__ __launch_bounds__((PromptShape<D, GROUPS>::kThreads), D == 256 ? 1 : 
 #pragma unroll
                 for (int e = 0; e < 16; ++e) x[e] = s[j][e];
                 if (a.cap > 0.f) {
-                    capped(x, both, a.cap * kLog2e);
+                    capped<16, true>(x, both, a.cap * kLog2e);
                 } else {
 #pragma unroll
                     for (int e = 0; e < 16; ++e) x[e] *= c;
@@ -334,10 +335,11 @@ __global__ __launch_bounds__((PromptShape<D, GROUPS>::kThreads), D == 256 ? 1 : 
             f = 1.f;
         }
         if (edge) {
+            const int back = tok - t0 - 4 * h;
 #pragma unroll
             for (int j = 0; j < 2; ++j)
 #pragma unroll
-                for (int e = 0; e < 16; ++e) s[j][e] = sees(t0 + 32 * j + 8 * (e >> 2) + 4 * h + (e & 3)) ? s[j][e] : -INFINITY;
+                for (int e = 0; e < 16; ++e) s[j][e] = (uint32_t)(back - (32 * j + 8 * (e >> 2) + (e & 3))) < reach ? s[j][e] : -INFINITY;
         }
         float top = s[0][0], other = s[1][0];
 #pragma unroll
