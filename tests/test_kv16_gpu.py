@@ -521,6 +521,38 @@ def test_prompt_layouts(pk):
     assert pk.pk_prompt_attention(cfg, q[:0], k[:0], v[:0], ints([0, 0, 0]), 0.1).shape == (0, hq, d)
 
 
+def test_prompts_of_one_key_and_of_tokens_far_apart(pk):
+    """Strides of 0 and of more than 2^24 elements, with offsets beyond 2^32 bytes."""
+    n, d, stride = 140, 64, (1 << 24) + 8
+    cfg = pk.PromptConfig(n_seq=2, n_kv_heads=1, n_q_heads=2, head_dim=d)
+    q, k, v = (torch.randn(n, h, d, device="cuda").half() for h in (2, 1, 1))
+    starts = ints([0, 71, n])
+    one = k[:1].expand(n, 1, d)
+    assert torch.equal(pk.pk_prompt_attention(cfg, q, one, v, starts, 0.1), pk.pk_prompt_attention(cfg, q, one.contiguous(), v, starts, 0.1))
+    assert torch.equal(pk.pk_prompt_attention(cfg, q, k, one, starts, 0.1), pk.pk_prompt_attention(cfg, q, k, one.contiguous(), starts, 0.1))
+    want = pk.pk_prompt_attention(cfg, q, k, v, starts, 0.1)
+    far = torch.empty((n - 1) * stride + 4 * d, dtype=torch.float16, device="cuda")
+    fk, fv = (far.as_strided((n, 1, d), (stride, d, 1), at) for at in (0, 64))
+    fk.copy_(k)
+    fv.copy_(v)
+    assert torch.equal(pk.pk_prompt_attention(cfg, q, fk, fv, starts, 0.1), want)
+    fq, fo = (far.as_strided((n, 2, d), (stride, d, 1), at) for at in (0, 128))   # (the keys' place is free now)
+    fq.copy_(q)
+    pk.pk_prompt_attention(cfg, fq, k, v, starts, 0.1, out=fo)
+    assert torch.equal(fo, want)
+
+
+def test_many_starts_that_fall(pk):
+    """More than 64 sequences, every other one of all rows: the launch has workgroups for a few of them; a row is as it was or right."""
+    n, d, n_seq = 200, 64, 100
+    cfg = pk.PromptConfig(n_seq=n_seq, n_kv_heads=1, n_q_heads=2, head_dim=d)
+    q, k, v = (torch.randn(n, h, d, device="cuda").half() for h in (2, 1, 1))
+    out = torch.full((n, 2, d), 7.0, dtype=torch.float16, device="cuda")
+    pk.pk_prompt_attention(cfg, q, k, v, ints([n * (i % 2) for i in range(n_seq + 1)]), 0.2, out=out)
+    want = pk.pk_prompt_attention(pk.PromptConfig(n_seq=1, n_kv_heads=1, n_q_heads=2, head_dim=d), q, k, v, ints([0, n]), 0.2)
+    assert ((out == want).all(-1) | (out == 7.0).all(-1)).all()
+
+
 # ---- together ----------------------------------------------------------------------------------------------------------------
 
 class Loop:
