@@ -786,12 +786,13 @@ __global__ __launch_bounds__(64 * NW, 2) void fp8_attention_kernel(Fp8AttentionA
 
 // The pieces of a row together: sum_s l_s 2^(m_s - m) o_s / sum_s l_s 2^(m_s - m).  A wave takes a row of a (sequence, KV head) that was
 // cut: the factors of 64 pieces in its lanes, then the pieces' results one after the other, a lane D / 64 channels (two of 48 lanes at
-// 96), with several loads in flight.  (A thread that read every piece's factors itself took 20 us for the 64 pieces of one sequence of 32k.)
+// 96), with TOGETHER loads in flight: four over the 8-bit cache (eight: drafts 55.4 -> 55.9 us), eight over the 16-bit one (four: one sequence of 32k tokens of 8 heads
+// 30.3 us, eight 29.4, sixteen 28.8, but 64 of 2000 tokens 53.2, 53.4 and 53.9).  (A thread that read every piece's factors itself took 20 us for the 64 pieces of one sequence of 32k.)
 constexpr int kMergeRows = 4;
-template <int D>
+template <int D, int TOGETHER = 4>
 __global__ __launch_bounds__(64 * kMergeRows) void fp8_merge_kernel(Fp8AttentionArgs a)
 {
-    constexpr int kPer = D <= 128 ? 2 : 4, kTogether = 4;   // channels per lane, pieces whose loads are on their way together
+    constexpr int kPer = D <= 128 ? 2 : 4, kTogether = TOGETHER;   // channels per lane, pieces whose loads are on their way together
     const int rows = a.in.r * a.in.n_query, hkv = a.in.c.n_kv_heads, groups = (rows + kMergeRows - 1) / kMergeRows;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int kvh = blockIdx.x % hkv, rest = blockIdx.x / hkv, row = rest % groups * kMergeRows + wave, seq = rest / groups;
@@ -1073,11 +1074,11 @@ void launch_rt(const Fp8AttentionArgs &a, uint32_t grid, bool opt, hipStream_t s
     else fp8_attention_kernel<D, RT, NW, BY_ROWS, false><<<grid, 64 * NW, 0, s>>>(a);
 }
 
-template <int D>
+template <int D, int TOGETHER = 4>
 hipError_t launch_merge_d(const Fp8AttentionArgs &a, hipStream_t s)
 {
     const int64_t rows = (int64_t)a.in.r * a.in.n_query;
-    fp8_merge_kernel<D><<<(uint32_t)((int64_t)a.in.n_seq * a.in.c.n_kv_heads * ((rows + kMergeRows - 1) / kMergeRows)), 64 * kMergeRows, 0, s>>>(a);
+    fp8_merge_kernel<D, TOGETHER><<<(uint32_t)((int64_t)a.in.n_seq * a.in.c.n_kv_heads * ((rows + kMergeRows - 1) / kMergeRows)), 64 * kMergeRows, 0, s>>>(a);
     return hipGetLastError();
 }
 
@@ -1140,10 +1141,10 @@ hipError_t launch_fp8_attention(Fp8AttentionArgs &a, hipStream_t s)
 
 hipError_t launch_attention_merge(const Fp8AttentionArgs &a, hipStream_t s)
 {
-    return a.in.d == 64    ? launch_merge_d<64>(a, s)
-           : a.in.d == 96  ? launch_merge_d<96>(a, s)
-           : a.in.d == 128 ? launch_merge_d<128>(a, s)
-                           : launch_merge_d<256>(a, s);
+    return a.in.d == 64    ? launch_merge_d<64, 8>(a, s)
+           : a.in.d == 96  ? launch_merge_d<96, 8>(a, s)
+           : a.in.d == 128 ? launch_merge_d<128, 8>(a, s)
+                           : launch_merge_d<256, 8>(a, s);
 }
 
 hipError_t launch_fp8_weights(Fp8WeightsArgs &a, hipStream_t s)
