@@ -65,7 +65,7 @@ __device__ __forceinline__ short8v numerators(const float (&p)[8])
 }
 
 template <int D, int RT, int NW, bool BF16, bool OPT>
-__global__ __launch_bounds__(64 * NW, 2) void kv16_attention_kernel(Fp8AttentionArgs a)
+__global__ __launch_bounds__(64 * NW, D == 256 && RT == 2 ? 1 : 2) void kv16_attention_kernel(Fp8AttentionArgs a)
 {
     using S = Part<D>;
     const int lane = threadIdx.x & 63, n = lane & 15, g = lane >> 4;
@@ -306,8 +306,10 @@ __global__ __launch_bounds__(64 * NW, 2) void kv16_attention_kernel(Fp8Attention
     }
 }
 
-// 16 query heads per tile; up to 128 channels two tiles share what is read, 256 channels leave registers for one
-int tiles_of(int64_t r, int d) { return d == 256 || r <= 16 ? 1 : 2; }
+// 16 query heads per tile, two tiles share what is read.  With 256 channels they take a SIMD's registers for one wave, which pays over many tokens (16 sequences of
+// 16k tokens, two KV heads of 32 heads each, 131 -> 114 us; of 10k tokens and 33 heads 152 -> 102; 32 of up to 20k, 20 heads, 113 -> 90; 256k tokens of all KV heads
+// 61.5 and 59.7, one sequence of 128k and two KV heads 64.4 and 66.1; but 160k with a window 39.9 -> 44.7, 4000 tokens 18 -> 24).
+int tiles_of(int64_t r, int d, int64_t tokens) { return r <= 16 || (d == 256 && tokens <= 1 << 18) ? 1 : 2; }
 
 template <int D, int RT, bool BF16>
 void launch_rt(const Fp8AttentionArgs &a, uint32_t grid, bool opt, hipStream_t s)
@@ -319,14 +321,14 @@ void launch_rt(const Fp8AttentionArgs &a, uint32_t grid, bool opt, hipStream_t s
 template <int D>
 hipError_t launch_d(Fp8AttentionArgs &a, hipStream_t s)
 {
-    const int tiles = tiles_of(a.in.r, D);
+    const int tiles = tiles_of(a.in.r, D, (int64_t)a.in.n_seq * a.in.c.n_kv_heads * a.bound);
     a.groups = (a.in.r + 16 * tiles - 1) / (16 * tiles);
     const uint32_t units = (uint32_t)((a.parts > 0 ? a.parts : a.in.n_seq) * a.in.c.n_kv_heads), grid = (units + 7) / 8 * 8 * a.groups;
     const bool opt = a.in.cap > 0.f || a.in.slopes;
     if (tiles == 1) {
         if (a.in.bf16) launch_rt<D, 1, true>(a, grid, opt, s);
         else launch_rt<D, 1, false>(a, grid, opt, s);
-    } else if constexpr (D < 256) {
+    } else {
         if (a.in.bf16) launch_rt<D, 2, true>(a, grid, opt, s);
         else launch_rt<D, 2, false>(a, grid, opt, s);
     }
@@ -341,7 +343,7 @@ hipError_t launch_d(Fp8AttentionArgs &a, hipStream_t s)
 // per CU: 364 and 362, 122 and 126.  (Short caches whole by eight waves, with nothing to merge: 22.5 us for 2k tokens of 8 heads where runs of 256 take 14.7.)
 int64_t kv16_attention_parts(int64_t n_seq, int64_t n_kv_heads, int64_t r, int d, int64_t bound)
 {
-    const int64_t rows = 16 * tiles_of(r, d), across = n_kv_heads * ((r + rows - 1) / rows);   // workgroups per run
+    const int64_t rows = 16 * tiles_of(r, d, n_seq * n_kv_heads * bound), across = n_kv_heads * ((r + rows - 1) / rows);   // workgroups per run
     int64_t parts = (256 / across >= n_seq ? 256 : 512) / across;
     if (parts < 1) parts = 1;
     if (n_seq > kMostSeqs || n_seq >= 4 * parts) return 0;

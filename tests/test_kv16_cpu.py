@@ -28,6 +28,14 @@ def pk():
 BASE = dict(n_seq=2, n_kv_heads=2, n_q_heads=8, head_dim=128, t_capacity=1024, page_tokens=16, n_pages=200)
 
 
+@pytest.mark.parametrize("change", [dict(), dict(n_kv_heads=1, n_q_heads=24, head_dim=256), dict(n_seq=5, n_q_heads=128, head_dim=256), dict(n_seq=250, n_q_heads=40), dict(n_seq=300)])
+def test_workspaces_grow_with_the_bound(pk, change):
+    cfg = pk.Kv16Config(**{**BASE, "t_capacity": 1 << 20, **change})
+    bounds = sorted({b for i in range(4, 21) for b in ((1 << i) - 1, 1 << i, (1 << i) + 1, 3 << (i - 1), 5 << (i - 2)) if b <= 1 << 20})
+    needs = [pk.pk_kv16_workspace_bytes(cfg, b) for b in bounds]
+    assert needs == sorted(needs) and (needs[-1] > 0 or cfg.n_seq == 300)
+
+
 def test_sizes(pk):
     cfg = pk.Kv16Config(**BASE)
     assert pk.pk_kv16_cache_bytes(cfg) == 200 * 2 * 16 * 128 * 2

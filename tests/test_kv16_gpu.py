@@ -296,6 +296,17 @@ def test_attention_over_long_caches(pk, dtype, d, lens):
     assert np.abs(a - b).max() <= 4 * EPS[dtype] * np.abs(a).max() and np.abs(al - bl).max() <= 1e-4
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("hkv,r", [(1, 17), (2, 24), (1, 33), (2, 64)])
+def test_attention_of_many_heads_of_256_channels(pk, dtype, hkv, r):
+    """More than 16 heads per KV head with a large bound, which takes them in pairs of row tiles, and a small one."""
+    s = Step(pk, [0, 1, 33, 300, 2100], seed=r, hkv=hkv, r=r, d=256, page=64, dtype=dtype, cap=1 << 17)
+    s.attend()
+    s.attend(slopes=True, cap=20.0, window=290)
+    s.attend(scale=-0.05, bound=1 << 16)
+    s.attend(bound=2100)
+
+
 def test_attention_of_many_sequences(pk):
     """More sequences than the keys are dealt out over, and one for each; unequal lengths."""
     rng = random.Random(2)
