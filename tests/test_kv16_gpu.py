@@ -564,6 +564,24 @@ def test_many_starts_that_fall(pk):
     assert ((out == want).all(-1) | (out == 7.0).all(-1)).all()
 
 
+def test_as_many_sequences_as_there_may_be(pk):
+    rng = random.Random(5)
+    run_prompts(pk, [rng.choice([0, 1, 2, 3, 40]) for _ in range(4096)], hkv=1, r=2, d=64)
+    p = Paged(pk, 65535, 1, 70000, 2, seed=1)
+    for counts in ([rng.choice([0, 1, 1, 2]) for _ in range(65535)], [rng.choice([-1, 0, 1]) for _ in range(65535)]):
+        plan, want = p.update(counts, 65000)
+        p.check(plan, want)
+    # a token or none each: the result is its value
+    n = 65535
+    cfg = pk.Kv16Config(n_seq=n, n_kv_heads=1, n_q_heads=1, head_dim=64, t_capacity=16, page_tokens=16, n_pages=n)
+    order = torch.randperm(n, device="cuda").to(torch.int32)
+    cache = pk.Kv16Cache(cfg, page_table=order[:, None])
+    cache.k.fill_(0.5), cache.v.copy_(torch.randn(cache.v.shape, device="cuda"))
+    cache.states[:, 0] = torch.randint(0, 2, (n,), device="cuda")
+    out = pk.pk_kv16_attention(cfg, cache, torch.randn(n, 1, 64, device="cuda").half(), 0.1)
+    assert torch.equal(out[:, 0], cache.v[order.long(), 0, 0] * cache.states[:, :1])
+
+
 # ---- together ----------------------------------------------------------------------------------------------------------------
 
 class Loop:
