@@ -786,8 +786,8 @@ __global__ __launch_bounds__(64 * NW, 2) void fp8_attention_kernel(Fp8AttentionA
 
 // The pieces of a row together: sum_s l_s 2^(m_s - m) o_s / sum_s l_s 2^(m_s - m).  A wave takes a row of a (sequence, KV head) that was
 // cut: the factors of 64 pieces in its lanes, then the pieces' results one after the other, a lane D / 64 channels (two of 48 lanes at
-// 96), with TOGETHER loads in flight: four over the 8-bit cache (eight: drafts 55.4 -> 55.9 us), eight over the 16-bit one (four: one sequence of 32k tokens of 8 heads
-// 30.3 us, eight 29.4, sixteen 28.8, but 64 of 2000 tokens 53.2, 53.4 and 53.9).  (A thread that read every piece's factors itself took 20 us for the 64 pieces of one sequence of 32k.)
+// 96), with TOGETHER loads in flight: eight over the 16-bit cache where there are many pieces (of eight sequences, 16 each, 256 channels, 5.6 us, four 6.7; of one of
+// 32k tokens the call 29.4 and 30.7; but of 64 sequences, two or so each, 6.7 and 6.0; over the 8-bit cache 55.9 and 55.4 for the call of drafts).  (A thread that read every piece's factors itself took 20 us for the 64 pieces of one sequence of 32k.)
 constexpr int kMergeRows = 4;
 template <int D, int TOGETHER = 4>
 __global__ __launch_bounds__(64 * kMergeRows) void fp8_merge_kernel(Fp8AttentionArgs a)
@@ -1141,10 +1141,12 @@ hipError_t launch_fp8_attention(Fp8AttentionArgs &a, hipStream_t s)
 
 hipError_t launch_attention_merge(const Fp8AttentionArgs &a, hipStream_t s)
 {
-    return a.in.d == 64    ? launch_merge_d<64, 8>(a, s)
-           : a.in.d == 96  ? launch_merge_d<96, 8>(a, s)
-           : a.in.d == 128 ? launch_merge_d<128, 8>(a, s)
-                           : launch_merge_d<256, 8>(a, s);
+    // eight loads in flight where a sequence has eight pieces or more (see fp8_merge_kernel)
+    const bool many = a.parts >= 8 * a.in.n_seq;
+    if (a.in.d == 64) return many ? launch_merge_d<64, 8>(a, s) : launch_merge_d<64>(a, s);
+    if (a.in.d == 96) return many ? launch_merge_d<96, 8>(a, s) : launch_merge_d<96>(a, s);
+    if (a.in.d == 128) return many ? launch_merge_d<128, 8>(a, s) : launch_merge_d<128>(a, s);
+    return many ? launch_merge_d<256, 8>(a, s) : launch_merge_d<256>(a, s);
 }
 
 hipError_t launch_fp8_weights(Fp8WeightsArgs &a, hipStream_t s)
