@@ -70,13 +70,30 @@ __device__ __forceinline__ float16v mfma32(short8v a, short8v b, float16v c)   /
 // Softmax numerators are 2^(score - reference).  The reference for a largest score `top` serves scores up to kRoom above it, so that it moves a few times in a
 // row, not with every larger score.  fp16's smallest step is 2^-24, so that its numerators go up to 2^11, 2^15 with the room (a token counts down to 2^-36 of the
 // largest one); scores of 2^20 and more, whose own steps are large, are the reference themselves.  bf16 has the exponents of binary32: numerators
-// of up to 2^-25 with the room, so that values up to the type's largest times 2^25 tokens stay finite.
-constexpr float kRoom = 4.f;
+// of up to 2^-25 with the room, so that values up to the type's largest times 2^25 tokens stay finite; from 2^29 on, where half a step is more than that and the
+// reference comes out as the score itself, numerators are taken kUnder below it (under_of).
+constexpr float kRoom = 4.f, kUnder = 25.f + kRoom;
 template <bool BF16>
 __device__ __forceinline__ float reference_of(float top)
 {
-    if constexpr (BF16) return top + (25.f + kRoom);
+    if constexpr (BF16) return top + kUnder;
     else return fabsf(top) < 0x1p20f ? top - 11.f : top;
+}
+// How far below the reference a row's numerators are taken, as a power of two.  most: the largest score that the reference serves, which from 2^20 on is the largest
+// score itself; -inf where nothing has been seen.
+template <bool BF16>
+__device__ __forceinline__ float under_of(float most)
+{
+    return BF16 && most + kUnder == most ? kUnder : 0.f;
+}
+// 2^(m - to), what numerators of the reference m are in those of `to`.  A row that comes to another side of 2^29 is seen to in a branch for the whole wave, which
+// only large references take (a prompt of 32k tokens 7.36 -> 7.41 ms; in line 7.40 -> 7.50).  Where `to` is less than 2^28 and m was 2^29 or more, the factor is 0 anyhow.
+template <bool BF16>
+__device__ __forceinline__ float change_of(float m, float to, float was, float most)
+{
+    float by = __builtin_amdgcn_exp2f(m - to);
+    if (BF16 && __any(fabsf(to) >= 0x1p28f)) by = __builtin_amdgcn_exp2f((m - to) + (under_of<BF16>(was) - under_of<BF16>(most)));
+    return by;
 }
 // From here on scores are rounded before the reference is taken off, as their largest is: the multiply-add would take the factor in unrounded, and the numerator
 // of a row's only token would be no power of two, which the 16-bit type holds exactly.

@@ -185,9 +185,10 @@ __global__ __launch_bounds__(64 * NW, D == 256 && RT == 2 ? 1 : 2) void kv16_att
                 top = fold_rows(one, MaxF());
                 by[rt] = 1.f;
                 if (top > most[rt]) {
+                    const float was = most[rt];
                     most[rt] = fabsf(top) < 0x1p20f ? top + kRoom : top;
                     const float to = reference_of<BF16>(top);
-                    by[rt] = exp2_(m[rt] - to);
+                    by[rt] = change_of<BF16>(m[rt], to, was, most[rt]);
                     m[rt] = to;
                     l[rt] *= by[rt];
                 }
@@ -196,11 +197,12 @@ __global__ __launch_bounds__(64 * NW, D == 256 && RT == 2 ? 1 : 2) void kv16_att
                 float e[8], sum = 0.f;
                 if (__any(fabsf(ref) >= kLarge)) {
                     // (see kLarge)
+                    const float under = under_of<BF16>(most[rt]);
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
                         x[i] *= f;
                         asm volatile("" : "+v"(x[i]));   // (not contracted)
-                        e[i] = exp2_(x[i] - ref);
+                        e[i] = exp2_((x[i] - ref) - under);
                     }
                 } else {
 #pragma unroll
@@ -251,6 +253,7 @@ __global__ __launch_bounds__(64 * NW, D == 256 && RT == 2 ? 1 : 2) void kv16_att
             for (int ct = 0; ct < S::kTiles; ++ct)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) o[rt][ct][i] = mean_of<BF16>(o[rt][ct][i] * inv);
+            l[rt] *= exp2_(under_of<BF16>(most[rt]));   // in units of 2^m, for the other waves and pieces
         }
         constexpr int kAtOnce = (D == 256 ? 8 : 16) * 4 / NW, kPad = 4;   // rows at a time: 32 to 34 KB of LDS
         __shared__ float sm_o[NW][kAtOnce][D + kPad];

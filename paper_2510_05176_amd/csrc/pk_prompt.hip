@@ -351,9 +351,10 @@ __global__ __launch_bounds__((PromptShape<D, GROUPS>::kThreads), D == 256 ? 1 : 
         top = op_rows(swap32(bits_of(top), bits_of(top)), MaxF()) * f;
         float by = 1.f;
         if (top > most) {
+            const float was = most;
             most = fabsf(top) < 0x1p20f ? top + kRoom : top;
             const float to = reference_of<BF16>(top);
-            by = exp2_(m - to);
+            by = change_of<BF16>(m, to, was, most);
             m = to;
             l *= by;
         }
@@ -365,11 +366,12 @@ __global__ __launch_bounds__((PromptShape<D, GROUPS>::kThreads), D == 256 ? 1 : 
         float sum[2] = {0.f, 0.f};
         if (__any(fabsf(ref) >= kLarge)) {
             // (see kLarge)
+            const float under = under_of<BF16>(most);
 #pragma unroll
             for (int e = 0; e < 32; ++e) {
                 float y = s[e >> 4][e & 15] * f;
                 asm volatile("" : "+v"(y));   // (not contracted)
-                s[e >> 4][e & 15] = y - ref;
+                s[e >> 4][e & 15] = (y - ref) - under;
             }
         } else {
 #pragma unroll
@@ -491,6 +493,7 @@ __global__ __launch_bounds__((PromptShape<D, GROUPS>::kThreads), D == 256 ? 1 : 
             *reinterpret_cast<uint2 *>(to + 2 * (32 * ct + 8 * i)) = make_uint2(narrow(o[ct][4 * i], o[ct][4 * i + 1], BF16), narrow(o[ct][4 * i + 2], o[ct][4 * i + 3], BF16));
     if (a.lse && h == 0) {
         // l's power of two joins the reference first: their sum is small where the log-sum-exp is, and takes no rounding of l's whole logarithm
+        l *= exp2_(under_of<BF16>(most));
         int e;
         const float part = frexpf(l, &e);
         a.lse[(int64_t)head * a.n_tokens + start + tok] = l == 0.f ? -INFINITY : (m + (float)e + log2f(part)) * kLn2;

@@ -750,3 +750,59 @@ def test_calls_check_the_device(pk):
     cfg = pk.PromptConfig(n_seq=1, n_kv_heads=8, n_q_heads=8)
     with pytest.raises(ValueError):
         pk.pk_prompt_attention(cfg, q, q, q, torch.zeros(2, dtype=torch.int32), 0.1)
+
+
+# ---- large scores by their values ----------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("scale", [2.0 ** 14, 2.0 ** 21, 2.0 ** 22, 2.0 ** 23, 2.0 ** 40, -2.0 ** 14, -2.0 ** 22, -2.0 ** 40])
+def test_the_largest_values_under_large_scores(pk, dtype, scale):
+    """Equal scores of every size over values of the type's largest: their mean is that value, and the sums that lead to it stay finite."""
+    d, lens, big = 128, [1, 2, 70, 700, 5000], torch.finfo(dtype).max
+    ones = lambda i, n: (torch.ones(n, 1, d, dtype=dtype, device="cuda"), None)   # noqa: E731
+    most = lambda i, n: (torch.full((n, 1, d), big, dtype=dtype, device="cuda"), None)   # noqa: E731
+    got, lse = Step(pk, lens, hkv=1, r=4, d=d, dtype=dtype, k=ones, v=most).attend(scale=scale, q=(torch.ones(len(lens), 4, d, device="cuda").to(dtype), None), checked=False)
+    # weights off by E each and a sum rounded n times: no further than 2 E from 1 in all, and the type's largest is not passed
+    assert (got >= big * (1 - 2 * EPS[dtype])).all() and (got <= big).all()
+    want = d * scale + np.log(lens)[:, None]
+    assert (np.abs(lse - want) <= 6 * 2.0 ** -24 * np.abs(want) + 2.0 ** -20).all()
+    for r, n in ((2, 300), (64, 2100)):
+        cfg = pk.PromptConfig(n_seq=1, n_kv_heads=1, n_q_heads=r, head_dim=d, dtype=code(pk, dtype))
+        x = [torch.full((n, h, d), y, device="cuda", dtype=dtype) for h, y in ((r, 1.0), (1, 1.0), (1, big))]
+        lse = torch.zeros(r, n, device="cuda")
+        got = pk.pk_prompt_attention(cfg, *x, ints([0, n]), scale, lse=lse).double()
+        assert (got >= big * (1 - 2 * EPS[dtype])).all() and (got <= big).all()
+        want = d * scale + np.log(1 + np.arange(n))[None]
+        assert (np.abs(lse.double().cpu().numpy() - want) <= 6 * 2.0 ** -24 * np.abs(want) + 2.0 ** -20).all()
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("sign", [1, -1])
+@pytest.mark.parametrize("n", [300, 3000])
+def test_scores_on_both_sides_of_a_large_one(pk, dtype, sign, n):
+    """Scores, in units of the exponent, of 2^29 and of its neighbour 32 below in binary32 (or their negatives): the smaller one's tokens come first and have 2^-32 of the weight each."""
+    d = 64
+    scale = np.float32(22.1808)   # 2^5 / log2 e and a little
+    x = 2.0 ** 24 - np.arange(0, 130)
+    y = (x.astype(np.float32) * np.float32(scale * np.float32(math.log2(math.e)))).astype(np.float64)
+    above, below = x[y >= 2.0 ** 29].min(), x[y < 2.0 ** 29].max()
+    less, more = (below, above) if sign > 0 else (above, below)
+    kn, vn = np.zeros((n, 1, d)), np.full((n, 1, d), 100.0)
+    kn[:, 0, 0], kn[:, 0, 1] = 4096.0, less - 2.0 ** 24
+    kn[n - 3, 0, 1] = more - 2.0 ** 24
+    vn[n - 3] = 1.0
+    kn[n - 2:], vn[n - 2:] = (0.0 if sign > 0 else 2 * 4096.0), 50.0
+    if sign < 0:
+        kn[n - 2:, 0, 1:] = 0.0
+    q = np.zeros((1, 2, d))
+    q[..., 0], q[..., 1] = 4096.0, 1.0
+    on = lambda t: torch.from_numpy(t).to(dtype).cuda()   # noqa: E731
+    for t in (kn, vn, q):
+        assert (on(t).double().cpu().numpy() == t).all()
+    # numerators of 2^-29 and less beside sums of 100 * 3000 * 2^-32 of the winner's 1: half a step of the result covers them
+    got, lse = Step(pk, [n], hkv=1, r=2, d=d, dtype=dtype, k=lambda i, n: (on(kn), kn), v=lambda i, n: (on(vn), vn)).attend(
+        scale=sign * float(scale), q=(on(q), q), checked=False)
+    assert (np.abs(got - 1.0) <= EPS[dtype]).all()
+    cfg = pk.PromptConfig(n_seq=1, n_kv_heads=1, n_q_heads=2, head_dim=d, dtype=code(pk, dtype))
+    got = pk.pk_prompt_attention(cfg, on(np.repeat(q, n, 0)), on(kn), on(vn), ints([0, n]), sign * float(scale)).double()
+    assert ((got[n - 3:] - 1.0).abs() <= EPS[dtype]).all() and (got[:n - 3] == 100.0).all()
