@@ -754,6 +754,80 @@ def test_calls_check_the_device(pk):
 
 # ---- large scores by their values ----------------------------------------------------------------------------------------------
 
+def chosen_scores(n, d, dtype, seed):
+    """Keys whose element h % 4 is a head's whole score (its query is 1 there, 0 elsewhere), whole numbers that both types hold: the largest one once; at four tokens; at every token; at the
+    last one, behind a row that grows.  Values are multiples of 4, so that means of 1, 2 or 4 of them are held too."""
+    rng = np.random.default_rng(seed)
+    k, v = rng.integers(-40, 41, (n, 1, d)).astype(np.float64), 4.0 * rng.integers(-16, 17, (n, 1, d))
+    k[rng.integers(n), 0, 0] = 41
+    k[rng.choice(n, min(n, 4), replace=False), 0, 1] = 41
+    k[:, 0, 2] = 7
+    k[:, 0, 3] = np.arange(n) * 250 // n - 100
+    k[n - 1, 0, 3] = 200
+    return k, v
+
+
+def one_hot(n, heads, d):
+    q = np.zeros((n, heads, d))
+    for h in range(heads):
+        q[:, h, h % 4] = 1.0
+    return q
+
+
+def check_chosen(got, got_lse, x, v, scale, dtype):
+    """got [rows][d] for scores x [rows][keys] (-inf: not seen), whole numbers times a scale that leaves e^0 and nothing else.  A single largest score above 0, or two or four equal ones, give the
+    mean exactly: numerators are powers of two.  Below 0 the reference may be rounded, which moves every numerator alike, by its rounding to the 16-bit type.  The log-sum-exp: six roundings (log2 e, its
+    product, the score, the reference, ln 2, the last product) and 2^-20 for the logarithm."""
+    E = EPS[dtype]
+    s = np.where(x == -math.inf, -math.inf, x * scale)   # (0 times -inf, and a scale below 0)
+    top = s.max(1, keepdims=True)
+    tied = s == top
+    n = tied.sum(1, keepdims=True)
+    want, mag = tied @ v / n, tied @ np.abs(v) / n
+    exact = np.isin(n, (1, 2, 4)) & (top > 0)
+    tol = np.where(exact, np.where(want == 0, 2.0 ** -20 * mag, 0.0), E * np.abs(want) + (E + n * 2.0 ** -24) * mag)
+    assert (np.abs(got - want) <= tol).all(), np.argwhere(~(np.abs(got - want) <= tol))[:4]
+    want_lse = (top + np.log(n))[:, 0]
+    assert (np.abs(got_lse - want_lse) <= 6 * 2.0 ** -24 * np.abs(want_lse) + 2.0 ** -20).all()
+
+
+LARGE = [2.0 ** 14, -2.0 ** 14, 2.0 ** 22, 2.0 ** 29, -2.0 ** 29, 2.0 ** 40, 2.0 ** 100]
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("scale", LARGE)
+@pytest.mark.parametrize("d,lens", [(128, [1, 2, 33, 500, 5000]), (256, [3, 700]), (64, [64] * 300)])
+def test_attention_of_large_scores_by_value(pk, dtype, scale, d, lens):
+    """The values of the largest score's tokens and no others, wherever they lie among tiles, waves and pieces."""
+    made = [chosen_scores(n, d, dtype, i) for i, n in enumerate(lens)]
+    on = lambda x: (torch.from_numpy(x).to(dtype).cuda(), x)   # noqa: E731
+    s = Step(pk, lens, hkv=1, r=4, d=d, dtype=dtype, k=lambda i, n: on(made[i][0]), v=lambda i, n: on(made[i][1]))
+    got, lse = s.attend(scale=scale, q=on(one_hot(len(lens), 4, d)), checked=False)
+    for i in range(len(lens)):
+        k, v = made[i]
+        check_chosen(got[i], lse[i], k[:, 0, :4].T, v[:, 0], scale, dtype)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("scale", LARGE)
+@pytest.mark.parametrize("d,r,lens", [(128, 4, [1, 70, 300]), (256, 4, [150, 33]), (64, 8, [200]), (128, 64, [640, 500, 300, 640])])
+def test_prompts_of_large_scores_by_value(pk, dtype, scale, d, r, lens):
+    made = [chosen_scores(n, d, dtype, i) for i, n in enumerate(lens)]
+    k, v = (torch.from_numpy(np.concatenate([m[i] for m in made])).to(dtype).cuda() for i in range(2))
+    n, starts = sum(lens), np.concatenate([[0], np.cumsum(lens)])
+    q = torch.from_numpy(one_hot(n, r, d)).to(dtype).cuda()
+    lse = torch.zeros(r, n, device="cuda")
+    cfg = pk.PromptConfig(n_seq=len(lens), n_kv_heads=1, n_q_heads=r, head_dim=d, dtype=code(pk, dtype))
+    got = pk.pk_prompt_attention(cfg, q, k, v, ints(starts.tolist()), scale, lse=lse).double().cpu().numpy()
+    lse = lse.double().cpu().numpy()
+    for i, (kn, vn) in enumerate(made):
+        at = slice(starts[i], starts[i + 1])
+        behind = np.triu(np.ones((lens[i], lens[i]), bool), 1)
+        for h in range(r):
+            x = np.where(behind, -math.inf, kn[None, :, 0, h % 4])
+            check_chosen(got[at, h], lse[h, at], x, vn[:, 0], scale, dtype)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("scale", [2.0 ** 14, 2.0 ** 21, 2.0 ** 22, 2.0 ** 23, 2.0 ** 40, -2.0 ** 14, -2.0 ** 22, -2.0 ** 40])
 def test_the_largest_values_under_large_scores(pk, dtype, scale):
