@@ -34,6 +34,8 @@ struct Kv16AppendArgs {
 hipError_t launch_kv16_append(const Kv16AppendArgs &a, hipStream_t s);
 
 // The 8-bit cache's arguments with 16-bit vectors in the places of the codes; n_query is 1.
+// With 256 channels and more than 16 heads per KV head calls of more tokens (sequences * KV heads * bound) than this take two row tiles per wave.
+constexpr int64_t kOneTileTokens = 1 << 18;
 int64_t kv16_attention_parts(int64_t n_seq, int64_t n_kv_heads, int64_t r, int d, int64_t bound);
 hipError_t launch_kv16_attention(Fp8AttentionArgs &a, hipStream_t s);
 

@@ -1,5 +1,6 @@
 // Host side of the paged 16-bit cache, its pages and the attention of prompts (pk_pages_*, pk_kv16_*, pk_prompt_attention of
 // include/patternkv.h): checks, sizes, launches.
+#include <algorithm>
 #include <cfloat>
 #include <cmath>
 #include <cstring>
@@ -167,8 +168,10 @@ uint64_t pk_kv16_cache_bytes(const pk_kv16_config *cfg)
 size_t pk_kv16_workspace_bytes(const pk_kv16_config *cfg, int64_t bound)
 {
     if (check_kv16(cfg) != PK_OK || bound < 0 || bound > cfg->t_capacity) return 0;
-    const AttentionPlan p = plan_attention(cfg, bound);
-    return p.o_bytes + p.ml_bytes;
+    // Each form of the kernel needs more for a larger bound, but the one of small bounds, with fewer rows to a workgroup, may have more runs than the other.
+    const int64_t turn = kOneTileTokens / ((int64_t)cfg->n_seq * cfg->n_kv_heads);
+    const AttentionPlan p = plan_attention(cfg, bound), small = plan_attention(cfg, std::min(bound, turn));
+    return std::max(p.o_bytes + p.ml_bytes, small.o_bytes + small.ml_bytes);
 }
 
 pk_status pk_kv16_append(const pk_kv16_config *cfg, const pk_kv16_cache *cache, const void *k_new, const void *v_new, const pk_strides *ks,

@@ -312,7 +312,7 @@ __global__ __launch_bounds__(64 * NW, D == 256 && RT == 2 ? 1 : 2) void kv16_att
 // 16 query heads per tile, two tiles share what is read.  With 256 channels they take a SIMD's registers for one wave, which pays over many tokens (16 sequences of
 // 16k tokens, two KV heads of 32 heads each, 131 -> 114 us; of 10k tokens and 33 heads 152 -> 102; 32 of up to 20k, 20 heads, 113 -> 90; 256k tokens of all KV heads
 // 61.5 and 59.7, one sequence of 128k and two KV heads 64.4 and 66.1; but 160k with a window 39.9 -> 44.7, 4000 tokens 18 -> 24).
-int tiles_of(int64_t r, int d, int64_t tokens) { return r <= 16 || (d == 256 && tokens <= 1 << 18) ? 1 : 2; }
+int tiles_of(int64_t r, int d, int64_t tokens) { return r <= 16 || (d == 256 && tokens <= kOneTileTokens) ? 1 : 2; }
 
 template <int D, int RT, bool BF16>
 void launch_rt(const Fp8AttentionArgs &a, uint32_t grid, bool opt, hipStream_t s)

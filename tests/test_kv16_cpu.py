@@ -36,6 +36,18 @@ def test_workspaces_grow_with_the_bound(pk, change):
     assert needs == sorted(needs) and (needs[-1] > 0 or cfg.n_seq == 300)
 
 
+def test_workspaces_for_a_larger_bound_serve_every_smaller_one(pk):
+    """Whichever form the kernel takes (256 channels with more than 16 heads per KV head have two, by sequences * KV heads * bound), and wherever the keys stop being dealt out."""
+    for hkv in (1, 2, 3, 4, 8):
+        for r in (1, 16, 17, 20, 33, 40, 48, 49, 64):
+            for n_seq in (1, 2, 26, 31, 32, 46, 61, 64, 85, 86, 100, 127, 128, 170, 171, 255, 256, 257):
+                cfg = pk.Kv16Config(**{**BASE, "t_capacity": 1 << 20, "n_seq": n_seq, "n_kv_heads": hkv, "n_q_heads": hkv * r, "head_dim": 256})
+                turn = (1 << 18) // (n_seq * hkv)
+                bounds = sorted({b for b in (0, 1, 256, 257, 1000, turn - 1, turn, turn + 1, turn + 100, 2 * turn, 1 << 20) if 0 <= b <= 1 << 20})
+                needs = [pk.pk_kv16_workspace_bytes(cfg, b) for b in bounds]
+                assert needs == sorted(needs), (hkv, r, n_seq, bounds, needs)
+
+
 def test_sizes(pk):
     cfg = pk.Kv16Config(**BASE)
     assert pk.pk_kv16_cache_bytes(cfg) == 200 * 2 * 16 * 128 * 2

@@ -385,6 +385,14 @@ def test_attention_layouts(pk):
         s.pk.pk_kv16_attention(cfg, s.cache, q.transpose(0, 1), 0.1, bound=1500, workspace=ws[:100])
 
 
+def test_a_workspace_for_the_capacity_serves_smaller_bounds(pk):
+    """Also where calls with a smaller bound take another form of the kernel, whose runs are more."""
+    s = Step(pk, [random.Random(i).randint(0, 300) for i in range(86)], hkv=1, r=33, d=256, page=64, cap=4096)
+    ws = torch.empty(pk.pk_kv16_workspace_bytes(s.cfg, 4096), dtype=torch.uint8, device="cuda")
+    for bound in (4096, 3049, 3048, 2000, 300):
+        s.attend(bound=bound, workspace=ws)
+
+
 # ---- prompts -----------------------------------------------------------------------------------------------------------------
 
 def run_prompts(pk, lens, hkv=2, r=4, d=128, dtype=torch.float16, scale=None, cap=0.0, window=0, slopes=False, seed=0, before=0, behind=0, spoil=None, q=None):
