@@ -778,6 +778,10 @@ class PagesConfig:
         object.__setattr__(self, "_parts", {})
 
 
+def _pages_valid(cfg: PagesConfig):
+    _need(cfg.workspace_bytes > 0, f"not a configuration of pages: {cfg}")
+
+
 class PagePool:
     """A pool of pages: `table` int32 [n_seq, pages_per_seq] (what the caches take as page_table), `free` int32 [n_pages], a stack of the free pages, and
     `n_free` int32 [4] (how many there are, 0, 0, 0).  A new pool has all pages free.  The tensors may be ones that the caller has; they
@@ -785,6 +789,7 @@ class PagePool:
 
     def __init__(self, cfg: PagesConfig, device="cuda", table: torch.Tensor | None = None, free: torch.Tensor | None = None, n_free: torch.Tensor | None = None):
         self.cfg = cfg
+        _pages_valid(cfg)
         if table is not None:
             device = table.device
         self.table = torch.zeros((cfg.n_seq, cfg.pages_per_seq), dtype=torch.int32, device=device) if table is None else table
@@ -828,6 +833,7 @@ def _pages_views(cfg: PagesConfig, n_tokens: int, buf: torch.Tensor, at) -> Page
 
 def pk_pages_plan(cfg: PagesConfig, n_tokens: int, device="cuda") -> PagesPlan:
     """Memory for a plan (to be passed to pk_pages_update as `out`, where a step is captured once and replayed)."""
+    _pages_valid(cfg)
     at = _pages_parts(cfg, n_tokens)
     return _pages_views(cfg, n_tokens, torch.empty(at[5], dtype=torch.int32, device=device), at)
 

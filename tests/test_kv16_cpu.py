@@ -209,6 +209,20 @@ def test_binding_refuses(pk):
     assert all(p % 16 == parts[0][0] % 16 for p, _ in parts) and all(a + n <= b for (a, n), (b, _) in zip(parts, parts[1:]))
 
 
+@pytest.mark.parametrize("change", [dict(n_seq=0), dict(n_seq=65536), dict(page_tokens=24), dict(n_pages=0), dict(n_pages=1 << 27), dict(pages_per_seq=0)])
+def test_binding_refuses_bad_pages(pk, change, monkeypatch):
+    """A configuration that the library refuses makes no pool and no plan, as it makes no cache; a step with memory of the caller's comes to an error of the binding's own."""
+    cfg = pk.PagesConfig(**{**dict(n_seq=4, page_tokens=16, n_pages=9, pages_per_seq=3), **change})
+    monkeypatch.setattr(pk, "_stream_of", lambda device: None)
+    n = cfg.n_seq
+    states, counts, starts = (torch.zeros(shape, dtype=torch.int32) for shape in ((n, 4), n, n + 1))
+    rows = torch.zeros(4, dtype=torch.int32)
+    with pytest.raises(ValueError, match="not a configuration"):
+        pk.pk_pages_update(cfg, pk.PagePool(cfg, device="cpu"), states, counts, 4, out=pk.PagesPlan(starts, rows, rows.clone(), counts.clone()))
+    with pytest.raises(ValueError, match="not a configuration"):
+        pk.pk_pages_plan(cfg, 4, "cpu")
+
+
 def test_reference_pages_belong_to_one_sequence():
     rng = random.Random(5)
     for _ in range(40):
