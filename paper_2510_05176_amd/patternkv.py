@@ -806,10 +806,11 @@ class PagePool:
 
 @dataclass
 class PagesPlan:
-    """What pk_pages_update leaves for a step's other calls, int32 on the device: starts [n_seq + 1], slots and positions [n_tokens], taken [n_seq]."""
+    """What pk_pages_update leaves for a step's other calls, int32 on the device: starts [n_seq + 1], slots and positions [n_tokens], taken [n_seq].
+    A plan of the caller's may have None for the positions; they are not written then."""
     starts: torch.Tensor
     slots: torch.Tensor
-    positions: torch.Tensor
+    positions: torch.Tensor | None
     taken: torch.Tensor
 
 
@@ -861,7 +862,8 @@ def pk_pages_update(cfg: PagesConfig, pool: PagePool, states: torch.Tensor, coun
         out = _pages_views(cfg, n_tokens, buf, at)
     else:
         starts, slots = _numbers(out.starts, (n + 1,), dev, "starts"), _numbers(out.slots, (n_tokens,), dev, "slots")
-        positions, taken = _numbers(out.positions, (n_tokens,), dev, "positions"), _numbers(out.taken, (n,), dev, "taken")
+        positions = None if out.positions is None else _numbers(out.positions, (n_tokens,), dev, "positions")
+        taken = _numbers(out.taken, (n,), dev, "taken")
         if workspace is None:
             workspace = _workspace_of(None, need, dev)
     if workspace is not None:

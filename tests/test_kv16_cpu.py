@@ -223,6 +223,23 @@ def test_binding_refuses_bad_pages(pk, change, monkeypatch):
         pk.pk_pages_plan(cfg, 4, "cpu")
 
 
+def test_binding_passes_a_plan_without_positions(pk, monkeypatch):
+    """The C call takes none; so does the binding, where the caller's plan has none."""
+    cfg = pk.PagesConfig(n_seq=4, page_tokens=16, n_pages=9, pages_per_seq=3)
+    calls = []
+
+    class Lib:
+        def pk_pages_update(self, *args):
+            calls.append(args)
+            return OK
+    pool, states, counts, plan = pk.PagePool(cfg, device="cpu"), torch.zeros(4, 4, dtype=torch.int32), torch.zeros(4, dtype=torch.int32), pk.pk_pages_plan(cfg, 5, "cpu")
+    plan.positions = None
+    monkeypatch.setattr(pk, "_stream_of", lambda device: None)
+    monkeypatch.setattr(pk, "_lib", Lib())
+    assert pk.pk_pages_update(cfg, pool, states, counts, 5, out=plan) is plan
+    assert calls[0][6:10] == (plan.starts.data_ptr(), plan.slots.data_ptr(), None, plan.taken.data_ptr())
+
+
 def test_reference_pages_belong_to_one_sequence():
     rng = random.Random(5)
     for _ in range(40):

@@ -130,6 +130,17 @@ def test_pages_take_whatever_is_there(pk):
         assert (plan.taken >= 0).all() and (plan.taken <= per_seq * page).all()
 
 
+@pytest.mark.parametrize("n_seq,n_tokens", [(6, 400), (6, 5000), (1100, 3000)])
+def test_steps_without_positions(pk, n_seq, n_tokens):
+    """A plan of the caller's that has none, in one launch and in two."""
+    p = Paged(pk, n_seq, 16, 60 + n_seq, 20)
+    out = pk.pk_pages_plan(p.cfg, n_tokens)
+    out.positions = None
+    for counts in ([100, 3, 0, 200, 16, 40], [5, -3, 70, -200, 1, 100]):
+        plan, want = p.update(counts + [1] * (n_seq - 6), n_tokens, out=out)
+        p.check(plan, want)
+
+
 # ---- append ------------------------------------------------------------------------------------------------------------------
 
 def packed(n, heads, d, dtype, seed, parts=1, extra=8):
