@@ -185,7 +185,7 @@ __global__ __launch_bounds__((PromptShape<D, GROUPS>::kThreads), D == 256 ? 1 : 
     const char *k_from = static_cast<const char *>(a.k) + 2 * (start * a.k_token + kvh * a.k_head);
     const char *v_from = static_cast<const char *>(a.v) + 2 * (start * a.v_token + kvh * a.v_head);
     // A tile's way into LDS, without registers in between.  Lane l of a wave's request writes 16 l bytes behind the request's place; what it reads is its to choose.
-    // (The compiler would wait for it before every read from LDS that follows, whatever tile that is of; it has no registers to wait for, and arrive() waits for it.  m0 is a reserved register, set before each use.)
+    // (The compiler would wait for it before every read from LDS that follows, whatever tile that is of; it has no registers to wait for, and arrive() waits for it.  m0, where the place goes, is an operand, so that the compiler writes it.)
     // A lane's part of the addresses is the same for every whole tile, where strides let it fit 32 bits.
     uint32_t k_lane[S::kPer], v_lane[S::kPer];
 #pragma unroll
@@ -203,7 +203,7 @@ __global__ __launch_bounds__((PromptShape<D, GROUPS>::kThreads), D == 256 ? 1 : 
         return D != 96 || ((slot % S::kSlots) ^ (v ? S::v_swizzle(key) : S::k_swizzle(key))) < D / 8;
     };
     const auto request_whole = [&](int j, const char *tile_from, const uint32_t (&lane_at)[S::kPer], const char *to, bool v) {
-        if (has_piece(j, v)) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "s"(place_of_piece(to, j)), "v"(lane_at[j]), "s"(tile_from) : "memory");
+        if (has_piece(j, v)) asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" : : "{m0}"(place_of_piece(to, j)), "v"(lane_at[j]), "s"(tile_from) : "memory");
     };
     // a tile that the sequence ends in, or with strides that do not fit: all of it
     const auto request_slowly = [&](const char *from, int64_t token, int t0, const char *to, bool v) {
@@ -211,7 +211,7 @@ __global__ __launch_bounds__((PromptShape<D, GROUPS>::kThreads), D == 256 ? 1 : 
         for (int j = 0; j < S::kPer; ++j) {
             const int slot = tid + j * S::kLoaders, key = slot / S::kSlots, piece = (slot % S::kSlots) ^ (v ? S::v_swizzle(key) : S::k_swizzle(key));
             const int64_t t = min(t0 + key, len - 1);   // (behind the last token: it again; those keys are masked)
-            if (has_piece(j, v)) asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(place_of_piece(to, j)), "v"(from + 2 * t * token + 16 * piece) : "memory");
+            if (has_piece(j, v)) asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "{m0}"(place_of_piece(to, j)), "v"(from + 2 * t * token + 16 * piece) : "memory");
         }
     };
     const bool loads = S::kGroups == 1 || wave < 4;

@@ -126,3 +126,62 @@ def test_append_counts_a_workgroup_when_all_its_waves_have_the_state(tmp_path):
             found.update({k: v for k, v in _arrives_without_a_barrier(r.stdout).items() if "fp8_append_kernel" in k})
     assert len(found) == 24
     assert [k for k, v in found.items() if v and "ILi64ELi32E" not in k] == []
+
+
+def _lds_requests(asm):
+    """(loads from memory to LDS, those that are not a wait state or more behind a scalar instruction that wrote m0 in the same run of instructions)"""
+    seen, bad, kernel, since, by = 0, [], None, None, None
+    for line in asm.splitlines():
+        line = line.split("//")[0].strip()
+        start = re.match(r"^[0-9a-f]* ?<(.*)>:", line)
+        if start:
+            kernel = kernel if re.fullmatch(r"L\d+", start.group(1)) else start.group(1)
+            since = by = None   # (a branch may come from anywhere)
+            continue
+        op, _, rest = line.partition(" ")
+        if not op or not re.match(r"[a-z]+_", op):
+            continue
+        if re.match(r"(global|buffer)_load_lds|buffer_load.*\blds\b", line):
+            seen += 1
+            if since is None or since < 1 or not by.startswith("s_"):
+                bad.append((kernel, by, since, line))
+        if re.match(r"m0\b", rest):
+            since, by = 0, op
+        elif since is not None:
+            since += 1 + int(rest) if op == "s_nop" else 1
+    return seen, bad
+
+
+def test_the_check_sees_a_missing_m0():
+    load = " global_load_lds_dwordx4 v1, s[0:1]\n"
+    assert _lds_requests("0 <_Zkernel>:\n s_mov_b32 m0, s4\n s_nop 0\n" + load) == (1, [])
+    assert _lds_requests("0 <_Zkernel>:\n s_add_i32 m0, s4, 0x400\n v_mov_b32_e32 v1, v2\n" + load) == (1, [])
+    for before in ("", " s_mov_b32 m0, s4\n", " v_readfirstlane_b32 m0, v4\n s_nop 0\n", " s_mov_b32 m0, s4\n s_nop 0\n0 <L0>:\n"):
+        assert len(_lds_requests("0 <_Zkernel>:\n" + before + load)[1]) == 1
+
+
+def test_loads_to_lds_have_their_place(tmp_path):
+    """A load from memory to LDS takes its place from m0, which a scalar instruction writes one wait state or more before it."""
+    shutil.copy(LIB, tmp_path / "lib.so")
+    subprocess.run([OBJDUMP, "--offloading", "lib.so"], cwd=tmp_path, check=True, capture_output=True)
+    total, bad = 0, []
+    for f in sorted(os.listdir(tmp_path)):
+        if f.endswith("gfx950") and b"prompt_kernel" in (tmp_path / f).read_bytes():
+            r = subprocess.run([OBJDUMP, "-d", "--mcpu=gfx950", "--no-show-raw-insn", "--symbolize-operands", f], cwd=tmp_path, check=True,
+                               capture_output=True, text=True)
+            seen, found = _lds_requests(r.stdout)
+            total, bad = total + seen, bad + found
+    assert total > 0
+    assert not bad, (len(bad), bad[:4])
+
+
+def test_no_assembly_writes_m0_behind_the_compilers_back():
+    """m0 is a reserved register, which no list of clobbers takes; as an operand ("{m0}") the compiler writes it itself and knows of it."""
+    csrc, found = os.path.join(ROOT, "paper_2510_05176_amd", "csrc"), []
+    for f in sorted(os.listdir(csrc)):
+        with open(os.path.join(csrc, f)) as text:
+            for statement in re.findall(r"\basm\b(?:\s+volatile)?\s*\((.*?)\);", text.read(), re.S):
+                template = "".join(re.findall(r'"((?:[^"\\]|\\.)*)"', statement.split(" : ", 1)[0]))
+                if re.search(r"\bm0\b", template.replace("\\n", "\n").replace("\\t", "\t")):
+                    found.append((f, template))
+    assert not found, found
