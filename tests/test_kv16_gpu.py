@@ -326,6 +326,17 @@ def test_attention_of_many_sequences(pk):
         Step(pk, lens, hkv=1, r=2, d=64, page=16).attend()
 
 
+@pytest.mark.parametrize("hkv,n_seq,n", [(1, 257, 6000), (16, 130, 2500), (32, 64, 2100), (8, 256, 1500)])
+def test_a_long_sequence_among_many(pk, hkv, n_seq, n):
+    """More (sequence, KV head) pairs than the keys are dealt out over: one workgroup each, whatever its length."""
+    rng = random.Random(hkv)
+    lens = [rng.choice([0, 1, rng.randint(1, 60)]) for _ in range(n_seq)]
+    lens[n_seq // 3] = n
+    s = Step(pk, lens, hkv=hkv, r=1, d=64, page=32)
+    s.attend()
+    s.attend(window=n - 77, slopes=True)
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 def test_attention_of_large_and_small_scores(pk, dtype):
     """Scores of 2^20 and more (rounded ones; results stay finite and are some token's value), of no size at all, and values near the type's largest."""
@@ -479,6 +490,17 @@ def test_prompts_of_many_rows(pk, dtype, d, how):
         for i, t in ((9, 100), (10, 0), (10, 333), (10, 639), (11, 60)):
             vt[starts[i] + t, t % 4, 7] = (math.nan, math.inf, -math.inf)[t % 3]
     run_prompts(pk, lens, hkv=4, r=16, d=d, dtype=dtype, behind=5, spoil=spoil, **how)
+
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("d", [96, 128])
+@pytest.mark.parametrize("n_seq,most,r", [(300, 25, 4), (70, 120, 4), (2100, 3, 8)])
+def test_many_short_prompts_of_many_rows(pk, dtype, d, n_seq, most, r):
+    """Rows enough in all for workgroups of two groups of waves, few of them in a sequence: most of a workgroup's waves have none."""
+    rng = random.Random(n_seq)
+    lens = [rng.choice([0, 1, rng.randint(1, most), most]) for _ in range(n_seq)]
+    hkv = -(-512 * 256 // (sum(lens) * r))
+    run_prompts(pk, lens, hkv=hkv, r=r, d=d, dtype=dtype, behind=3)
 
 
 def test_a_long_prompt(pk):
