@@ -597,7 +597,7 @@ typedef struct {
 /* Bytes of one of k and v.  0 for an invalid configuration.  Host-only. */
 uint64_t pk_kv16_cache_bytes(const pk_kv16_config *cfg);
 
-/* Bytes of workspace of pk_kv16_attention with that bound, not shrinking as the bound grows.  0 for an invalid configuration or bound.  Host-only. */
+/* Bytes of workspace of pk_kv16_attention with that bound or a smaller one.  0 for an invalid configuration or bound.  Host-only. */
 size_t pk_kv16_workspace_bytes(const pk_kv16_config *cfg, int64_t bound);
 
 /*
@@ -611,13 +611,15 @@ pk_status pk_kv16_append(const pk_kv16_config *cfg, const pk_kv16_cache *cache, 
 
 /*
  * Attention of one token per sequence, the last one that the cache holds, over the tokens held: out = softmax(scores) V.
- *   bound      host: no sequence holds more tokens than this (t_capacity is always right); sizes the launch and the workspace.  Results do not depend
+ *   bound      host: no sequence holds more tokens than this (t_capacity is always right); sizes the launch and the workspace, and with 256 channels and
+ *              more than 16 query heads per KV head picks the kernel's form (a bound near what is held is the faster one).  Results do not depend
  *              on sequences staying below it, only the balance of the work does.
  *   q, qs      queries, (seq, head) at seq * qs.seq + head * qs.head; out, os: results in the same type; `token` is not used
  *   scores     as for the 8-bit cache; positions are the tokens' numbers in the sequence
  *   lse        optional float [n_seq][n_q_heads]: log-sum-exp of the scores
  * A sequence that holds no token has out = 0 and lse = -inf.  Slots behind the tokens held never contribute, whatever they hold, nor do tokens that the window masks.
- * Strides of 0 are taken in the inputs; in `out` none is shorter than a vector.  Scores and outputs are accumulated in binary32; softmax
+ * Strides of 0 are taken in the inputs; in `out` none is shorter than a vector, and its vectors do not overlap.  Scores and the scale, times
+ * log2 e, lie within binary32 (beyond it a result may be NaN).  Scores and outputs are accumulated in binary32; softmax
  * numerators are rounded to the 16-bit type (fp16: off by up to 2^-11 of themselves, or 2^-36 of the largest one where they are smaller; bf16: 2^-8), their
  * sum, which makes the log-sum-exp, is not.  Finite values have no result beyond the type's
  * largest; an infinite one that is seen makes it infinite, or NaN where its numerator rounds to 0.  `out` does not overlap with the inputs.

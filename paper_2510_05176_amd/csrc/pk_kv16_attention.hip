@@ -311,7 +311,8 @@ __global__ __launch_bounds__(64 * NW, D == 256 && RT == 2 ? 1 : 2) void kv16_att
 
 // 16 query heads per tile, two tiles share what is read.  With 256 channels they take a SIMD's registers for one wave, which pays over many tokens (16 sequences of
 // 16k tokens, two KV heads of 32 heads each, 131 -> 114 us; of 10k tokens and 33 heads 152 -> 102; 32 of up to 20k, 20 heads, 113 -> 90; 256k tokens of all KV heads
-// 61.5 and 59.7, one sequence of 128k and two KV heads 64.4 and 66.1; but 160k with a window 39.9 -> 44.7, 4000 tokens 18 -> 24).
+// 61.5 and 59.7, one sequence of 128k and two KV heads 64.4 and 66.1; but 160k with a window 39.9 -> 44.7, 4000 tokens 18 -> 24).  The tokens are the bound's, the window or not: two KV heads of 24 over
+// 4000 tokens in a cache of 2^18 take 21.7 us with the capacity as the bound, 17.8 with 4000.
 int tiles_of(int64_t r, int d, int64_t tokens) { return r <= 16 || (d == 256 && tokens <= kOneTileTokens) ? 1 : 2; }
 
 template <int D, int RT, bool BF16>
@@ -344,6 +345,8 @@ hipError_t launch_d(Fp8AttentionArgs &a, hipStream_t s)
 // Runs for one workgroup per CU where a run stays in one or two sequences (16 sequences x 32k tokens 354 us, 361 with two workgroups per CU; one of 32k 31 and 35, of
 // 128k 103 and 107), for two where it goes through more, each with its end (64 sequences of up to 6000 tokens 130 and 121; of up to 2000 56 and 53).  Three and four
 // per CU: 364 and 362, 122 and 126.  (Short caches whole by eight waves, with nothing to merge: 22.5 us for 2k tokens of 8 heads where runs of 256 take 14.7.)
+// From four sequences to a run on, and beyond kMostSeqs, a workgroup has a sequence of a KV head whatever its length (256 sequences of 8 KV heads, 128 of 16, 64 of 32): lengths of 1 to
+// 6000 make little of it (300 sequences of 8 KV heads 657 us, their bytes 630), but one of 32k tokens among 255 of 500 takes 515 us, among 199, which are dealt, 111.
 int64_t kv16_attention_parts(int64_t n_seq, int64_t n_kv_heads, int64_t r, int d, int64_t bound)
 {
     const int64_t rows = 16 * tiles_of(r, d, n_seq * n_kv_heads * bound), across = n_kv_heads * ((r + rows - 1) / rows);   // workgroups per run

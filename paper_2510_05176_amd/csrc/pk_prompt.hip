@@ -7,9 +7,9 @@
 // walk together, two of each; V's operands are read transposed.  Tiles go to LDS without registers in between, 16-byte pieces swapped within their rows so that
 // neither read has bank conflicts (none counted), and are asked for a phase before they are needed.
 //
-// The matrix instructions bound it, and beside them the numerators, some 4.5 vector instructions per score, of which a SIMD starts one in four to ten cycles: at 128
-// channels both take the same time, and two groups of waves that change places hide one behind the other; at 64 the numerators take twice the products' time.
-// One prompt of 32k tokens, 32 heads of 128 channels, 8.9 TFLOP: 7.4 ms, 1.2 PFLOP/s, where a library product of 16384 cubed reaches 1.31 to 1.35 (one group 8.2 ms,
+// The matrix instructions bound it, and beside them the numerators, 4.5 vector instructions per score of their own (5.2 with all others counted, 6.0 at 64 channels), of which
+// a SIMD starts one in four to ten cycles: at 128 channels both take the same time, and two groups of waves that change places hide one behind the other; at 64 the numerators take twice the products' time.
+// One prompt of 32k tokens, 32 heads of 128 channels, 8.9 TFLOP: 7.4 ms (7.3 to 8.1 from card to card), 1.2 PFLOP/s, where a library product of 16384 cubed reaches 1.31 to 1.35 (one group 8.2 ms,
 // tiles through registers 8.4).  The card's power is the last bound of it: the same launch over zeros, which take less, runs a quarter to a third faster.
 #include <cfloat>
 #include <type_traits>
@@ -504,6 +504,8 @@ __global__ __launch_bounds__((PromptShape<D, GROUPS>::kThreads), D == 256 ? 1 : 
 // prompt of 32k tokens, 32 heads of 128 channels 7.69 ms, one group 8.24; 16 of 512 tokens 79 and 81 us; but one of 1000 tokens 32 and 29, 2048 tokens of
 // one KV head 52 and 46.  With 64 channels (a packed batch 779 and 713 us) or a cap and distance bias (8k tokens 1146 and 907) the numerators are longer, and
 // two groups that wait for each other waste the matrix unit's time; 256 channels leave registers for one wave per SIMD.
+// Rows are those of the whole call, whatever a sequence has of them: 64 prompts of 128 tokens 58 and 60 us, but 70 of 64 tokens 45 and 42, and 300 of 20 tokens (80
+// rows in each workgroup of 256 or 128) 92 and 56.
 int groups_of(int64_t rows, int d, bool opt) { return (d == 96 || d == 128) && !opt && rows >= 512 * 256 ? 2 : 1; }
 
 template <int D, int GROUPS>
